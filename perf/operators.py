@@ -322,7 +322,7 @@ def run(s):
             return {"loss": loss, "lp": lp, "stats": stats, "dx": _logits_gradient(s["x"], y, s["tau"], row_stats, d_lp, None, None)}
         sr, T = _sr(), s["lp"].numel()
         sr.sr_policy_loss_logits(s["x"], s["y"], s["old"], s["ref"], s["adv"], s["weight"], s["row_start"], s["mask"], s["clip"][0], s["clip"][1], s["beta"], s["tau"],
-                                 loss=s["loss"], logp=s["lp"], d_logits=s["dx"], stats=s["stats"], workspace=_scratch(s, "loss_ws", lambda: sr.sr_policy_loss_workspace_bytes(T)))
+                                 loss=s["loss"], logp=s["lp"], d_logits=s["dx"], stats=s["stats"], workspace=_scratch(s, "loss_ws", lambda: sr.sr_policy_loss_logits_workspace_bytes(T)))
         return {"loss": s["loss"], "lp": s["lp"], "stats": s["stats"], "dx": s["dx"]}
     if not own:
         norm = s["flat"].float().square().sum(dtype=torch.float64).sqrt().float().reshape(1)

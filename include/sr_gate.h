@@ -38,13 +38,17 @@ extern "C" {
 #define SR_ERR_NULL (-1)           /* a required pointer is NULL */
 #define SR_ERR_BAD_N (-2)          /* N < 2 or N > SR_MAX_N, or n_groups < 0 */
 #define SR_ERR_BAD_K (-3)          /* K < 0, K > stride, K > SR_MAX_K, bad max_steps */
-#define SR_ERR_ALIGN (-4)          /* seqs not 16-byte aligned or stride % 4 != 0 */
+#define SR_ERR_ALIGN (-4)          /* seqs not 16-byte aligned or stride % 4 != 0; a pointer off its element type */
 #define SR_ERR_STATE_SIZE (-5)     /* incremental state buffer too small */
 #define SR_ERR_WORKSPACE (-6)      /* workspace NULL, misaligned or too small */
 #define SR_ERR_CUDA (-7)           /* a CUDA call failed; see sr_last_cuda_error() */
-#define SR_ERR_BAD_MODE (-8)       /* unknown norm_mode */
+#define SR_ERR_BAD_MODE (-8)       /* unknown norm_mode or loss mode */
 #define SR_ERR_SCRATCH_LIMIT (-9)  /* sr_gate_noalloc: problem needs more than the built-in scratch */
 #define SR_ERR_BAD_OFFSETS (-10)   /* sr_gate_host_packed: row_start malformed */
+#define SR_ERR_BAD_SIZE (-11)      /* sr_train.h: negative count, empty vocabulary, pitch < vocab */
+#define SR_ERR_BAD_DTYPE (-12)     /* sr_train.h: unknown element type */
+#define SR_ERR_BAD_VALUE (-13)     /* sr_train.h: temperature, clip range, beta, scale or max_norm out of range */
+#define SR_ERR_OVERLAP (-14)       /* sr_train.h: buffers that must not overlap do */
 
 /* limits */
 #define SR_MAX_N 32                /* rollouts per group */
@@ -62,6 +66,8 @@ extern "C" {
 #define SR_STATUS_NEG_LEN 1        /* a negative length was treated as 0 */
 #define SR_STATUS_STEP_OVERFLOW 2  /* an action arrived for a rollout already at max_steps; ignored */
 #define SR_STATUS_BAD_STATE 4      /* incremental state header does not match the call; step skipped */
+#define SR_STATUS_BAD_TARGET 8     /* a target token >= vocab was treated as one that does not count */
+#define SR_STATUS_NONFINITE 16     /* the gradient norm is not finite; gradients were not scaled */
 
 int sr_version(void);
 const char* sr_strerror(int code);      /* static string */

@@ -1,4 +1,4 @@
-"""Thin binding of the sr_gate C ABI (include/sr_gate.h, include/sr_probe.h).
+"""Thin binding of the sr_gate C ABI (include/sr_gate.h, include/sr_train.h, include/sr_probe.h).
 
 Argument marshalling only: every step of the path runs in the CUDA library.  The calls
 a program makes per batch or per step go through a compiled extension
@@ -24,13 +24,18 @@ SR_ERR_NULL, SR_ERR_BAD_N, SR_ERR_BAD_K, SR_ERR_ALIGN = -1, -2, -3, -4
 SR_ERR_STATE_SIZE, SR_ERR_WORKSPACE, SR_ERR_CUDA, SR_ERR_BAD_MODE = -5, -6, -7, -8
 SR_ERR_SCRATCH_LIMIT = -9
 SR_ERR_BAD_OFFSETS = -10
+SR_ERR_BAD_SIZE, SR_ERR_BAD_DTYPE, SR_ERR_BAD_VALUE, SR_ERR_OVERLAP = -11, -12, -13, -14
 SR_NORM_MAXLEN, SR_NORM_NONE = 0, 1
 SR_NO_ACTION = -(2 ** 31)
 SR_STATUS_NEG_LEN, SR_STATUS_STEP_OVERFLOW, SR_STATUS_BAD_STATE = 1, 2, 4
+SR_STATUS_BAD_TARGET, SR_STATUS_NONFINITE = 8, 16
+SR_DTYPE_F32, SR_DTYPE_BF16, SR_DTYPE_F16 = 0, 1, 2
+SR_LOSS_SUM, SR_LOSS_TOKEN_MEAN, SR_LOSS_ROLLOUT_MEAN = 0, 1, 2
 SR_MAX_N, SR_MAX_K, SR_MAX_INCR_STEPS = 32, 1024, 32
 SR_PROBE_LOGIC, SR_PROBE_ADD, SR_PROBE_MIX = 0, 1, 2
 
 _vp, _i32, _f64, _f32, _sz = ctypes.c_void_p, ctypes.c_int32, ctypes.c_double, ctypes.c_float, ctypes.c_size_t
+_i64 = ctypes.c_int64
 
 _SIGNATURES = {
     "sr_version": (ctypes.c_int, []),
@@ -62,6 +67,19 @@ _SIGNATURES = {
     "sr_savings_fraction": (ctypes.c_double, [ctypes.c_int64, ctypes.c_int64, _i32, _i32]),
     "sr_dilution_gain": (ctypes.c_double, [_f64, _f64]),
     "sr_grpo_advantage": (ctypes.c_int, [_vp, _vp, _i32, _i32, _f32, _vp, _vp, _vp]),
+    "sr_token_logprob": (ctypes.c_int, [_vp, _i32, _i32, _i32, _i64, _vp, _f64, _vp, _vp, _vp, _vp, _vp]),
+    "sr_token_logprob_backward": (ctypes.c_int, [_vp, _i32, _i32, _i32, _i64, _vp, _vp, _vp, _vp, _vp, _f64, _vp, _i64, _vp]),
+    "sr_loss_weights": (ctypes.c_int, [_vp, _vp, _i32, _vp, _i32, _i32, _i32, _f64, _vp, _vp, _vp, _sz, _vp]),
+    "sr_loss_weights_workspace_bytes": (_sz, [_i32]),
+    "sr_policy_loss": (ctypes.c_int, [_vp, _vp, _vp, _vp, _vp, _vp, _i32, _vp, _i32, _f64, _f64, _f64, _vp, _vp, _vp, _vp,
+                                      _sz, _vp]),
+    "sr_policy_loss_workspace_bytes": (_sz, [_i32]),
+    "sr_policy_loss_logits": (ctypes.c_int, [_vp, _i32, _i32, _i32, _i64, _vp, _vp, _vp, _vp, _vp, _vp, _i32, _vp, _f64, _f64,
+                                             _f64, _f64, _vp, _vp, _vp, _i64, _vp, _vp, _vp, _sz, _vp]),
+    "sr_policy_loss_logits_workspace_bytes": (_sz, [_i32]),
+    "sr_grad_norm": (ctypes.c_int, [_vp, _vp, _vp, _i32, _vp, _vp, _sz, _vp]),
+    "sr_grad_norm_workspace_bytes": (_sz, [_i32]),
+    "sr_clip_grads": (ctypes.c_int, [_vp, _vp, _vp, _i32, _vp, _f64, _vp, _vp, _vp]),
     "sr_gate_stages": (ctypes.c_int, [_vp, _vp, _i32, _i32, _i32, _i32, _f64, _i32, _vp, _vp, _vp, _vp,
                                       _vp, _vp, _sz, _vp, _vp]),
     "sr_probe_int32": (ctypes.c_int, [_i32, _i32, _i32, _i32, _vp, _vp]),
@@ -294,6 +312,78 @@ def sr_dilution_gain(before: float, after: float) -> float:
 def sr_grpo_advantage(rewards: torch.Tensor, drop_mask: Optional[torch.Tensor], eps: float, *,
                       adv: torch.Tensor, zero_var: Optional[torch.Tensor] = None, stream=None) -> None:
     _check(_native().sr_grpo_advantage(rewards, drop_mask, eps, adv, zero_var, stream))
+
+
+def sr_token_logprob(logits: torch.Tensor, targets: torch.Tensor, temperature: float = 1.0, *, logp: torch.Tensor,
+                     row_stats: Optional[torch.Tensor] = None, entropy: Optional[torch.Tensor] = None,
+                     status: Optional[torch.Tensor] = None, stream=None) -> None:
+    """logits [T, V] (float32, bfloat16 or float16; rows may lie apart), targets int32 [T], negative = does not count.
+    logp float32 [T]; row_stats float32 [T, 2] is what sr_token_logprob_backward starts from."""
+    _check(_native().sr_token_logprob(logits, targets, temperature, logp, row_stats, entropy, status, stream))
+
+
+def sr_token_logprob_backward(logits: torch.Tensor, targets: torch.Tensor, row_stats: torch.Tensor,
+                              entropy: Optional[torch.Tensor], d_logp: torch.Tensor, d_entropy: Optional[torch.Tensor],
+                              temperature: float = 1.0, *, d_logits: torch.Tensor, stream=None) -> None:
+    """d_logits of the logits' type and shape; may be the logits themselves."""
+    _check(_native().sr_token_logprob_backward(logits, targets, row_stats, entropy, d_logp, d_entropy, temperature,
+                                               d_logits, stream))
+
+
+def sr_loss_weights_workspace_bytes(n_rollouts: int) -> int:
+    return int(load().sr_loss_weights_workspace_bytes(n_rollouts))
+
+
+def sr_loss_weights(row_start: torch.Tensor, mask: Optional[torch.Tensor], drop_mask: Optional[torch.Tensor], N: int,
+                    mode: int = SR_LOSS_TOKEN_MEAN, scale: float = 1.0, *, weight: torch.Tensor,
+                    counts: Optional[torch.Tensor] = None, workspace: torch.Tensor = None, stream=None) -> None:
+    """row_start int64 [G * N + 1], mask uint8 [T], drop_mask uint8 [G] (sr_gate's stop) -> weight float32 [G * N]."""
+    _check(_native().sr_loss_weights(row_start, mask, drop_mask, N, mode, scale, weight, counts, workspace, stream))
+
+
+def sr_policy_loss_workspace_bytes(n_tokens: int) -> int:
+    return int(load().sr_policy_loss_workspace_bytes(n_tokens))
+
+
+def sr_policy_loss(logp: torch.Tensor, logp_old: Optional[torch.Tensor], logp_ref: Optional[torch.Tensor],
+                   adv: torch.Tensor, weight: torch.Tensor, row_start: torch.Tensor, mask: Optional[torch.Tensor],
+                   clip_low: float, clip_high: float, beta: float, *, loss: torch.Tensor,
+                   d_logp: Optional[torch.Tensor] = None, stats: Optional[torch.Tensor] = None,
+                   workspace: torch.Tensor = None, stream=None) -> None:
+    """Clipped policy loss with a KL term over packed rollouts, its gradient (d_logp) and four figures (stats)."""
+    _check(_native().sr_policy_loss(logp, logp_old, logp_ref, adv, weight, row_start, mask, clip_low, clip_high, beta,
+                                    loss, d_logp, stats, workspace, stream))
+
+
+def sr_policy_loss_logits_workspace_bytes(n_tokens: int) -> int:
+    return int(load().sr_policy_loss_logits_workspace_bytes(n_tokens))
+
+
+def sr_policy_loss_logits(logits: torch.Tensor, targets: torch.Tensor, logp_old: Optional[torch.Tensor],
+                          logp_ref: Optional[torch.Tensor], adv: torch.Tensor, weight: torch.Tensor,
+                          row_start: torch.Tensor, mask: Optional[torch.Tensor], clip_low: float, clip_high: float,
+                          beta: float, temperature: float = 1.0, *, loss: torch.Tensor, logp: torch.Tensor,
+                          d_logits: torch.Tensor, stats: Optional[torch.Tensor] = None,
+                          status: Optional[torch.Tensor] = None, workspace: torch.Tensor = None, stream=None) -> None:
+    """sr_policy_loss from logits, with the gradient of the logits (may be written over them) in the same pass."""
+    _check(_native().sr_policy_loss_logits(logits, targets, logp_old, logp_ref, adv, weight, row_start, mask, clip_low,
+                                           clip_high, beta, temperature, loss, logp, d_logits, stats, status, workspace,
+                                           stream))
+
+
+def sr_grad_norm_workspace_bytes(n_tensors: int) -> int:
+    return int(load().sr_grad_norm_workspace_bytes(n_tensors))
+
+
+def sr_grad_norm(grads, *, norm: torch.Tensor, workspace: torch.Tensor = None, stream=None) -> None:
+    """grads: list of dense float32, bfloat16 or float16 tensors; norm float32 [1]: their L2 norm together."""
+    _check(_native().sr_grad_norm(grads, norm, workspace, stream))
+
+
+def sr_clip_grads(grads, norm: torch.Tensor, max_norm: float, *, out=None, status: Optional[torch.Tensor] = None,
+                  stream=None) -> None:
+    """grads times min(1, max_norm / (norm + 1e-6)), in place or into ``out`` (a list alike)."""
+    _check(_native().sr_clip_grads(grads, norm, max_norm, out, status, stream))
 
 
 def sr_probe_int32(variant: int, iters: int, blocks: int, threads: int, sink: torch.Tensor,

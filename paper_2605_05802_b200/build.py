@@ -16,7 +16,8 @@ LIB = os.path.join(HERE, "libsr_gate.so")
 NATIVE = os.path.join(HERE, "_native.so")
 BINDING = os.path.join(CSRC, "torch_binding.cpp")
 SOURCES = ["api.cu", "gate_single.cu", "gate_multi.cu", "incremental.cu", "advantage.cu", "probe.cu",
-           "gate_noalloc.cu", "signals.cu", "gate_packed.cu", "compact.cu"]
+           "gate_noalloc.cu", "signals.cu", "gate_packed.cu", "compact.cu", "train.cu", "logprob.cu",
+           "policy.cu", "grads.cu"]
 
 
 def _stale(target: str, sources) -> bool:

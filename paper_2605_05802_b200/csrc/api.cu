@@ -57,13 +57,17 @@ const char* sr_strerror(int code) {
         case SR_ERR_NULL: return "a required pointer is NULL";
         case SR_ERR_BAD_N: return "N outside 2..32 or negative group count";
         case SR_ERR_BAD_K: return "K / stride / max_steps out of range";
-        case SR_ERR_ALIGN: return "seqs must be 16-byte aligned and stride a multiple of 4";
+        case SR_ERR_ALIGN: return "seqs must be 16-byte aligned and stride a multiple of 4, every pointer on its element type";
         case SR_ERR_STATE_SIZE: return "incremental state buffer too small";
         case SR_ERR_WORKSPACE: return "workspace missing, misaligned or too small";
         case SR_ERR_CUDA: return "a CUDA call failed (see sr_last_cuda_error)";
-        case SR_ERR_BAD_MODE: return "unknown norm_mode";
+        case SR_ERR_BAD_MODE: return "unknown norm_mode or loss mode";
         case SR_ERR_SCRATCH_LIMIT: return "problem needs more scratch than sr_gate_noalloc's built-in array";
         case SR_ERR_BAD_OFFSETS: return "row_start does not begin at 0, decreases, or exceeds rows x stride symbols";
+        case SR_ERR_BAD_SIZE: return "negative count, empty vocabulary, or a pitch below the vocabulary";
+        case SR_ERR_BAD_DTYPE: return "unknown element type";
+        case SR_ERR_BAD_VALUE: return "temperature, clip range, beta, scale or max_norm out of range";
+        case SR_ERR_OVERLAP: return "buffers overlap that must not";
         default: return "unknown error code";
     }
 }

@@ -1,0 +1,95 @@
+// Element types of logits and gradients: 16-byte vectors of them, and single ones.
+#pragma once
+
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <string.h>
+#include <type_traits>
+
+#include "common.cuh"
+#include "sr_train.h"
+
+namespace sr {
+
+__device__ __forceinline__ float to_float(float x) { return x; }
+__device__ __forceinline__ float to_float(__nv_bfloat16 x) { return __bfloat162float(x); }
+__device__ __forceinline__ float to_float(__half x) { return __half2float(x); }
+template <typename T>
+__device__ __forceinline__ T from_float(float x);             // to nearest even
+template <>
+__device__ __forceinline__ float from_float<float>(float x) { return x; }
+template <>
+__device__ __forceinline__ __nv_bfloat16 from_float<__nv_bfloat16>(float x) { return __float2bfloat16_rn(x); }
+template <>
+__device__ __forceinline__ __half from_float<__half>(float x) { return __float2half_rn(x); }
+
+// The elements of a 16-byte vector, in order.
+template <typename T>
+struct Vec {
+    static constexpr int kElems = 16 / (int)sizeof(T);
+};
+__device__ __forceinline__ void unpack(const uint4& v, float (&x)[4], float) {
+    x[0] = __uint_as_float(v.x); x[1] = __uint_as_float(v.y); x[2] = __uint_as_float(v.z); x[3] = __uint_as_float(v.w);
+}
+__device__ __forceinline__ void unpack(const uint4& v, float (&x)[8], __nv_bfloat16) {
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        x[2 * k] = __uint_as_float(w[k] << 16);
+        x[2 * k + 1] = __uint_as_float(w[k] & 0xFFFF0000u);
+    }
+}
+__device__ __forceinline__ void unpack(const uint4& v, float (&x)[8], __half) {
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        __half2 h;
+        memcpy(&h, &w[k], 4);
+        const float2 f = __half22float2(h);
+        x[2 * k] = f.x;
+        x[2 * k + 1] = f.y;
+    }
+}
+__device__ __forceinline__ uint4 pack(const float (&x)[4], float) {
+    return make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3]));
+}
+__device__ __forceinline__ uint4 pack(const float (&x)[8], __nv_bfloat16) {
+    uint32_t w[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const __nv_bfloat162 h = __floats2bfloat162_rn(x[2 * k], x[2 * k + 1]);
+        memcpy(&w[k], &h, 4);
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+__device__ __forceinline__ uint4 pack(const float (&x)[8], __half) {
+    uint32_t w[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const __half2 h = __floats2half2_rn(x[2 * k], x[2 * k + 1]);
+        memcpy(&w[k], &h, 4);
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+inline int dtype_bytes(int32_t dtype) { return dtype == SR_DTYPE_F32 ? 4 : dtype == SR_DTYPE_BF16 || dtype == SR_DTYPE_F16 ? 2 : 0; }
+
+// logprob.cu
+struct LogitsArgs {
+    const void* logits;
+    int32_t dtype, n_tokens, vocab;
+    int64_t pitch;
+    const int32_t* targets;
+    double temperature;
+};
+int launch_token_logprob(const LogitsArgs& a, float* logp, float* row_stats, float* entropy, int32_t* status, cudaStream_t s);
+int launch_token_logprob_backward(const LogitsArgs& a, const float* row_stats, const float* entropy, const float* d_logp, const float* d_entropy, void* d_logits,
+                                  int64_t d_pitch, cudaStream_t s);
+
+// grads.cu
+size_t grad_norm_workspace_bytes(int32_t n_tensors);
+int launch_grad_norm(const void* const* grads, const int64_t* counts, const int32_t* dtypes, int32_t n_tensors, float* norm, void* ws, cudaStream_t s);
+int launch_clip_grads(const void* const* grads, const int64_t* counts, const int32_t* dtypes, int32_t n_tensors, const float* norm, float max_norm,
+                      void* const* out, int32_t* status, cudaStream_t s);
+
+}  // namespace sr

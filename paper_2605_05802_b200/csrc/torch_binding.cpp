@@ -9,13 +9,16 @@
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 
+#include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <string>
+#include <vector>
 
 #include "sr_gate.h"
 #include "sr_probe.h"
+#include "sr_train.h"
 
 namespace {
 
@@ -33,6 +36,8 @@ const char* dtype_name(c10::ScalarType t) {
         case c10::ScalarType::Byte: return "torch.uint8";
         case c10::ScalarType::Float: return "torch.float32";
         case c10::ScalarType::Double: return "torch.float64";
+        case c10::ScalarType::Half: return "torch.float16";
+        case c10::ScalarType::BFloat16: return "torch.bfloat16";
         default: return c10::toString(t);
     }
 }
@@ -362,12 +367,252 @@ PyObject* py_grpo_advantage(PyObject*, PyObject* const* argv, Py_ssize_t argc) {
     });
 }
 
+// ------------------------------------------------------------------ the trainer's operators (sr_train.h)
+// These run on the device their tensors are on, whichever is current; all tensors of a call share it.
+struct OneDevice {
+    c10::cuda::OptionalCUDAGuard guard;
+    int index = -1;
+    const at::Tensor* add(const at::Tensor* t, const char* name) {
+        if (t == nullptr) return t;
+        if (!t->is_cuda()) raise(PyExc_ValueError, std::string(name) + " must be a CUDA tensor");
+        const int at = t->device().index();
+        if (index < 0) {
+            index = at;
+            guard.set_index((c10::DeviceIndex)at);
+        } else if (at != index) {
+            raise(PyExc_ValueError, std::string(name) + " is on another device than the tensors before it");
+        }
+        return t;
+    }
+};
+template <typename T>
+T* on(OneDevice& dev, const at::Tensor* t, c10::ScalarType type, int64_t need, const char* name) {
+    return static_cast<T*>(Args::address(dev.add(t, name), type, need, false, name));
+}
+void* scratch_on(OneDevice& dev, Args& a, size_t& bytes) {
+    const at::Tensor* t = dev.add(a.tensor("workspace"), "workspace");
+    bytes = t ? (size_t)t->numel() * t->element_size() : 0;
+    return Args::address(t, kAnyType, kAnySize, false, "workspace");
+}
+int32_t dtype_code(const at::Tensor& t, const char* name) {
+    switch (t.scalar_type()) {
+        case c10::ScalarType::Float: return SR_DTYPE_F32;
+        case c10::ScalarType::BFloat16: return SR_DTYPE_BF16;
+        case c10::ScalarType::Half: return SR_DTYPE_F16;
+        default: raise(PyExc_TypeError, std::string(name) + ": expected torch.float32, torch.bfloat16 or torch.float16, got " + dtype_name(t.scalar_type()));
+    }
+}
+int32_t count32(int64_t n, const char* name) {
+    if (n > INT32_MAX) raise(PyExc_ValueError, std::string(name) + " has more than 2^31 - 1 rows or elements a row");
+    return (int32_t)n;
+}
+
+// [tokens, vocabulary], rows apart by any pitch that does not make them overlap
+struct Logits {
+    void* data;
+    int32_t dtype, n, vocab;
+    int64_t pitch;
+    Logits(OneDevice& dev, const at::Tensor* t, const char* name) {
+        if (t == nullptr || t->dim() != 2) raise(PyExc_ValueError, std::string(name) + " must be [tokens, vocabulary]");
+        dtype = dtype_code(*dev.add(t, name), name);
+        n = count32(t->size(0), name);
+        vocab = count32(t->size(1), name);
+        if (vocab > 1 && t->stride(1) != 1) raise(PyExc_ValueError, std::string(name) + ": the logits of a row must be consecutive");
+        pitch = n > 1 ? t->stride(0) : vocab;
+        data = t->data_ptr();
+    }
+};
+Logits same_logits(OneDevice& dev, const at::Tensor* t, const Logits& as, const char* name) {
+    Logits l(dev, t, name);
+    if (l.dtype != as.dtype) raise(PyExc_TypeError, std::string(name) + " must have the logits' type");
+    if (l.n != as.n || l.vocab != as.vocab) raise(PyExc_ValueError, std::string(name) + " must have the logits' shape");
+    return l;
+}
+
+PyObject* py_token_logprob(PyObject*, PyObject* const* argv, Py_ssize_t argc) {
+    return guarded(argv, argc, 8, [](Args& a) {
+        OneDevice dev;
+        const Logits x(dev, a.tensor("logits"), "logits");
+        const int32_t* targets = on<int32_t>(dev, a.tensor("targets"), kI32, x.n, "targets");
+        const double temperature = a.real();
+        float* logp = on<float>(dev, a.tensor("logp"), kF32, x.n, "logp");
+        float* stats = on<float>(dev, a.tensor("row_stats"), kF32, 2 * (int64_t)x.n, "row_stats");
+        float* entropy = on<float>(dev, a.tensor("entropy"), kF32, x.n, "entropy");
+        int32_t* status = on<int32_t>(dev, a.tensor("status"), kI32, 1, "status");
+        void* s = a.stream();
+        return unlocked([&] { return sr_token_logprob(x.data, x.dtype, x.n, x.vocab, x.pitch, targets, temperature, logp, stats, entropy, status, s); });
+    });
+}
+
+PyObject* py_token_logprob_backward(PyObject*, PyObject* const* argv, Py_ssize_t argc) {
+    return guarded(argv, argc, 9, [](Args& a) {
+        OneDevice dev;
+        const Logits x(dev, a.tensor("logits"), "logits");
+        const int32_t* targets = on<int32_t>(dev, a.tensor("targets"), kI32, x.n, "targets");
+        const float* stats = on<float>(dev, a.tensor("row_stats"), kF32, 2 * (int64_t)x.n, "row_stats");
+        const float* entropy = on<float>(dev, a.tensor("entropy"), kF32, x.n, "entropy");
+        const float* d_logp = on<float>(dev, a.tensor("d_logp"), kF32, x.n, "d_logp");
+        const float* d_entropy = on<float>(dev, a.tensor("d_entropy"), kF32, x.n, "d_entropy");
+        const double temperature = a.real();
+        const Logits dx = same_logits(dev, a.tensor("d_logits"), x, "d_logits");
+        void* s = a.stream();
+        return unlocked([&] { return sr_token_logprob_backward(x.data, x.dtype, x.n, x.vocab, x.pitch, targets, stats, entropy, d_logp, d_entropy, temperature, dx.data, dx.pitch, s); });
+    });
+}
+
+int32_t rollouts_of(const at::Tensor* row_start) {
+    if (row_start == nullptr || row_start->numel() < 1) raise(PyExc_ValueError, "row_start needs an entry for every rollout and one more");
+    return count32(row_start->numel() - 1, "row_start");
+}
+
+PyObject* py_loss_weights(PyObject*, PyObject* const* argv, Py_ssize_t argc) {
+    return guarded(argv, argc, 10, [](Args& a) {
+        OneDevice dev;
+        const at::Tensor *rt = a.tensor("row_start"), *mt = a.tensor("mask"), *dt = a.tensor("drop_mask");
+        const int32_t rows = rollouts_of(rt), N = a.integer(), mode = a.integer();
+        if (N < 1 || rows % N) raise(PyExc_ValueError, "row_start needs n_groups * N + 1 entries");
+        const double scale = a.real();
+        const int64_t* start = on<int64_t>(dev, rt, kI64, kAnySize, "row_start");
+        const uint8_t* mask = on<uint8_t>(dev, mt, kU8, kAnySize, "mask");
+        const int32_t n = mt ? count32(mt->numel(), "mask") : 0;
+        const uint8_t* drop = on<uint8_t>(dev, dt, kU8, rows / N, "drop_mask");
+        float* weight = on<float>(dev, a.tensor("weight"), kF32, rows, "weight");
+        int64_t* counts = on<int64_t>(dev, a.tensor("counts"), kI64, 2, "counts");
+        size_t bytes;
+        void* ws = scratch_on(dev, a, bytes);
+        void* s = a.stream();
+        return unlocked([&] { return sr_loss_weights(start, mask, n, drop, rows / N, N, mode, scale, weight, counts, ws, bytes, s); });
+    });
+}
+
+// What the loss is computed over, as the calls take it: old and reference log-probabilities, advantages, weights, row starts, mask, clip range, beta.
+struct Batch {
+    const float *old_logp, *ref_logp, *adv, *weight;
+    const int64_t* row_start;
+    const uint8_t* mask;
+    int32_t rows;
+    double clip_low, clip_high, beta;
+    Batch(OneDevice& dev, Args& a, int32_t n) {
+        old_logp = on<float>(dev, a.tensor("logp_old"), kF32, n, "logp_old");
+        ref_logp = on<float>(dev, a.tensor("logp_ref"), kF32, n, "logp_ref");
+        const at::Tensor *at = a.tensor("adv"), *wt = a.tensor("weight"), *rt = a.tensor("row_start");
+        rows = rollouts_of(rt);
+        adv = on<float>(dev, at, kF32, rows, "adv");
+        weight = on<float>(dev, wt, kF32, rows, "weight");
+        row_start = on<int64_t>(dev, rt, kI64, kAnySize, "row_start");
+        mask = on<uint8_t>(dev, a.tensor("mask"), kU8, n, "mask");
+        clip_low = a.real();
+        clip_high = a.real();
+        beta = a.real();
+    }
+};
+
+PyObject* py_policy_loss(PyObject*, PyObject* const* argv, Py_ssize_t argc) {
+    return guarded(argv, argc, 15, [](Args& a) {
+        OneDevice dev;
+        const at::Tensor* t = a.tensor("logp");
+        if (t == nullptr) raise(PyExc_ValueError, "logp must be a tensor");
+        const float* logp = on<float>(dev, t, kF32, kAnySize, "logp");
+        const int32_t n = count32(t->numel(), "logp");
+        const Batch b(dev, a, n);
+        float* loss = on<float>(dev, a.tensor("loss"), kF32, 1, "loss");
+        float* d_logp = on<float>(dev, a.tensor("d_logp"), kF32, n, "d_logp");
+        float* stats = on<float>(dev, a.tensor("stats"), kF32, 4, "stats");
+        size_t bytes;
+        void* ws = scratch_on(dev, a, bytes);
+        void* s = a.stream();
+        return unlocked([&] { return sr_policy_loss(logp, b.old_logp, b.ref_logp, b.adv, b.weight, b.row_start, b.rows, b.mask, n, b.clip_low, b.clip_high, b.beta, loss, d_logp, stats, ws, bytes, s); });
+    });
+}
+
+PyObject* py_policy_loss_logits(PyObject*, PyObject* const* argv, Py_ssize_t argc) {
+    return guarded(argv, argc, 19, [](Args& a) {
+        OneDevice dev;
+        const Logits x(dev, a.tensor("logits"), "logits");
+        const int32_t* targets = on<int32_t>(dev, a.tensor("targets"), kI32, x.n, "targets");
+        const Batch b(dev, a, x.n);
+        const double temperature = a.real();
+        float* loss = on<float>(dev, a.tensor("loss"), kF32, 1, "loss");
+        float* logp = on<float>(dev, a.tensor("logp"), kF32, x.n, "logp");
+        const Logits dx = same_logits(dev, a.tensor("d_logits"), x, "d_logits");
+        float* stats = on<float>(dev, a.tensor("stats"), kF32, 4, "stats");
+        int32_t* status = on<int32_t>(dev, a.tensor("status"), kI32, 1, "status");
+        size_t bytes;
+        void* ws = scratch_on(dev, a, bytes);
+        void* s = a.stream();
+        return unlocked([&] { return sr_policy_loss_logits(x.data, x.dtype, x.n, x.vocab, x.pitch, targets, b.old_logp, b.ref_logp, b.adv, b.weight, b.row_start, b.rows, b.mask, b.clip_low, b.clip_high, b.beta, temperature, loss, logp, dx.data, dx.pitch, stats, status, ws, bytes, s); });
+    });
+}
+
+// A list or tuple of tensors, each dense (whatever the order of its dimensions).
+struct Grads {
+    std::vector<const void*> data;
+    std::vector<int64_t> counts;
+    std::vector<int32_t> dtypes;
+    std::vector<const at::Tensor*> tensors;
+    Grads(OneDevice& dev, PyObject* list, const char* name) {
+        if (!PyList_Check(list) && !PyTuple_Check(list)) raise(PyExc_TypeError, std::string(name) + " must be a list or tuple of tensors");
+        const Py_ssize_t n = PySequence_Fast_GET_SIZE(list);
+        count32(n, name);
+        PyObject** items = PySequence_Fast_ITEMS(list);
+        data.reserve(n); counts.reserve(n); dtypes.reserve(n); tensors.reserve(n);
+        for (Py_ssize_t i = 0; i < n; ++i) {
+            if (!THPVariable_Check(items[i])) raise(PyExc_TypeError, std::string(name) + " must be a list or tuple of tensors");
+            const at::Tensor& t = THPVariable_Unpack(items[i]);
+            dev.add(&t, name);
+            dtypes.push_back(dtype_code(t, name));
+            if (!t.is_non_overlapping_and_dense()) raise(PyExc_ValueError, std::string(name) + ": every tensor must be dense");
+            counts.push_back(t.numel());
+            data.push_back(t.numel() ? t.data_ptr() : nullptr);
+            tensors.push_back(&t);
+        }
+    }
+};
+
+PyObject* py_grad_norm(PyObject*, PyObject* const* argv, Py_ssize_t argc) {
+    return guarded(argv, argc, 4, [](Args& a) {
+        OneDevice dev;
+        const Grads g(dev, *a.at++, "grads");
+        float* norm = on<float>(dev, a.tensor("norm"), kF32, 1, "norm");
+        size_t bytes;
+        void* ws = scratch_on(dev, a, bytes);
+        void* s = a.stream();
+        return unlocked([&] { return sr_grad_norm(g.data.data(), g.counts.data(), g.dtypes.data(), (int32_t)g.data.size(), norm, ws, bytes, s); });
+    });
+}
+
+PyObject* py_clip_grads(PyObject*, PyObject* const* argv, Py_ssize_t argc) {
+    return guarded(argv, argc, 6, [](Args& a) {
+        OneDevice dev;
+        const Grads g(dev, *a.at++, "grads");
+        const float* norm = on<float>(dev, a.tensor("norm"), kF32, 1, "norm");
+        const double max_norm = a.real();
+        PyObject* given = *a.at++;
+        std::vector<void*> out;
+        if (given != Py_None) {
+            const Grads o(dev, given, "out");
+            if (o.data.size() != g.data.size()) raise(PyExc_ValueError, "out must have a tensor for every gradient");
+            for (size_t i = 0; i < o.data.size(); ++i) {
+                if (o.dtypes[i] != g.dtypes[i]) raise(PyExc_TypeError, "out: a tensor has another type than its gradient");
+                if (o.tensors[i]->sizes() != g.tensors[i]->sizes() || o.tensors[i]->strides() != g.tensors[i]->strides())
+                    raise(PyExc_ValueError, "out: a tensor has another shape or layout than its gradient");
+                out.push_back(const_cast<void*>(o.data[i]));
+            }
+        }
+        int32_t* status = on<int32_t>(dev, a.tensor("status"), kI32, 1, "status");
+        void* s = a.stream();
+        return unlocked([&] { return sr_clip_grads(g.data.data(), g.counts.data(), g.dtypes.data(), (int32_t)g.data.size(), norm, max_norm, given != Py_None ? out.data() : nullptr, status, s); });
+    });
+}
+
 #define SR_METHOD(name) {"sr_" #name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(py_##name)), METH_FASTCALL, nullptr}
 PyMethodDef g_methods[] = {
     SR_METHOD(gate), SR_METHOD(gate_noalloc), SR_METHOD(gate_decide), SR_METHOD(gate_host),
     SR_METHOD(gate_host_packed), SR_METHOD(incr_init), SR_METHOD(gate_step_incremental),
     SR_METHOD(gate_or_rule), SR_METHOD(group_signals), SR_METHOD(batch_stats),
-    SR_METHOD(kept_groups), SR_METHOD(grpo_advantage), {nullptr, nullptr, 0, nullptr}};
+    SR_METHOD(kept_groups), SR_METHOD(grpo_advantage), SR_METHOD(token_logprob), SR_METHOD(token_logprob_backward),
+    SR_METHOD(loss_weights), SR_METHOD(policy_loss), SR_METHOD(policy_loss_logits), SR_METHOD(grad_norm),
+    SR_METHOD(clip_grads), {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_native", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -72,6 +72,41 @@ __device__ __forceinline__ uint4 pack(const float (&x)[8], __half) {
     return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
+// Largest elements of vectors, a NaN only where there is nothing else: kept packed as long as more come.
+template <typename T>
+struct VecMax;
+template <>
+struct VecMax<float> {
+    float m;
+    __device__ __forceinline__ explicit VecMax(float first) : m(first) {}
+    __device__ __forceinline__ void take(const uint4& v) {
+        m = fmaxf(fmaxf(m, fmaxf(__uint_as_float(v.x), __uint_as_float(v.y))), fmaxf(__uint_as_float(v.z), __uint_as_float(v.w)));
+    }
+    __device__ __forceinline__ float value() const { return m; }
+};
+template <>
+struct VecMax<__nv_bfloat16> {
+    __nv_bfloat162 m;
+    __device__ __forceinline__ explicit VecMax(float first) : m(__float2bfloat162_rn(first)) {}
+    __device__ __forceinline__ void take(const uint4& v) {
+        __nv_bfloat162 h[4];
+        memcpy(h, &v, 16);
+        m = __hmax2(m, __hmax2(__hmax2(h[0], h[1]), __hmax2(h[2], h[3])));
+    }
+    __device__ __forceinline__ float value() const { return fmaxf(__low2float(m), __high2float(m)); }
+};
+template <>
+struct VecMax<__half> {
+    __half2 m;
+    __device__ __forceinline__ explicit VecMax(float first) : m(__float2half2_rn(first)) {}
+    __device__ __forceinline__ void take(const uint4& v) {
+        __half2 h[4];
+        memcpy(h, &v, 16);
+        m = __hmax2(m, __hmax2(__hmax2(h[0], h[1]), __hmax2(h[2], h[3])));
+    }
+    __device__ __forceinline__ float value() const { return fmaxf(__low2float(m), __high2float(m)); }
+};
+
 inline int dtype_bytes(int32_t dtype) { return dtype == SR_DTYPE_F32 ? 4 : dtype == SR_DTYPE_BF16 || dtype == SR_DTYPE_F16 ? 2 : 0; }
 
 // logprob.cu

@@ -20,8 +20,10 @@
 namespace sr {
 namespace {
 
-constexpr int kRowThreads = 512;
+constexpr int kRowThreads = 256;
 constexpr int kUnroll = 4;
+constexpr int kHeldThreads = 256, kMostVecs = 10;
+constexpr int kMaxCtas = 8;              // to a row: the portable cluster size
 constexpr double kLn2 = 0.693147180559945309417232;
 
 __device__ __forceinline__ float exp2_approx(float t) {        // 2^t within 2 ulp; 2^-inf = 0
@@ -37,22 +39,9 @@ struct RowSums {
     double s, u;
 };
 
-// Takes N more elements.  A maximum of -inf (nothing but such logits so far) stands for 0 in the exponents, which gives
-// terms of 0; NaN and +inf end up in s.
+// Terms of N elements, none of them above m (or NaN, or +inf: these end up in s).
 template <int N, bool kEntropy>
-__device__ __forceinline__ void take(const float (&x)[N], float c, RowSums& r) {
-    float top = x[0];
-#pragma unroll
-    for (int k = 1; k < N; ++k) top = fmaxf(top, x[k]);
-    if (top > r.m) {
-        const float shift = (r.m - top) * c;                    // -inf at first: factor 0
-        const double f = (double)exp2_approx(shift);
-        if (kEntropy) r.u = f * (r.u + (double)fmaxf(shift, -1000.0f) * r.s);
-        r.s *= f;
-        r.m = top;
-    }
-    const float m = r.m == minus_inf() ? 0.0f : r.m;
-    float s[4] = {0.0f, 0.0f, 0.0f, 0.0f}, u[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+__device__ __forceinline__ void add_terms(const float (&x)[N], float m, float c, float (&s)[4], float (&u)[4]) {
 #pragma unroll
     for (int k = 0; k < N; ++k) {
         const float t = (x[k] - m) * c;
@@ -60,8 +49,27 @@ __device__ __forceinline__ void take(const float (&x)[N], float c, RowSums& r) {
         s[k & 3] += e;
         if (kEntropy) u[k & 3] = fmaf(e, fmaxf(t, -1000.0f), u[k & 3]);      // 0 * -inf is 0 here; a NaN is in s already
     }
-    r.s += (double)((s[0] + s[1]) + (s[2] + s[3]));
-    if (kEntropy) r.u += (double)((u[0] + u[1]) + (u[2] + u[3]));
+}
+// Makes `top` the maximum where it is larger.
+template <bool kEntropy>
+__device__ __forceinline__ void grow(float top, float c, RowSums& r) {
+    if (!(top > r.m)) return;
+    const float shift = (r.m - top) * c;                        // -inf at first: factor 0
+    const double f = (double)exp2_approx(shift);
+    if (kEntropy) r.u = f * (r.u + (double)fmaxf(shift, -1000.0f) * r.s);
+    r.s *= f;
+    r.m = top;
+}
+// Takes one more element.  A maximum of -inf (nothing but such logits so far) stands for 0 in the exponents, which gives terms
+// of 0.
+template <bool kEntropy>
+__device__ __forceinline__ void take(float x, float c, RowSums& r) {
+    grow<kEntropy>(x, c, r);
+    const float one[1] = {x};
+    float s[4] = {0.0f, 0.0f, 0.0f, 0.0f}, u[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    add_terms<1, kEntropy>(one, r.m == minus_inf() ? 0.0f : r.m, c, s, u);
+    r.s += (double)s[0];
+    if (kEntropy) r.u += (double)u[0];
 }
 
 // r, seen from the maximum M of several parts.
@@ -75,12 +83,12 @@ __device__ __forceinline__ void rescale(RowSums& r, float M, float c) {
     r.m = M;
 }
 
-// Sums of all threads' parts, in every thread.  kCluster: over the cluster.
-template <bool kEntropy, bool kCluster>
-__device__ __forceinline__ RowSums combine(RowSums r, float c) {
+// Sums of all threads' parts, in every thread; over the cluster where it has several CTAs.
+template <bool kEntropy>
+__device__ __forceinline__ RowSums combine(RowSums r, float c, int ctas) {
     __shared__ float s_m[32];
     __shared__ double s_s[32], s_u[32];
-    __shared__ RowSums s_cta;
+    __shared__ RowSums s_cta[kMaxCtas];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
     float M = r.m;
 #pragma unroll
@@ -106,25 +114,32 @@ __device__ __forceinline__ RowSums combine(RowSums r, float c) {
         r.s += s_s[w];
         if (kEntropy) r.u += s_u[w];
     }
-    if (kCluster) {
+    if (ctas > 1) {
+        // every CTA writes its sums to all the others: after the barrier each reads its own memory, and may leave
         const auto cluster = cooperative_groups::this_cluster();
-        if (threadIdx.x == 0) s_cta = r;
+        if ((int)threadIdx.x < ctas) *cluster.map_shared_rank(&s_cta[cluster.block_rank()], threadIdx.x) = r;
         cluster.sync();
-        const unsigned n = cluster.num_blocks();
         float top = minus_inf();
-        for (unsigned b = 0; b < n; ++b) top = fmaxf(top, cluster.map_shared_rank(&s_cta, b)->m);
+        for (int b = 0; b < ctas; ++b) top = fmaxf(top, s_cta[b].m);
         RowSums sum = {top, 0.0, 0.0};
-        for (unsigned b = 0; b < n; ++b) {
-            RowSums part = *cluster.map_shared_rank(&s_cta, b);
+        for (int b = 0; b < ctas; ++b) {
+            RowSums part = s_cta[b];
             rescale<kEntropy>(part, top, c);
             sum.s += part.s;
             if (kEntropy) sum.u += part.u;
         }
-        cluster.sync();                        // nobody leaves while its sums are read
         r = sum;
     }
     if (r.m == minus_inf()) r.s = CUDART_NAN;  // no token can occur: there is no distribution
     return r;
+}
+
+// Unpacks a vector; the compiler is kept from holding on to elements that it has unpacked before, which would take twice the
+// registers.
+template <int E, typename T>
+__device__ __forceinline__ void unpack_again(uint4 v, float (&x)[E], T) {
+    asm volatile("" : "+r"(v.x), "+r"(v.y), "+r"(v.z), "+r"(v.w));
+    unpack(v, x, T());
 }
 
 // How a row falls into single elements before the first 16-byte boundary, vectors, and single elements behind them.
@@ -147,33 +162,43 @@ __device__ __forceinline__ uint4 all_minus_inf() {
     return make_uint4(w, w, w, w);
 }
 
-// Sums over the part of a row that thread `at` of `threads` has.
-template <typename T, bool kEntropy>
+// Sums over the part of a row that thread `at` of `threads` has.  kAgain: it is read again soon, and may stay in L2.
+template <typename T, bool kEntropy, bool kAgain>
 __device__ __forceinline__ RowSums sum_row(const T* row, int vocab, int at, int threads, float c) {
     constexpr int E = Vec<T>::kElems;
     const RowParts<T> parts(row, vocab);
     RowSums r = {minus_inf(), 0.0, 0.0};
-    if (at < parts.head + parts.tail) {
-        const float x[1] = {to_float(row[parts.single(at)])};
-        take<1, kEntropy>(x, c, r);
-    }
+    if (at < parts.head + parts.tail) take<kEntropy>(to_float(row[parts.single(at)]), c, r);
     const uint4* body = reinterpret_cast<const uint4*>(row + parts.head);
-    for (long long v = at; v < parts.vecs; v += (long long)threads * kUnroll) {
-        uint4 q[kUnroll];
+    uint4 next[kUnroll];                       // the batch after the one at hand is on its way while that is summed up
+    auto load = [&](long long v) {
 #pragma unroll
         for (int k = 0; k < kUnroll; ++k) {
             const long long i = v + (long long)k * threads;
-            q[k] = i < parts.vecs ? body[i] : all_minus_inf<T>();
+            next[k] = i >= parts.vecs ? all_minus_inf<T>() : kAgain ? body[i] : __ldcs(body + i);
         }
-        float x[kUnroll * E];
+    };
+    const long long step = (long long)threads * kUnroll;
+    if (at < parts.vecs) load(at);
+    for (long long v = at; v < parts.vecs; v += step) {
+        uint4 q[kUnroll];
+#pragma unroll
+        for (int k = 0; k < kUnroll; ++k) q[k] = next[k];
+        if (v + step < parts.vecs) load(v + step);
+        VecMax<T> top(minus_inf());
+#pragma unroll
+        for (int k = 0; k < kUnroll; ++k) top.take(q[k]);
+        grow<kEntropy>(top.value(), c, r);
+        const float m = r.m == minus_inf() ? 0.0f : r.m;
+        float s[4] = {0.0f, 0.0f, 0.0f, 0.0f}, u[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
         for (int k = 0; k < kUnroll; ++k) {
-            float y[E];
-            unpack(q[k], y, T());
-#pragma unroll
-            for (int j = 0; j < E; ++j) x[k * E + j] = y[j];
+            float x[E];
+            unpack_again(q[k], x, T());
+            add_terms<E, kEntropy>(x, m, c, s, u);
         }
-        take<kUnroll * E, kEntropy>(x, c, r);
+        r.s += (double)((s[0] + s[1]) + (s[2] + s[3]));
+        if (kEntropy) r.u += (double)((u[0] + u[1]) + (u[2] + u[3]));
     }
     return r;
 }
@@ -189,6 +214,77 @@ __device__ __forceinline__ float gradient(const RowGradient& g, float x) {
     const float e = exp2_approx(t);
     return kEntropy ? e * fmaf(g.k1, fmaxf(t, -1000.0f), g.k0) : e * g.k0;
 }
+// A row spread over the registers of a cluster: kVecs vectors a thread, and a single element where the row has some.  It is read
+// once, whatever is made of it, and all of a thread's loads are on their way together.
+template <typename T, int kVecs>
+struct HeldRow {
+    static constexpr int E = Vec<T>::kElems;
+    uint4 q[kVecs];
+    float x1;
+    int single;                      // place of x1, or -1
+
+    __device__ __forceinline__ void load(const T* row, const RowParts<T>& parts, int at, int threads) {
+        const uint4* body = reinterpret_cast<const uint4*>(row + parts.head);
+#pragma unroll
+        for (int k = 0; k < kVecs; ++k) {
+            const int i = at + k * threads;
+            q[k] = i < parts.vecs ? __ldcs(body + i) : all_minus_inf<T>();
+        }
+        single = at < parts.head + parts.tail ? parts.single(at) : -1;
+        x1 = single >= 0 ? to_float(row[single]) : minus_inf();
+    }
+    // The thread's own maximum first, then the terms: nothing is rescaled.
+    template <bool kEntropy>
+    __device__ __forceinline__ RowSums sums(float c) const {
+        VecMax<T> top(x1);                                     // x1 is an element: exact in its type
+#pragma unroll
+        for (int k = 0; k < kVecs; ++k) top.take(q[k]);
+        RowSums r = {top.value(), 0.0, 0.0};
+        if (!(r.m > minus_inf())) r.m = minus_inf();           // a NaN alone is no maximum
+        take<kEntropy>(x1, c, r);
+        const float m = r.m == minus_inf() ? 0.0f : r.m;
+        float s[4] = {0.0f, 0.0f, 0.0f, 0.0f}, u[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int k = 0; k < kVecs; ++k) {
+            float x[E];
+            unpack_again(q[k], x, T());
+            add_terms<E, kEntropy>(x, m, c, s, u);
+            if (k % 4 == 3 || k == kVecs - 1) {
+                r.s += (double)((s[0] + s[1]) + (s[2] + s[3]));
+                if (kEntropy) r.u += (double)((u[0] + u[1]) + (u[2] + u[3]));
+#pragma unroll
+                for (int j = 0; j < 4; ++j) s[j] = u[j] = 0.0f;
+            }
+        }
+        return r;
+    }
+    __device__ __forceinline__ void write_gradient(T* out, const RowParts<T>& parts, int at, int threads, const RowGradient& g) const {
+        uint4* to = reinterpret_cast<uint4*>(out + parts.head);
+        const int target_vec = g.target < parts.head ? -1 : (g.target - parts.head) / E;
+#pragma unroll
+        for (int k = 0; k < kVecs; ++k) {
+            const int i = at + k * threads;
+            if (i >= parts.vecs) break;
+            float x[E];
+            unpack_again(q[k], x, T());
+#pragma unroll
+            for (int j = 0; j < E; ++j) x[j] = gradient<false>(g, x[j]);
+            if (i == target_vec) {
+                const int at_j = (g.target - parts.head) % E;
+#pragma unroll
+                for (int j = 0; j < E; ++j)
+                    if (j == at_j) x[j] += g.at_target;
+            }
+            __stcs(to + i, pack(x, T()));
+        }
+        if (single >= 0) {
+            float v = gradient<false>(g, x1);
+            if (single == g.target) v += g.at_target;
+            out[single] = from_float<T>(v);
+        }
+    }
+};
+
 // kZero: the row's gradient is 0 and its logits are not read.
 template <typename T, bool kEntropy, bool kZero>
 __device__ __forceinline__ void write_gradient(const T* row, T* out, int vocab, int at, int threads, const RowGradient& g) {
@@ -242,12 +338,12 @@ __device__ __forceinline__ bool counts_as_target(int32_t y, int vocab, int32_t* 
     return y >= 0 && y < vocab;
 }
 
-template <typename T, bool kEntropy, bool kCluster>
-__global__ void __launch_bounds__(kRowThreads)
+template <typename T, bool kEntropy>
+__global__ void __launch_bounds__(kRowThreads, 4)
 token_logprob_kernel(const T* __restrict__ logits, int vocab, long long pitch, const int32_t* __restrict__ targets, double temperature, float c, int ctas,
                      float* __restrict__ logp, float* __restrict__ row_stats, float* __restrict__ entropy, int32_t* __restrict__ status) {
     grid_begin();
-    const int t = kCluster ? blockIdx.x / ctas : blockIdx.x, part = kCluster ? blockIdx.x % ctas : 0;
+    const int t = blockIdx.x / ctas, part = blockIdx.x % ctas;
     const int32_t y = targets[t];
     const bool first = part == 0 && threadIdx.x == 0;
     if (!counts_as_target(y, vocab, status, first)) {
@@ -259,11 +355,44 @@ token_logprob_kernel(const T* __restrict__ logits, int vocab, long long pitch, c
         return;
     }
     const T* row = logits + (size_t)t * pitch;
-    RowSums r = sum_row<T, kEntropy>(row, vocab, part * kRowThreads + threadIdx.x, ctas * kRowThreads, c);
-    r = combine<kEntropy, kCluster>(r, c);
+    const float x_y = first ? to_float(row[y]) : 0.0f;        // on its way meanwhile
+    RowSums r = sum_row<T, kEntropy, false>(row, vocab, part * kRowThreads + threadIdx.x, ctas * kRowThreads, c);
+    r = combine<kEntropy>(r, c, ctas);
     if (first) {
         const double log_S = log(r.s);
-        logp[t] = (float)(((double)to_float(row[y]) - (double)r.m) / temperature - log_S);
+        logp[t] = (float)(((double)x_y - (double)r.m) / temperature - log_S);
+        if (row_stats) {
+            row_stats[2 * (size_t)t] = r.m;
+            row_stats[2 * (size_t)t + 1] = (float)r.s;
+        }
+        if (kEntropy) entropy[t] = (float)(log_S - kLn2 * r.u / r.s);
+    }
+}
+
+template <typename T, int kVecs, bool kEntropy>
+__global__ void __launch_bounds__(kHeldThreads, kVecs > 7 ? 3 : 4)
+held_logprob_kernel(const T* __restrict__ logits, int vocab, long long pitch, const int32_t* __restrict__ targets, double temperature, float c, int ctas,
+                    float* __restrict__ logp, float* __restrict__ row_stats, float* __restrict__ entropy, int32_t* __restrict__ status) {
+    grid_begin();
+    const int t = blockIdx.x / ctas, part = blockIdx.x % ctas;
+    const int32_t y = targets[t];
+    const bool first = part == 0 && threadIdx.x == 0;
+    if (!counts_as_target(y, vocab, status, first)) {
+        if (first) {
+            logp[t] = 0.0f;
+            if (row_stats) row_stats[2 * (size_t)t] = row_stats[2 * (size_t)t + 1] = 0.0f;
+            if (kEntropy) entropy[t] = 0.0f;
+        }
+        return;
+    }
+    const T* row = logits + (size_t)t * pitch;
+    HeldRow<T, kVecs> held;
+    held.load(row, RowParts<T>(row, vocab), part * kHeldThreads + threadIdx.x, ctas * kHeldThreads);
+    const float x_y = first ? to_float(row[y]) : 0.0f;        // on its way meanwhile
+    const RowSums r = combine<kEntropy>(held.template sums<kEntropy>(c), c, ctas);
+    if (first) {
+        const double log_S = log(r.s);
+        logp[t] = (float)(((double)x_y - (double)r.m) / temperature - log_S);
         if (row_stats) {
             row_stats[2 * (size_t)t] = r.m;
             row_stats[2 * (size_t)t + 1] = (float)r.s;
@@ -315,12 +444,40 @@ token_rows_kernel(PolicyBatch b, const int32_t* __restrict__ targets, int vocab,
     row_of[t] = r;
 }
 
-template <typename T, bool kCluster>
-__global__ void __launch_bounds__(kRowThreads)
+// By one thread: the token's terms of the loss and the gradient of its row.  A function of its own, so that the registers of a
+// held row are put aside for it in that thread alone.
+__device__ __noinline__ void token_gradient(const PolicyBatch& b, int t, float x_y, float A, float w, float m, double S, double temperature, float* logp,
+                                            PolicyTerms<float>* terms, RowGradient* g) {
+    const double lp = ((double)x_y - (double)m) / temperature - log(S);
+    PolicyTerms<float> term;
+    const float d = policy_token(b, (size_t)t, lp, A, w, term);
+    if (logp) {
+        logp[t] = (float)lp;
+        terms[t] = term;
+    }
+    g->k0 = (float)(-(double)d / (S * temperature));
+    g->at_target = (float)((double)d / temperature);
+}
+// The gradient of a row, in every thread of the CTA; `first` writes down the token's figures.
+__device__ __forceinline__ RowGradient loss_gradient(const PolicyBatch& b, int t, float x_y, int y, float A, float w, const RowSums& r, double temperature, float c,
+                                                     bool first, float* logp, PolicyTerms<float>* terms) {
+    __shared__ RowGradient s_g;
+    if (threadIdx.x == 0) token_gradient(b, t, x_y, A, w, r.m, r.s, temperature, first ? logp : nullptr, terms, &s_g);
+    __syncthreads();
+    RowGradient g = s_g;
+    g.M = r.m;
+    g.c = c;
+    g.k1 = 0.0f;
+    g.target = y;
+    return g;
+}
+
+template <typename T>
+__global__ void __launch_bounds__(kRowThreads, 4)
 policy_loss_logits_kernel(PolicyBatch b, const T* logits, int vocab, long long pitch, const int32_t* __restrict__ targets, const int32_t* __restrict__ row_of,
                           double temperature, float c, int ctas, float* __restrict__ logp, PolicyTerms<float>* __restrict__ terms, T* d_logits, long long d_pitch) {
     grid_begin();
-    const int t = kCluster ? blockIdx.x / ctas : blockIdx.x, part = kCluster ? blockIdx.x % ctas : 0;
+    const int t = blockIdx.x / ctas, part = blockIdx.x % ctas;
     const int at = part * kRowThreads + threadIdx.x, threads = ctas * kRowThreads;
     const int rollout = row_of[t];
     const bool first = part == 0 && threadIdx.x == 0;
@@ -337,44 +494,87 @@ policy_loss_logits_kernel(PolicyBatch b, const T* logits, int vocab, long long p
     const T* row = logits + (size_t)t * pitch;
     const int32_t y = targets[t];
     const float A = b.adv[rollout], w = b.weight[rollout];
-    const double x_y = (double)to_float(row[y]);               // before anyone writes: d_logits may be the logits
-    RowSums r = sum_row<T, false>(row, vocab, at, threads, c);
-    r = combine<false, kCluster>(r, c);
-    __shared__ RowGradient s_g;
-    if (threadIdx.x == 0) {
-        const double lp = (x_y - (double)r.m) / temperature - log(r.s);
-        PolicyTerms<float> term;
-        const float d = policy_token(b, (size_t)t, lp, A, w, term);
-        if (first) {
-            logp[t] = (float)lp;
-            terms[t] = term;
-        }
-        g.M = r.m;
-        g.c = c;
-        g.k0 = (float)(-(double)d / (r.s * temperature));
-        g.at_target = (float)((double)d / temperature);
-        g.target = y;
-        s_g = g;
-    }
-    __syncthreads();
-    g = s_g;
+    const float x_y = to_float(row[y]);                        // before anyone writes: d_logits may be the logits
+    RowSums r = sum_row<T, false, true>(row, vocab, at, threads, c);
+    r = combine<false>(r, c, ctas);
+    g = loss_gradient(b, t, x_y, y, A, w, r, temperature, c, first, logp, terms);
     write_gradient<T, false, false>(row, out, vocab, at, threads, g);
+}
+
+template <typename T, int kVecs>
+__global__ void __launch_bounds__(kHeldThreads, kVecs > 7 ? 3 : 4)
+held_policy_loss_kernel(PolicyBatch b, const T* logits, int vocab, long long pitch, const int32_t* __restrict__ targets, const int32_t* __restrict__ row_of,
+                        double temperature, float c, int ctas, float* __restrict__ logp, PolicyTerms<float>* __restrict__ terms, T* d_logits, long long d_pitch) {
+    grid_begin();
+    const int t = blockIdx.x / ctas, part = blockIdx.x % ctas;
+    const int at = part * kHeldThreads + threadIdx.x, threads = ctas * kHeldThreads;
+    const int rollout = row_of[t];
+    const bool first = part == 0 && threadIdx.x == 0;
+    T* out = d_logits + (size_t)t * d_pitch;
+    if (rollout < 0) {
+        write_gradient<T, false, true>(nullptr, out, vocab, at, threads, RowGradient());
+        if (first) {
+            logp[t] = 0.0f;
+            terms[t] = PolicyTerms<float>{0.0f, 0.0f, 0.0f, 0.0f};
+        }
+        return;
+    }
+    const T* row = logits + (size_t)t * pitch;
+    const RowParts<T> parts(row, vocab);
+    HeldRow<T, kVecs> held;
+    held.load(row, parts, at, threads);
+    const int32_t y = targets[t];
+    const float A = b.adv[rollout], w = b.weight[rollout];
+    const float x_y = to_float(row[y]);                        // before anyone writes: d_logits may be the logits
+    const RowSums r = combine<false>(held.template sums<false>(c), c, ctas);
+    const RowGradient g = loss_gradient(b, t, x_y, y, A, w, r, temperature, c, first, logp, terms);
+    held.write_gradient(out, parts, at, threads, g);
+}
+
+// How a row is held: CTAs to a row and vectors a thread, or no way to.  One CTA, or, where the rows alone do not fill the GPU, a
+// cluster as long as each thread still has a vector.
+struct Held {
+    int ctas, vecs;
+};
+Held held_row(int n_tokens, int vocab, int elem) {
+    const long long need = ((long long)vocab * elem + 15) / 16;
+    Held h = {1, 0};
+    while (h.ctas < kMaxCtas && (long long)n_tokens * h.ctas < 2 * 148 && need > (long long)h.ctas * kHeldThreads) h.ctas *= 2;
+    const long long least = (need + (long long)h.ctas * kHeldThreads - 1) / ((long long)h.ctas * kHeldThreads);
+    h.vecs = least > kMostVecs ? 0 : least <= 1 ? 1 : least <= 2 ? 2 : least <= 4 ? 4 : least <= 7 ? 7 : kMostVecs;
+    return h;
+}
+template <typename F>
+int with_vecs(int vecs, F f) {
+    switch (vecs) {
+        case 1: return f(std::integral_constant<int, 1>());
+        case 2: return f(std::integral_constant<int, 2>());
+        case 4: return f(std::integral_constant<int, 4>());
+        case 7: return f(std::integral_constant<int, 7>());
+        default: return f(std::integral_constant<int, kMostVecs>());
+    }
 }
 
 // CTAs to a row: one where the rows alone fill the GPU; else a power of two up to the portable cluster size, of which each
 // still has a vector or two a thread.
 int ctas_of_row(int n_tokens, int vocab, int elem) {
     int ctas = 1;
-    while (ctas < 8 && (long long)n_tokens * ctas < 2 * 148 && (long long)vocab * elem > 2LL * ctas * kRowThreads * 16) ctas *= 2;
+    while (ctas < kMaxCtas && (long long)n_tokens * ctas < 2 * 148 && (long long)vocab * elem > 2LL * ctas * kRowThreads * 16) ctas *= 2;
     return ctas;
 }
 
 template <typename T>
 int launch_forward(const LogitsArgs& a, float* logp, float* row_stats, float* entropy, int32_t* status, cudaStream_t s) {
     const float c = (float)(1.0 / (kLn2 * a.temperature));
+    const Held held = held_row(a.n_tokens, a.vocab, (int)sizeof(T));
+    if (held.vecs)
+        return with_vecs(held.vecs, [&](auto vecs) {
+            const auto kernel = entropy ? held_logprob_kernel<T, vecs(), true> : held_logprob_kernel<T, vecs(), false>;
+            return launch_as(true, held.ctas, "held_logprob_kernel", kernel, a.n_tokens * held.ctas, kHeldThreads, 0, s, static_cast<const T*>(a.logits), a.vocab, (long long)a.pitch, a.targets,
+                             a.temperature, c, held.ctas, logp, row_stats, entropy, status);
+        });
     const int ctas = ctas_of_row(a.n_tokens, a.vocab, (int)sizeof(T));
-    const auto kernel = ctas > 1 ? (entropy ? token_logprob_kernel<T, true, true> : token_logprob_kernel<T, false, true>)
-                                 : (entropy ? token_logprob_kernel<T, true, false> : token_logprob_kernel<T, false, false>);
+    const auto kernel = entropy ? token_logprob_kernel<T, true> : token_logprob_kernel<T, false>;
     return launch_as(true, ctas, "token_logprob_kernel", kernel, a.n_tokens * ctas, kRowThreads, 0, s, static_cast<const T*>(a.logits), a.vocab, (long long)a.pitch, a.targets,
                      a.temperature, c, ctas, logp, row_stats, entropy, status);
 }
@@ -391,9 +591,16 @@ int launch_backward(const LogitsArgs& a, const float* row_stats, const float* en
 template <typename T>
 int launch_step(const LogitsArgs& a, const PolicyBatch& b, const int32_t* row_of, float* logp, PolicyTerms<float>* terms, void* d_logits, int64_t d_pitch, cudaStream_t s) {
     const float c = (float)(1.0 / (kLn2 * a.temperature));
+    // held rows are written as they were read: both lie alike against 16 bytes
+    const Held held = held_row(a.n_tokens, a.vocab, (int)sizeof(T));
+    const uintptr_t apart = reinterpret_cast<uintptr_t>(a.logits) ^ reinterpret_cast<uintptr_t>(d_logits);
+    if (held.vecs && (apart & 15) == 0 && ((a.pitch - d_pitch) * (int64_t)sizeof(T)) % 16 == 0)
+        return with_vecs(held.vecs, [&](auto vecs) {
+            return launch_as(true, held.ctas, "held_policy_loss_kernel", held_policy_loss_kernel<T, vecs()>, a.n_tokens * held.ctas, kHeldThreads, 0, s, b, static_cast<const T*>(a.logits),
+                             a.vocab, (long long)a.pitch, a.targets, row_of, a.temperature, c, held.ctas, logp, terms, static_cast<T*>(d_logits), (long long)d_pitch);
+        });
     const int ctas = ctas_of_row(a.n_tokens, a.vocab, (int)sizeof(T));
-    const auto kernel = ctas > 1 ? policy_loss_logits_kernel<T, true> : policy_loss_logits_kernel<T, false>;
-    return launch_as(true, ctas, "policy_loss_logits_kernel", kernel, a.n_tokens * ctas, kRowThreads, 0, s, b, static_cast<const T*>(a.logits), a.vocab, (long long)a.pitch, a.targets, row_of,
+    return launch_as(true, ctas, "policy_loss_logits_kernel", policy_loss_logits_kernel<T>, a.n_tokens * ctas, kRowThreads, 0, s, b, static_cast<const T*>(a.logits), a.vocab, (long long)a.pitch, a.targets, row_of,
                      a.temperature, c, ctas, logp, terms, static_cast<T*>(d_logits), (long long)d_pitch);
 }
 

@@ -80,7 +80,7 @@ __device__ __forceinline__ double piece_square_sum(const T* p, int n) {
 #pragma unroll
     for (int k = 0; k < kVecsInFlight; ++k) {
         const int i = threadIdx.x + k * kGradThreads;
-        q[k] = i < vecs ? __ldcs(body + i) : make_uint4(0u, 0u, 0u, 0u);
+        q[k] = i < vecs ? load_once(body + i) : make_uint4(0u, 0u, 0u, 0u);
     }
 #pragma unroll
     for (int k = 0; k < kVecsInFlight; k += 2) {
@@ -109,7 +109,7 @@ __device__ __forceinline__ double block_sum(double v) {
 
 template <int kCap>
 __global__ void __launch_bounds__(kGradThreads)
-grad_squares_kernel(const __grid_constant__ GradList<kCap> list, double* __restrict__ partial) {
+grad_squares_kernel(const __grid_constant__ GradList<kCap> list, double* partial) {
     grid_begin();
     double sum = 0.0;
     for_pieces(list, [&](int i, int64_t at, int n) {
@@ -122,7 +122,7 @@ grad_squares_kernel(const __grid_constant__ GradList<kCap> list, double* __restr
 }
 
 __global__ void __launch_bounds__(1024)
-grad_norm_kernel(const double* __restrict__ partial, int n, float* __restrict__ norm) {
+grad_norm_kernel(const double* partial, int n, float* norm) {
     grid_begin();
     double sum = 0.0;
     for (int i = threadIdx.x; i < n; i += 1024) sum += partial[i];
@@ -166,7 +166,7 @@ __device__ __forceinline__ void scale_piece(const T* p, T* out, int n, float fac
 
 template <int kCap>
 __global__ void __launch_bounds__(kGradThreads)
-clip_grads_kernel(const __grid_constant__ GradList<kCap> list, const float* __restrict__ norm, float max_norm, int32_t* __restrict__ status) {
+clip_grads_kernel(const __grid_constant__ GradList<kCap> list, const float* norm, float max_norm, int32_t* status) {
     grid_begin();
     const float total = *norm;
     const bool finite = isfinite(total);

@@ -11,6 +11,16 @@
 
 namespace sr {
 
+// Kernels here read with plain loads and with these.  What the compiler may take for constant while the kernel runs (__ldg, const
+// __restrict__) it may also load before grid_begin() has waited for the kernel that writes it: the first row start of a batch was
+// read too early that way.  Statements that are volatile stay in their order.
+__device__ __forceinline__ uint4 load_once(const uint4* p) {            // not read again soon
+    uint4 v;
+    asm volatile("ld.global.cs.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
+    return v;
+}
+__device__ __forceinline__ void store_once(uint4* p, const uint4& v) { __stcs(p, v); }
+
 __device__ __forceinline__ float to_float(float x) { return x; }
 __device__ __forceinline__ float to_float(__nv_bfloat16 x) { return __bfloat162float(x); }
 __device__ __forceinline__ float to_float(__half x) { return __half2float(x); }

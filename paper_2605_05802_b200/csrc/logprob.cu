@@ -175,7 +175,7 @@ __device__ __forceinline__ RowSums sum_row(const T* row, int vocab, int at, int 
 #pragma unroll
         for (int k = 0; k < kUnroll; ++k) {
             const long long i = v + (long long)k * threads;
-            next[k] = i >= parts.vecs ? all_minus_inf<T>() : kAgain ? body[i] : __ldcs(body + i);
+            next[k] = i >= parts.vecs ? all_minus_inf<T>() : kAgain ? body[i] : load_once(body + i);
         }
     };
     const long long step = (long long)threads * kUnroll;
@@ -228,7 +228,7 @@ struct HeldRow {
 #pragma unroll
         for (int k = 0; k < kVecs; ++k) {
             const int i = at + k * threads;
-            q[k] = i < parts.vecs ? __ldcs(body + i) : all_minus_inf<T>();
+            q[k] = i < parts.vecs ? load_once(body + i) : all_minus_inf<T>();
         }
         single = at < parts.head + parts.tail ? parts.single(at) : -1;
         x1 = single >= 0 ? to_float(row[single]) : minus_inf();
@@ -275,7 +275,7 @@ struct HeldRow {
                 for (int j = 0; j < E; ++j)
                     if (j == at_j) x[j] += g.at_target;
             }
-            __stcs(to + i, pack(x, T()));
+            store_once(to + i, pack(x, T()));
         }
         if (single >= 0) {
             float v = gradient<false>(g, x1);
@@ -340,8 +340,8 @@ __device__ __forceinline__ bool counts_as_target(int32_t y, int vocab, int32_t* 
 
 template <typename T, bool kEntropy>
 __global__ void __launch_bounds__(kRowThreads, 4)
-token_logprob_kernel(const T* __restrict__ logits, int vocab, long long pitch, const int32_t* __restrict__ targets, double temperature, float c, int ctas,
-                     float* __restrict__ logp, float* __restrict__ row_stats, float* __restrict__ entropy, int32_t* __restrict__ status) {
+token_logprob_kernel(const T* logits, int vocab, long long pitch, const int32_t* targets, double temperature, float c, int ctas,
+                     float* logp, float* row_stats, float* entropy, int32_t* status) {
     grid_begin();
     const int t = blockIdx.x / ctas, part = blockIdx.x % ctas;
     const int32_t y = targets[t];
@@ -371,8 +371,8 @@ token_logprob_kernel(const T* __restrict__ logits, int vocab, long long pitch, c
 
 template <typename T, int kVecs, bool kEntropy>
 __global__ void __launch_bounds__(kHeldThreads, kVecs > 7 ? 3 : 4)
-held_logprob_kernel(const T* __restrict__ logits, int vocab, long long pitch, const int32_t* __restrict__ targets, double temperature, float c, int ctas,
-                    float* __restrict__ logp, float* __restrict__ row_stats, float* __restrict__ entropy, int32_t* __restrict__ status) {
+held_logprob_kernel(const T* logits, int vocab, long long pitch, const int32_t* targets, double temperature, float c, int ctas,
+                    float* logp, float* row_stats, float* entropy, int32_t* status) {
     grid_begin();
     const int t = blockIdx.x / ctas, part = blockIdx.x % ctas;
     const int32_t y = targets[t];
@@ -403,8 +403,8 @@ held_logprob_kernel(const T* __restrict__ logits, int vocab, long long pitch, co
 
 template <typename T, bool kEntropy>
 __global__ void __launch_bounds__(kRowThreads)
-token_logprob_backward_kernel(const T* logits, int vocab, long long pitch, const int32_t* __restrict__ targets, const float* __restrict__ row_stats,
-                              const float* __restrict__ entropy, const float* __restrict__ d_logp, const float* __restrict__ d_entropy, double temperature, float c,
+token_logprob_backward_kernel(const T* logits, int vocab, long long pitch, const int32_t* targets, const float* row_stats,
+                              const float* entropy, const float* d_logp, const float* d_entropy, double temperature, float c,
                               int parts, T* d_logits, long long d_pitch) {
     grid_begin();
     const int t = blockIdx.x / parts, part = blockIdx.x % parts;
@@ -432,7 +432,7 @@ token_logprob_backward_kernel(const T* logits, int vocab, long long pitch, const
 
 // The rollout of every token that counts, -1 for the others, so that the rows of the next kernel start reading at once.
 __global__ void __launch_bounds__(256)
-token_rows_kernel(PolicyBatch b, const int32_t* __restrict__ targets, int vocab, int n, int32_t* __restrict__ row_of, int32_t* __restrict__ status) {
+token_rows_kernel(PolicyBatch b, const int32_t* targets, int vocab, int n, int32_t* row_of, int32_t* status) {
     grid_begin();
     const int t = blockIdx.x * 256 + threadIdx.x;
     if (t >= n) return;
@@ -450,7 +450,7 @@ __device__ __noinline__ void token_gradient(const PolicyBatch& b, int t, float x
                                             PolicyTerms<float>* terms, RowGradient* g) {
     const double lp = ((double)x_y - (double)m) / temperature - log(S);
     PolicyTerms<float> term;
-    const float d = policy_token(b, (size_t)t, lp, A, w, term);
+    const float d = policy_token(b, PolicyToken{b.old_logp ? b.old_logp[t] : 0.0f, b.ref_logp ? b.ref_logp[t] : 0.0f, A, w}, lp, term);
     if (logp) {
         logp[t] = (float)lp;
         terms[t] = term;
@@ -474,8 +474,8 @@ __device__ __forceinline__ RowGradient loss_gradient(const PolicyBatch& b, int t
 
 template <typename T>
 __global__ void __launch_bounds__(kRowThreads, 4)
-policy_loss_logits_kernel(PolicyBatch b, const T* logits, int vocab, long long pitch, const int32_t* __restrict__ targets, const int32_t* __restrict__ row_of,
-                          double temperature, float c, int ctas, float* __restrict__ logp, PolicyTerms<float>* __restrict__ terms, T* d_logits, long long d_pitch) {
+policy_loss_logits_kernel(PolicyBatch b, const T* logits, int vocab, long long pitch, const int32_t* targets, const int32_t* row_of,
+                          double temperature, float c, int ctas, float* logp, PolicyTerms<float>* terms, T* d_logits, long long d_pitch) {
     grid_begin();
     const int t = blockIdx.x / ctas, part = blockIdx.x % ctas;
     const int at = part * kRowThreads + threadIdx.x, threads = ctas * kRowThreads;
@@ -503,8 +503,8 @@ policy_loss_logits_kernel(PolicyBatch b, const T* logits, int vocab, long long p
 
 template <typename T, int kVecs>
 __global__ void __launch_bounds__(kHeldThreads, kVecs > 7 ? 3 : 4)
-held_policy_loss_kernel(PolicyBatch b, const T* logits, int vocab, long long pitch, const int32_t* __restrict__ targets, const int32_t* __restrict__ row_of,
-                        double temperature, float c, int ctas, float* __restrict__ logp, PolicyTerms<float>* __restrict__ terms, T* d_logits, long long d_pitch) {
+held_policy_loss_kernel(PolicyBatch b, const T* logits, int vocab, long long pitch, const int32_t* targets, const int32_t* row_of,
+                        double temperature, float c, int ctas, float* logp, PolicyTerms<float>* terms, T* d_logits, long long d_pitch) {
     grid_begin();
     const int t = blockIdx.x / ctas, part = blockIdx.x % ctas;
     const int at = part * kHeldThreads + threadIdx.x, threads = ctas * kHeldThreads;

@@ -1,13 +1,12 @@
 // Clipped policy loss over packed rollouts: the weights that share it out, the loss and its gradient.
 //
-// Weights.  weight[r] needs the tokens of r that count and their total over the batch.  A warp takes 1024 mask bytes, 32 a
-// lane, as bits with a prefix sum of their number; the rollouts that meet those bytes are then dealt to the lanes, each of
-// which has its count from two look-ups, and one integer atomic adds it to the rollout's (whole numbers: any order gives the
-// same).  One cluster then sums up and divides.  A byte per token and 16 bytes per rollout.
+// Weights.  weight[r] needs the tokens of r that count and their total over the batch.  A warp counts a rollout's mask bytes, 32 a
+// lane; one cluster then sums up and divides.  A byte per token and 16 bytes per rollout: bound by the launches, or by HBM for
+// very large batches.
 //
-// Loss.  Four tokens a thread, 17 bytes a token, bound by HBM for large batches and by the launch for small ones.  Which
-// rollout a token is in comes from a search of row_start by the warp for its first and last token; only where these differ
-// do lanes search, between the two.
+// Loss.  Four tokens a thread, 17 bytes a token, bound by HBM for large batches and by the launch for small ones.  A warp
+// searches row_start once, for the first of its tokens, and moves on from there: 128 tokens mostly lie in one rollout or a few,
+// whose starts the lanes look at together.
 #include <cooperative_groups.h>
 
 #include "policy.cuh"
@@ -15,144 +14,239 @@
 namespace sr {
 namespace {
 
-// Bit k set iff byte k of the 32 from `at` on is non-zero and lies below `end`.
-__device__ __forceinline__ uint32_t mask_bits(const uint8_t* __restrict__ mask, long long at, long long end) {
-    uint32_t bits = 0u;
-    if (at + 32 <= end && (reinterpret_cast<uintptr_t>(mask + at) & 15) == 0) {
-        const uint4 a = __ldg(reinterpret_cast<const uint4*>(mask + at)), b = __ldg(reinterpret_cast<const uint4*>(mask + at) + 1);
-        const uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+// Mask bytes of [a, e) that are not zero, among the 32 from `at` on, and 0 <= a, e <= n_tokens; `at` lies so that a vector may be
+// loaded there.
+__device__ __forceinline__ int count_32(const uint8_t* mask, int n_tokens, long long a, long long e, long long at) {
+    const int lo = (int)max(0LL, min(32LL, a - at)), hi = (int)max(0LL, min(32LL, e - at));
+    if (lo >= hi) return 0;
+    if (at >= 0 && at + 32 <= n_tokens) {
+        const uint4 x = reinterpret_cast<const uint4*>(mask + at)[0], y = reinterpret_cast<const uint4*>(mask + at)[1];
+        const uint32_t w[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
+        uint32_t bits = 0u;
 #pragma unroll
         for (int q = 0; q < 8; ++q)      // one bit per byte, gathered by a product whose partial products do not meet
             bits |= (((__vminu4(w[q], 0x01010101u) * 0x00204081u) >> 21) & 0xFu) << (4 * q);
-        return bits;
+        return __popc(bits & low_mask(hi) & ~low_mask(lo));
     }
-    for (int k = 0; k < 32 && at + k < end; ++k) bits |= (mask[at + k] != 0 ? 1u : 0u) << k;
-    return bits;
+    int n = 0;
+    for (int k = lo; k < hi; ++k) n += mask[at + k] != 0;
+    return n;
 }
 
-constexpr int kMaskTile = 1024;          // mask bytes a warp
+constexpr int kLongRollout = 16384;      // mask bytes: a whole CTA counts them
+constexpr int kRowsOfCta = 256;          // at most
+
+// Tokens that count of rollouts first .. first + rows - 1, by a CTA: a warp to a rollout, and all of it to a long one.
+// Rollouts of groups that are cut are not looked at.
+__device__ __forceinline__ void count_rows(const int64_t* row_start, const uint8_t* mask, int n_tokens,
+                                           const uint8_t* drop_mask, int N, int first, int rows, int32_t* s_count) {
+    __shared__ int s_part[32];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
+    const int off = (int)((16 - (reinterpret_cast<uintptr_t>(mask) & 15)) & 15);         // positions off, off + 16, ... are aligned
+    const auto begin_of = [&](long long a) { return a - ((a - off) & 15); };
+    int any_long = 0;
+    for (int i = warp; i < rows; i += warps) {
+        long long a = 0, e = 0;
+        if (!(drop_mask && drop_mask[(first + i) / N])) {
+            a = min(max((long long)row_start[first + i], 0LL), (long long)n_tokens);
+            e = min(max((long long)row_start[first + i + 1], a), (long long)n_tokens);
+        }
+        int n = 0;
+        if (e - a > kLongRollout) {
+            n = -1;
+            any_long = 1;
+        } else {
+            for (long long at = begin_of(a) + 32 * lane; at < e; at += 1024) n += count_32(mask, n_tokens, a, e, at);
+            n = __reduce_add_sync(0xFFFFFFFFu, n);
+        }
+        if (lane == 0) s_count[i] = n;
+    }
+    if (!__syncthreads_or(any_long)) return;
+    for (int i = 0; i < rows; ++i) {
+        if (s_count[i] >= 0) continue;
+        const long long a = max((long long)row_start[first + i], 0LL), e = min((long long)row_start[first + i + 1], (long long)n_tokens);
+        int n = 0;
+        for (long long at = begin_of(a) + 32LL * threadIdx.x; at < e; at += 32LL * blockDim.x) n += count_32(mask, n_tokens, a, e, at);
+        n = __reduce_add_sync(0xFFFFFFFFu, n);
+        if (lane == 0) s_part[warp] = n;
+        __syncthreads();
+        if (threadIdx.x == 0) {
+            for (int w = 1; w < warps; ++w) n += s_part[w];
+            s_count[i] = n;
+        }
+        __syncthreads();
+    }
+}
 
 __global__ void __launch_bounds__(256)
-count_tokens_kernel(const int64_t* __restrict__ row_start, int rows, const uint8_t* __restrict__ mask, int n_tokens, int32_t* __restrict__ tokens) {
+count_tokens_kernel(const int64_t* row_start, int rows, const uint8_t* mask, int n_tokens, const uint8_t* drop_mask, int N, int rows_of_cta,
+                    int32_t* tokens) {
     grid_begin();
-    const int lane = threadIdx.x & 31;
-    const long long first = ((long long)blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5)) * kMaskTile;
-    if (first >= n_tokens) return;
-    const long long last = min(first + kMaskTile, (long long)n_tokens);
-    const uint32_t bits = mask_bits(mask, first + 32 * lane, last);
-    const int own = __popc(bits);
-    int before = own;
-#pragma unroll
-    for (int d = 1; d < 32; d <<= 1) {
-        const int up = __shfl_up_sync(0xFFFFFFFFu, before, d);
-        if (lane >= d) before += up;
-    }
-    before -= own;
-    // set bits below position `at` of the tile, 0 .. kMaskTile
-    const int all = __shfl_sync(0xFFFFFFFFu, before + own, 31);
-    auto below = [&](int at) {
-        const uint32_t b = __shfl_sync(0xFFFFFFFFu, bits, (at >> 5) & 31);
-        const int n = __shfl_sync(0xFFFFFFFFu, before, (at >> 5) & 31);
-        return at >= kMaskTile ? all : n + __popc(b & low_mask(at & 31));
-    };
-    int r = warp_row_between(row_start, 0, rows, first) + lane;
-    for (;; r += 32) {
-        long long a = last, e = last;
-        if (r < rows) {
-            a = min(max((long long)__ldg(row_start + r), first), last);
-            e = min(max((long long)__ldg(row_start + r + 1), a), last);
-        }
-        const int n = below((int)(e - first)) - below((int)(a - first));
-        if (n > 0) atomicAdd(tokens + r, n);
-        if (__all_sync(0xFFFFFFFFu, a >= last)) break;      // ascending starts: the rest lies behind the tile
-        if (__shfl_sync(0xFFFFFFFFu, r, 31) >= rows - 1) break;
-    }
+    __shared__ int32_t s_count[kRowsOfCta];
+    const int first = blockIdx.x * rows_of_cta, have = min(rows_of_cta, rows - first);
+    count_rows(row_start, mask, n_tokens, drop_mask, N, first, have, s_count);
+    for (int i = threadIdx.x; i < have; i += 256) tokens[first + i] = s_count[i];
 }
 
 constexpr int kWeightThreads = 1024;
 
-// tokens: counts of the rollouts, or NULL where every token counts.
+// One cluster.  kCount: its CTAs count the tokens of up to kRowsOfCta rollouts each; otherwise `tokens` holds the counts, or is
+// NULL where every token counts.
+template <bool kCount>
 __global__ void __launch_bounds__(kWeightThreads)
-loss_weights_kernel(const int64_t* __restrict__ row_start, const int32_t* __restrict__ tokens, const uint8_t* __restrict__ drop_mask, int N, int rows,
-                    int mode, double scale, float* __restrict__ weight, int64_t* __restrict__ counts) {
+loss_weights_kernel(const int64_t* row_start, const uint8_t* mask, int n_tokens, const int32_t* tokens,
+                    const uint8_t* drop_mask, int N, int rows, int mode, double scale, float* weight, int64_t* counts) {
     grid_begin();
-    __shared__ long long s_tokens[32], s_total;
-    __shared__ int s_live[32], s_rows;
-    const int stride = gridDim.x * kWeightThreads, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    auto tokens_of = [&](int r) -> long long {
-        if (drop_mask && drop_mask[r / N]) return 0;
+    __shared__ long long s_tokens[32], s_total[8];
+    __shared__ int s_live[32], s_rows[8];
+    __shared__ int32_t s_count[kCount ? kRowsOfCta : 1];
+    const auto cluster = cooperative_groups::this_cluster();
+    const int ctas = gridDim.x, lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
+    const int first = (int)((long long)rows * blockIdx.x / ctas), last = (int)((long long)rows * (blockIdx.x + 1) / ctas);
+    if (kCount) {
+        count_rows(row_start, mask, n_tokens, drop_mask, N, first, last - first, s_count);
+        __syncthreads();
+    }
+    const auto tokens_of = [&](int r) -> long long {
+        if (kCount) return s_count[r - first];
         if (tokens) return tokens[r];
+        if (drop_mask && drop_mask[r / N]) return 0;
         return max((long long)(row_start[r + 1] - row_start[r]), 0LL);
     };
-    long long sum = 0;
-    int live = 0;
-    for (long long r = blockIdx.x * kWeightThreads + threadIdx.x; r < rows; r += stride) {
+    const int own = first + (int)threadIdx.x;                  // most batches have no more rollouts than threads
+    const long long own_tokens = own < last ? tokens_of(own) : 0;
+    long long sum = own_tokens;
+    int live = own_tokens > 0;
+    for (long long r = (long long)own + blockDim.x; r < last; r += blockDim.x) {
         const long long n = tokens_of((int)r);
         sum += n;
         live += n > 0;
     }
 #pragma unroll
-    for (int off = 16; off > 0; off >>= 1) {
-        sum += __shfl_xor_sync(0xFFFFFFFFu, sum, off);
-        live += __shfl_xor_sync(0xFFFFFFFFu, live, off);
-    }
+    for (int off = 16; off > 0; off >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, off);
+    live = __reduce_add_sync(0xFFFFFFFFu, live);
     if (lane == 0) { s_tokens[warp] = sum; s_live[warp] = live; }
     __syncthreads();
-    if (threadIdx.x == 0) {
-        for (int w = 1; w < kWeightThreads / 32; ++w) { sum += s_tokens[w]; live += s_live[w]; }
-        s_total = sum;
-        s_rows = live;
+    if (warp == 0) {
+        sum = lane < warps ? s_tokens[lane] : 0;
+        live = __reduce_add_sync(0xFFFFFFFFu, lane < warps ? s_live[lane] : 0);
+#pragma unroll
+        for (int off = 16; off > 0; off >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, off);
+        if (lane < ctas) {                 // to every CTA's own memory: after the barrier nobody reads another's
+            *cluster.map_shared_rank(&s_total[blockIdx.x], lane) = sum;
+            *cluster.map_shared_rank(&s_rows[blockIdx.x], lane) = live;
+        }
     }
-    const auto cluster = cooperative_groups::this_cluster();
     cluster.sync();
     sum = 0;
     live = 0;
-    for (unsigned b = 0; b < gridDim.x; ++b) {
-        sum += *cluster.map_shared_rank(&s_total, b);
-        live += *cluster.map_shared_rank(&s_rows, b);
-    }
-    cluster.sync();                        // nobody leaves while its sums are read
+    for (int c = 0; c < ctas; ++c) { sum += s_total[c]; live += s_rows[c]; }
     if (counts && blockIdx.x == 0 && threadIdx.x == 0) { counts[0] = sum; counts[1] = live; }
-    for (long long r = blockIdx.x * kWeightThreads + threadIdx.x; r < rows; r += stride) {
-        const long long n = tokens_of((int)r);
+    const auto weigh = [&](long long r, long long n) {
         double w = scale;
         if (mode == SR_LOSS_TOKEN_MEAN) w /= (double)sum;
         if (mode == SR_LOSS_ROLLOUT_MEAN) w /= (double)live * (double)n;
         weight[r] = n > 0 ? (float)w : 0.0f;
+    };
+    if (own < last) weigh(own, own_tokens);
+    for (long long r = (long long)own + blockDim.x; r < last; r += blockDim.x) weigh(r, tokens_of((int)r));
+}
+
+// What thread 0 of every CTA does with its sum.  kCluster: the grid is one cluster, whose sums meet in shared memory and become
+// the loss.
+template <bool kCluster>
+__device__ __forceinline__ void leave_sum(PolicyTerms<double> sum, double beta, double* partial, float* loss, float* stats) {
+    if (!kCluster) {
+        if (threadIdx.x == 0) reinterpret_cast<PolicyTerms<double>*>(partial)[blockIdx.x] = sum;
+        return;
+    }
+    __shared__ PolicyTerms<double> s_sum[8];
+    const auto cluster = cooperative_groups::this_cluster();
+    if (threadIdx.x == 0) *cluster.map_shared_rank(&s_sum[blockIdx.x], 0) = sum;
+    cluster.sync();                        // the first CTA's memory alone is read after it
+    if (blockIdx.x == 0 && threadIdx.x == 0) {
+        for (unsigned c = 1; c < gridDim.x; ++c) add_terms(sum, s_sum[c]);
+        write_policy_loss(sum, beta, loss, stats);
     }
 }
 
-// kCluster: the grid is one cluster and its sums meet in shared memory: one launch.
+// kCluster: one launch, see above.  A warp has a run of tokens, 128 at a time;
+// the next 128 are on their way while it works on these.
 template <bool kVec, bool kCluster>
-__global__ void __launch_bounds__(kCluster ? 1024 : 256)
-policy_loss_kernel(PolicyBatch b, const float* logp, float* d_logp, int n, double* __restrict__ partial, float* __restrict__ loss, float* __restrict__ stats) {
+__global__ void __launch_bounds__(kCluster ? 1024 : 256, kCluster ? 1 : 4)
+policy_loss_kernel(const __grid_constant__ PolicyBatch b, const float* logp, float* d_logp, int n, double* partial, float* loss,
+                   float* stats) {
     grid_begin();
-    const int lane = threadIdx.x & 31;
+    const int lane = threadIdx.x & 31, warps = blockDim.x >> 5;
+    const int all = gridDim.x * warps, warp = blockIdx.x * warps + (threadIdx.x >> 5);
+    const long long lots = ((long long)n + 127) >> 7;
+    long long lot = lots * warp / all;
+    const long long end = lots * (warp + 1) / all;
     PolicyTerms<double> sum = {0.0, 0.0, 0.0, 0.0};
-    const long long rows_begin = b.rows > 0 ? __ldg(b.row_start) : 0, rows_end = b.rows > 0 ? __ldg(b.row_start + b.rows) : 0;
-    for (long long t0 = ((long long)blockIdx.x * blockDim.x + threadIdx.x) * 4; t0 - 4 * lane < n; t0 += 4LL * gridDim.x * blockDim.x) {
-        const long long w0 = t0 - 4 * lane;                     // the warp's tokens are w0 .. w0 + 127
-        const int have = (int)max(0LL, min(4LL, n - t0));
-        float lp[4] = {0.0f, 0.0f, 0.0f, 0.0f}, grad[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-        if (kVec && have == 4) {
+    struct Four {
+        float lp[4], old_logp[4], ref_logp[4];
+        uint32_t mask;
+    } next;
+    auto load = [&](long long t0) {
+        if (kVec && t0 + 4 <= n) {
             const float4 v = *reinterpret_cast<const float4*>(logp + t0);
-            lp[0] = v.x; lp[1] = v.y; lp[2] = v.z; lp[3] = v.w;
-        } else {
-            for (int k = 0; k < have; ++k) lp[k] = logp[t0 + k];
+            next.lp[0] = v.x; next.lp[1] = v.y; next.lp[2] = v.z; next.lp[3] = v.w;
+            if (b.old_logp) {
+                const float4 o = *reinterpret_cast<const float4*>(b.old_logp + t0);
+                next.old_logp[0] = o.x; next.old_logp[1] = o.y; next.old_logp[2] = o.z; next.old_logp[3] = o.w;
+            }
+            if (b.ref_logp) {
+                const float4 f = *reinterpret_cast<const float4*>(b.ref_logp + t0);
+                next.ref_logp[0] = f.x; next.ref_logp[1] = f.y; next.ref_logp[2] = f.z; next.ref_logp[3] = f.w;
+            }
+            next.mask = b.mask ? *reinterpret_cast<const uint32_t*>(b.mask + t0) : 0xFFFFFFFFu;
+            return;
         }
+        next.mask = 0u;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            if (t0 + k >= n) continue;
+            next.lp[k] = logp[t0 + k];
+            if (b.old_logp) next.old_logp[k] = b.old_logp[t0 + k];
+            if (b.ref_logp) next.ref_logp[k] = b.ref_logp[t0 + k];
+            next.mask |= (b.mask ? (uint32_t)b.mask[t0 + k] : 1u) << (8 * k);
+        }
+    };
+    if (lot < end) load((lot << 7) + 4 * lane);
+    RowWalk walk;
+    if (lot < end && b.rows > 0) walk.find(b.row_start, b.rows, lot << 7);
+    for (; lot < end; ++lot) {
+        const Four four = next;
+        const long long w0 = lot << 7, t0 = w0 + 4 * lane;
+        if (lot + 1 < end) load(t0 + 128);
+        float grad[4] = {0.0f, 0.0f, 0.0f, 0.0f};
         PolicyTerms<float> mine = {0.0f, 0.0f, 0.0f, 0.0f};
         if (b.rows > 0) {
-            const int r_first = warp_row_between(b.row_start, 0, b.rows, w0);
-            const int r_last = warp_row_between(b.row_start, r_first, b.rows, min(w0 + 127, (long long)n - 1));
-            int r = r_first == r_last ? r_first : row_between(b.row_start, r_first, r_last + 1, t0);
-            for (int k = 0; k < have; ++k) {
-                const long long t = t0 + k;
-                if (t < rows_begin || t >= rows_end || (b.mask && b.mask[t] == 0)) continue;
-                while (r < r_last && __ldg(b.row_start + r + 1) <= t) ++r;
-                const float w = __ldg(b.weight + r);
-                if (w == 0.0f) continue;
+            long long until;
+            int r = walk.row_of(w0, t0, until);
+            // of the four tokens, those from skip to stop lie in a rollout
+            const int skip = (int)max(0LL, min(4LL, walk.begin - t0)), stop = (int)max(0LL, min(4LL, walk.end - t0));
+            PolicyToken k;
+            k.weight = b.weight[r];
+            k.adv = b.adv[r];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const long long t = t0 + j;
+                if (t >= until) {                                // into the next rollout, or past empty ones
+                    ++r;
+                    until = r + 1 < b.rows ? b.row_start[r + 1] : INT64_MAX;
+                    if (t >= until) {
+                        r = row_between(b.row_start, r, b.rows, t);
+                        until = r + 1 < b.rows ? b.row_start[r + 1] : INT64_MAX;
+                    }
+                    k.weight = b.weight[r];
+                    k.adv = b.adv[r];
+                }
+                if (j < skip || j >= stop || ((four.mask >> (8 * j)) & 0xFFu) == 0u || k.weight == 0.0f) continue;
+                k.old_logp = four.old_logp[j];
+                k.ref_logp = four.ref_logp[j];
                 PolicyTerms<float> term;
-                grad[k] = policy_token(b, (size_t)t, lp[k], __ldg(b.adv + r), w, term);
+                grad[j] = policy_token(b, k, four.lp[j], term);
                 mine.gain += term.gain;
                 mine.kl += term.kl;
                 mine.clipped += term.clipped;
@@ -164,41 +258,30 @@ policy_loss_kernel(PolicyBatch b, const float* logp, float* d_logp, int n, doubl
         sum.clipped += (double)mine.clipped;
         sum.rho += (double)mine.rho;
         if (d_logp) {
-            if (kVec && have == 4) *reinterpret_cast<float4*>(d_logp + t0) = make_float4(grad[0], grad[1], grad[2], grad[3]);
-            else
-                for (int k = 0; k < have; ++k) d_logp[t0 + k] = grad[k];
+            if (kVec && t0 + 4 <= n) {
+                *reinterpret_cast<float4*>(d_logp + t0) = make_float4(grad[0], grad[1], grad[2], grad[3]);
+            } else {
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    if (t0 + j < n) d_logp[t0 + j] = grad[j];
+            }
         }
     }
-    sum = block_sum(sum);
-    if (kCluster) {
-        __shared__ PolicyTerms<double> s_sum;
-        const auto cluster = cooperative_groups::this_cluster();
-        if (threadIdx.x == 0) s_sum = sum;
-        cluster.sync();
-        if (blockIdx.x == 0 && threadIdx.x == 0) {
-            for (unsigned c = 1; c < gridDim.x; ++c) add_terms(sum, *cluster.map_shared_rank(&s_sum, c));
-            write_policy_loss(sum, b.beta, loss, stats);
-        }
-        cluster.sync();                        // nobody leaves while its sums are read
-    } else if (threadIdx.x == 0) {
-        reinterpret_cast<PolicyTerms<double>*>(partial)[blockIdx.x] = sum;
-    }
+    leave_sum<kCluster>(block_sum(sum), b.beta, partial, loss, stats);
 }
 
 // Sums of terms: of the CTAs before (double), or of the tokens themselves (float).
-template <typename F>
-__global__ void __launch_bounds__(256)
-sum_terms_kernel(const PolicyTerms<F>* __restrict__ terms, int n, double beta, PolicyTerms<double>* __restrict__ partial, float* __restrict__ loss, float* __restrict__ stats) {
+template <typename F, bool kCluster>
+__global__ void __launch_bounds__(1024)
+sum_terms_kernel(const PolicyTerms<F>* terms, int n, double beta, double* partial, float* loss, float* stats) {
     grid_begin();
     PolicyTerms<double> sum = {0.0, 0.0, 0.0, 0.0};
-    for (long long i = blockIdx.x * 256 + threadIdx.x; i < n; i += gridDim.x * 256) {
+#pragma unroll 4
+    for (long long i = (long long)blockIdx.x * blockDim.x + threadIdx.x; i < n; i += (long long)gridDim.x * blockDim.x) {
         const PolicyTerms<F> t = terms[i];
         add_terms(sum, PolicyTerms<double>{(double)t.gain, (double)t.kl, (double)t.clipped, (double)t.rho});
     }
-    sum = block_sum(sum);
-    if (threadIdx.x != 0) return;
-    if (gridDim.x == 1) write_policy_loss(sum, beta, loss, stats);
-    else partial[blockIdx.x] = sum;
+    leave_sum<kCluster>(block_sum(sum), beta, partial, loss, stats);
 }
 
 }  // namespace
@@ -210,38 +293,43 @@ int launch_loss_weights(const int64_t* row_start, const uint8_t* mask, int32_t n
         if (counts) SR_CUDA_TRY(cudaMemsetAsync(counts, 0, 2 * sizeof(int64_t), s));
         return SR_OK;
     }
-    int32_t* const tokens = mask ? static_cast<int32_t*>(ws) : nullptr;
-    if (mask) {
-        SR_CUDA_TRY(cudaMemsetAsync(tokens, 0, (size_t)rows * sizeof(int32_t), s));
-        const int tiles = (int)(((long long)n_tokens + kMaskTile - 1) / kMaskTile);
-        if (tiles > 0) SR_LAUNCH("count_tokens_kernel", count_tokens_kernel, (tiles + 7) / 8, 256, 0, s, row_start, rows, mask, n_tokens, tokens);
+    // Masked batches of up to 2048 rollouts and a million tokens count in the cluster itself, in one launch: eight SMs read the
+    // mask, larger ones on all SMs in a launch of its own.
+    const bool here = mask != nullptr && rows <= 8 * kRowsOfCta && n_tokens <= 1 << 20;
+    int32_t* const tokens = mask && !here ? static_cast<int32_t*>(ws) : nullptr;
+    if (tokens) {
+        const int of_cta = min(kRowsOfCta, max(8, rows / (148 * 8) & ~7));
+        SR_LAUNCH("count_tokens_kernel", count_tokens_kernel, (rows + of_cta - 1) / of_cta, 256, 0, s, row_start, rows, mask, n_tokens, drop_mask, N, of_cta, tokens);
     }
-    int ctas = 1;                                  // up to the portable cluster size
-    while (ctas < 8 && ctas * kWeightThreads < rows) ctas *= 2;
-    return launch_as(true, ctas, "loss_weights_kernel", loss_weights_kernel, ctas, kWeightThreads, 0, s, row_start, tokens, drop_mask, N, rows, mode, scale, weight, counts);
+    // up to the portable cluster size
+    const int ctas = here ? min(8, (rows + 31) / 32) : min(8, (int)(((long long)rows + kWeightThreads - 1) / kWeightThreads));
+    const int threads = here ? kWeightThreads : min(kWeightThreads, (rows + 31) & ~31);
+    return launch_as(true, ctas, "loss_weights_kernel", here ? loss_weights_kernel<true> : loss_weights_kernel<false>, ctas, threads, 0, s, row_start, mask, n_tokens, tokens,
+                     drop_mask, N, rows, mode, scale, weight, counts);
 }
 
+// Up to 32768 tokens, four a thread, and sums of up to 131072 are one cluster's work: one launch.
 int launch_sum_terms(const PolicyTerms<float>* terms, int n, double beta, float* loss, float* stats, double* partial, cudaStream_t s) {
-    auto* const part = reinterpret_cast<PolicyTerms<double>*>(partial);
-    const int blocks = n > 8192 ? min(kMaxPartials, (n + 2047) / 2048) : 1;
-    SR_LAUNCH("sum_terms_kernel", sum_terms_kernel<float>, blocks, 256, 0, s, terms, n, beta, part, loss, stats);
-    if (blocks > 1) SR_LAUNCH("sum_terms_kernel", sum_terms_kernel<double>, 1, 256, 0, s, part, blocks, beta, part, loss, stats);
+    if (n <= 1 << 17) {
+        const int ctas = max(1, min(8, (n + 1023) / 1024)), threads = max(32, min(1024, (n + 31) & ~31));
+        return launch_as(true, ctas, "sum_terms_kernel", sum_terms_kernel<float, true>, ctas, threads, 0, s, terms, n, beta, partial, loss, stats);
+    }
+    const int blocks = min(kMaxPartials, (n + 4095) / 4096);
+    SR_LAUNCH("sum_terms_kernel", sum_terms_kernel<float, false>, blocks, 1024, 0, s, terms, n, beta, partial, loss, stats);
+    SR_LAUNCH("sum_terms_kernel", sum_terms_kernel<double, true>, 1, 1024, 0, s, reinterpret_cast<const PolicyTerms<double>*>(partial), blocks, beta, partial, loss, stats);
     return SR_OK;
 }
 
 int launch_policy_loss(const PolicyBatch& b, const float* logp, int32_t n, float* loss, float* d_logp, float* stats, double* partial, cudaStream_t s) {
-    const uintptr_t at = reinterpret_cast<uintptr_t>(logp) | reinterpret_cast<uintptr_t>(d_logp);
-    const bool vec = (at & 15) == 0;
+    const uintptr_t at = reinterpret_cast<uintptr_t>(logp) | reinterpret_cast<uintptr_t>(d_logp) | reinterpret_cast<uintptr_t>(b.old_logp) | reinterpret_cast<uintptr_t>(b.ref_logp);
+    const bool vec = (at & 15) == 0 && (reinterpret_cast<uintptr_t>(b.mask) & 3) == 0;
     if (n <= 8 * 1024 * 4) {
-        int ctas = 1;
-        while (ctas < 8 && ctas * 1024 < n) ctas *= 2;
-        const int threads = max(32, ((n + ctas * 4 - 1) / (ctas * 4) + 31) & ~31);
+        const int lots = (n + 127) / 128, ctas = max(1, min(8, (lots + 3) / 4)), threads = max(1, min(32, (lots + ctas - 1) / ctas)) * 32;
         return launch_as(true, ctas, "policy_loss_kernel", vec ? policy_loss_kernel<true, true> : policy_loss_kernel<false, true>, ctas, threads, 0, s, b, logp, d_logp, n, partial, loss, stats);
     }
-    const int blocks = (int)min((long long)kMaxPartials, ((long long)n + 1023) / 1024);
+    const int blocks = (int)min((long long)(148 * 4), ((long long)n + 1023) / 1024);
     SR_LAUNCH("policy_loss_kernel", vec ? policy_loss_kernel<true, false> : policy_loss_kernel<false, false>, blocks, 256, 0, s, b, logp, d_logp, n, partial, loss, stats);
-    auto* const part = reinterpret_cast<PolicyTerms<double>*>(partial);
-    SR_LAUNCH("sum_terms_kernel", sum_terms_kernel<double>, 1, 256, 0, s, part, blocks, b.beta, part, loss, stats);
+    SR_LAUNCH("sum_terms_kernel", sum_terms_kernel<double, true>, 1, 1024, 0, s, reinterpret_cast<const PolicyTerms<double>*>(partial), blocks, b.beta, partial, loss, stats);
     return SR_OK;
 }
 

@@ -15,6 +15,11 @@ struct PolicyBatch {
     const uint8_t* mask;
     int rows;
     double clip_low, clip_high, beta;
+    float low, high;                 // 1 - clip_low, 1 + clip_high
+};
+// What the loss reads of one token beside its log-probability.
+struct PolicyToken {
+    float old_logp, ref_logp, adv, weight;
 };
 
 // Weighted terms of one token, or their sums.
@@ -25,27 +30,71 @@ struct PolicyTerms {
 
 // Largest r in [lo, hi) with start[r] <= t, by one thread; lo where there is none.  Whatever the array holds, the result lies in
 // the range.
-__device__ __forceinline__ int row_between(const int64_t* __restrict__ start, int lo, int hi, long long t) {
+__device__ __forceinline__ int row_between(const int64_t* start, int lo, int hi, long long t) {
     while (hi - lo > 1) {
         const int mid = lo + ((hi - lo) >> 1);
-        if (__ldg(start + mid) <= t) lo = mid;
+        if (start[mid] <= t) lo = mid;
         else hi = mid;
     }
     return lo;
 }
 
 // The same by a whole warp, 32 places at a time: three dependent loads for 30000 rollouts.
-__device__ __forceinline__ int warp_row_between(const int64_t* __restrict__ start, int lo, int hi, long long t) {
+__device__ __forceinline__ int warp_row_between(const int64_t* start, int lo, int hi, long long t) {
     const int lane = threadIdx.x & 31;
     while (hi - lo > 1) {
         const int step = (hi - lo + 31) >> 5;              // below hi - lo: the range shrinks
         const long long at = lo + (long long)lane * step;
-        const bool below = lane == 0 || (at < hi && __ldg(start + at) <= t);
+        const bool below = lane == 0 || (at < hi && start[at] <= t);
         lo += (31 - __clz(__ballot_sync(0xFFFFFFFFu, below))) * step;
         hi = min(hi, lo + step);
     }
     return lo;
 }
+
+// The rollouts of the tokens that a warp passes through in ascending order, 128 at a time, four a lane.
+struct RowWalk {
+    const int64_t* start;
+    int rows, r;                     // r: the rollout of the first token of the 128 at hand, or the one before the first
+    long long begin, end;            // tokens that lie in a rollout
+
+    __device__ __forceinline__ void find(const int64_t* row_start, int n_rows, long long first) {
+        start = row_start;
+        rows = n_rows;
+        begin = start[0];
+        end = start[rows];
+        r = warp_row_between(start, 0, rows, first);
+    }
+    // Row of token t0 (this lane's) of the 128 that begin at w0, and the token behind its last; moves on.  Lanes look at the
+    // next 32 starts together; where the 128 tokens have more rollouts they search for themselves.
+    __device__ __forceinline__ int row_of(long long w0, long long t0, long long& until) {
+        const int lane = threadIdx.x & 31;
+        const int at = r + 1 + lane;
+        const long long next = at < rows ? start[at] : INT64_MAX;       // start of rollout r + 1 + lane
+        const unsigned within = __ballot_sync(0xFFFFFFFFu, next <= w0 + 127);
+        int row = r;
+        if (within == 0u) {                                      // all in one rollout
+            until = INT64_MAX;
+        } else if (within != 0xFFFFFFFFu) {
+            // as many of the (ascending) starts as are not behind t0
+            int before = 0;
+#pragma unroll
+            for (int step = 16; step > 0; step >>= 1) {
+                const long long probe = __shfl_sync(0xFFFFFFFFu, next, before + step - 1);
+                if (probe <= t0) before += step;
+            }
+            row = r + before;
+            until = __shfl_sync(0xFFFFFFFFu, next, before & 31);
+            r += __popc(__ballot_sync(0xFFFFFFFFu, next <= w0 + 128));
+        } else {
+            const int last = warp_row_between(start, r, rows, w0 + 128);
+            row = row_between(start, r, last + 1, t0);
+            until = row + 1 < rows ? start[row + 1] : INT64_MAX;
+            r = last;
+        }
+        return row;
+    }
+};
 
 // Terms of a token that counts, and the gradient of its log-probability.  `lp` is fp32 where it came from memory, fp64
 // where it has just been computed.
@@ -55,26 +104,25 @@ __device__ __forceinline__ int warp_row_between(const int64_t* __restrict__ star
 // wholly wrong gradient).  And e^d - 1 - d of policies that nearly agree: below 1/2 it is d^2 times the Taylor series of
 // (e^d - 1 - d) / d^2, cut where the next term is below 2^-29 of the sum.
 template <typename F>
-__device__ __forceinline__ float policy_token(const PolicyBatch& b, size_t t, F lp, float A, float w, PolicyTerms<float>& out) {
+__device__ __forceinline__ float policy_token(const PolicyBatch& b, const PolicyToken& k, F lp, PolicyTerms<float>& out) {
+    const float A = k.adv, w = k.weight;
     float rho = lp == lp ? 1.0f : (float)lp;        // a NaN stays one
-    const float low = (float)(1.0 - b.clip_low), high = (float)(1.0 + b.clip_high);
+    const float border = A > 0.0f ? b.high : b.low;
     bool clipped = false;
     if (b.old_logp) {
-        const F delta = lp - (F)b.old_logp[t];
+        const F delta = lp - (F)k.old_logp;
         rho = expf((float)delta);
-        if (A > 0.0f) clipped = rho > high;
-        else if (A < 0.0f) clipped = rho < low;
-        const float border = A > 0.0f ? high : low;
+        clipped = A > 0.0f ? rho > border : A < 0.0f && rho < border;
         if (fabsf(rho - border) <= 9.5367431640625e-7f * border) {
-            const double exact = exp((double)lp - (double)b.old_logp[t]);
+            const double exact = exp((double)lp - (double)k.old_logp);
             clipped = A > 0.0f ? exact > 1.0 + b.clip_high : A < 0.0f && exact < 1.0 - b.clip_low;
         }
     }
-    const float gain = A > 0.0f ? A * (clipped ? high : rho) : A < 0.0f ? A * (clipped ? low : rho) : A;   // A = 0, or NaN
+    const float gain = A == 0.0f ? 0.0f : A * (clipped ? border : rho);
     float d_lp = clipped || A == 0.0f ? 0.0f : -A * rho;
     float kl = 0.0f;
     if (b.ref_logp) {
-        const float d = (float)((F)b.ref_logp[t] - lp);
+        const float d = (float)((F)k.ref_logp - lp);
         float em1;
         if (fabsf(d) < 0.5f) {
             float s = 1.0f / 362880.0f;

@@ -43,7 +43,7 @@ int check_gradient(const void* logits, int32_t dtype, int32_t n_tokens, int32_t 
 }
 
 int check_policy(const float* adv, const float* weight, const int64_t* row_start, int32_t n_rollouts, double clip_low, double clip_high, double beta, const float* loss) {
-    if (n_rollouts < 0) return SR_ERR_BAD_N;
+    if (n_rollouts < 0 || n_rollouts > (1 << 30)) return SR_ERR_BAD_N;
     if (!(clip_low >= 0.0 && clip_high >= 0.0 && beta >= 0.0) || isinf(clip_low) || isinf(clip_high) || isinf(beta)) return SR_ERR_BAD_VALUE;
     if (loss == nullptr || (n_rollouts > 0 && (adv == nullptr || weight == nullptr || row_start == nullptr))) return SR_ERR_NULL;
     if (!aligned(row_start, 8)) return SR_ERR_ALIGN;
@@ -118,7 +118,7 @@ int sr_policy_loss(const float* logp, const float* logp_old, const float* logp_r
     if (rc != SR_OK) return rc;
     if (n_tokens > 0 && logp == nullptr) return SR_ERR_NULL;
     if (short_of(workspace, workspace_bytes, kPartialBytes)) return SR_ERR_WORKSPACE;
-    const PolicyBatch b{logp_old, logp_ref, adv, weight, row_start, mask, n_rollouts, clip_low, clip_high, beta};
+    const PolicyBatch b{logp_old, logp_ref, adv, weight, row_start, mask, n_rollouts, clip_low, clip_high, beta, (float)(1.0 - clip_low), (float)(1.0 + clip_high)};
     return launch_policy_loss(b, logp, n_tokens, loss, d_logp, stats, static_cast<double*>(workspace), static_cast<cudaStream_t>(stream));
 }
 
@@ -138,7 +138,7 @@ int sr_policy_loss_logits(const void* logits, int32_t dtype, int32_t n_tokens, i
     rc = check_gradient(logits, dtype, n_tokens, vocab, pitch, d_logits, d_pitch);
     if (rc != SR_OK) return rc;
     if (short_of(workspace, workspace_bytes, sr_policy_loss_logits_workspace_bytes(n_tokens))) return SR_ERR_WORKSPACE;
-    const PolicyBatch b{logp_old, logp_ref, adv, weight, row_start, mask, n_rollouts, clip_low, clip_high, beta};
+    const PolicyBatch b{logp_old, logp_ref, adv, weight, row_start, mask, n_rollouts, clip_low, clip_high, beta, (float)(1.0 - clip_low), (float)(1.0 + clip_high)};
     StepScratch ws;
     ws.partial = static_cast<double*>(workspace);
     ws.terms = reinterpret_cast<PolicyTerms<float>*>(static_cast<char*>(workspace) + kPartialBytes);

@@ -170,25 +170,82 @@ __device__ __forceinline__ void leave_sum(PolicyTerms<double> sum, double beta, 
     }
 }
 
+// policy_token for the rare token that the code below leaves to it.
+__device__ __noinline__ float one_token(const PolicyBatch& b, float old_logp, float ref_logp, float adv, float weight, float lp, PolicyTerms<float>& out) {
+    return policy_token(b, PolicyToken{old_logp, ref_logp, adv, weight}, lp, out);
+}
+// policy_token of four tokens side by side, without branches: one that does not count (bit 8 j of `counts`) has weight 0 and
+// policies that agree.  What needs another look (a ratio at a border of the clip range, numbers near overflow) gets it afterwards.
+__device__ __forceinline__ void four_tokens(const PolicyBatch& b, const float (&lp)[4], const float (&old_logp)[4], const float (&ref_logp)[4], const float (&w)[4],
+                                            const float (&a)[4], uint32_t counts, float (&grad)[4], PolicyTerms<float>& sum) {
+    bool again = false;
+    float gain[4], kl[4], rho[4], past[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const bool is = (counts >> (8 * j)) & 1u;
+        const float A = a[j], border = A > 0.0f ? b.high : b.low, side = A > 0.0f ? 1.0f : A < 0.0f ? -1.0f : 0.0f;
+        float delta = b.old_logp ? lp[j] - old_logp[j] : lp[j] - lp[j];          // a NaN stays one
+        if (!b.old_logp && isinf(lp[j])) delta = 0.0f;
+        delta = is ? delta : 0.0f;
+        rho[j] = expf(delta);
+        const float over = rho[j] - border;
+        past[j] = over * side > 0.0f ? 1.0f : 0.0f;
+        gain[j] = A * (over * side > 0.0f ? border : rho[j]);
+        grad[j] = over * side > 0.0f ? 0.0f : -gain[j];
+        kl[j] = 0.0f;
+        again |= is && (fabsf(over) <= 9.5367431640625e-7f * border || delta > 80.0f);
+    }
+    if (b.ref_logp) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const float d = (counts >> (8 * j)) & 1u ? ref_logp[j] - lp[j] : 0.0f;
+            float em1;
+            exp_less_line_near(d, em1, kl[j]);
+            grad[j] = fmaf(-b.beta32, em1, grad[j]);
+            again |= fabsf(d) > 80.0f;
+        }
+    }
+    PolicyTerms<float> term[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const bool is = (counts >> (8 * j)) & 1u;
+        const float weight = is ? w[j] : 0.0f;
+        term[j] = PolicyTerms<float>{weight * gain[j], weight * kl[j], weight * past[j], weight * rho[j]};
+        grad[j] = is ? weight * grad[j] : 0.0f;
+    }
+    if (again) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if ((counts >> (8 * j)) & 1u) grad[j] = one_token(b, old_logp[j], ref_logp[j], a[j], w[j], lp[j], term[j]);
+    }
+    sum.gain += (term[0].gain + term[1].gain) + (term[2].gain + term[3].gain);
+    sum.kl += (term[0].kl + term[1].kl) + (term[2].kl + term[3].kl);
+    sum.clipped += (term[0].clipped + term[1].clipped) + (term[2].clipped + term[3].clipped);
+    sum.rho += (term[0].rho + term[1].rho) + (term[2].rho + term[3].rho);
+}
+
 // kCluster: one launch, see above.  A warp has a run of tokens, 128 at a time;
-// the next 128 are on their way while it works on these.
+// the next two lots are on their way while it works on one.
 template <bool kVec, bool kCluster>
-__global__ void __launch_bounds__(kCluster ? 1024 : 256, kCluster ? 1 : 4)
+__global__ void __launch_bounds__(kCluster ? 512 : 256, kCluster ? 1 : 2)
 policy_loss_kernel(const __grid_constant__ PolicyBatch b, const float* logp, float* d_logp, int n, double* partial, float* loss,
                    float* stats) {
     grid_begin();
     const int lane = threadIdx.x & 31, warps = blockDim.x >> 5;
     const int all = gridDim.x * warps, warp = blockIdx.x * warps + (threadIdx.x >> 5);
+    const uint32_t tokens = (uint32_t)n;                       // token numbers are unsigned: the last lot may end behind 2^31
     const long long lots = ((long long)n + 127) >> 7;
-    long long lot = lots * warp / all;
-    const long long end = lots * (warp + 1) / all;
+    uint32_t lot = (uint32_t)(lots * warp / all);
+    const uint32_t end = (uint32_t)(lots * (warp + 1) / all);
     PolicyTerms<double> sum = {0.0, 0.0, 0.0, 0.0};
+    PolicyTerms<float> mine = {0.0f, 0.0f, 0.0f, 0.0f};
     struct Four {
         float lp[4], old_logp[4], ref_logp[4];
         uint32_t mask;
-    } next;
-    auto load = [&](long long t0) {
-        if (kVec && t0 + 4 <= n) {
+    } next, later;
+    auto load = [&](uint32_t t0) {
+        Four next;
+        if (kVec && t0 + 4 <= tokens) {
             const float4 v = *reinterpret_cast<const float4*>(logp + t0);
             next.lp[0] = v.x; next.lp[1] = v.y; next.lp[2] = v.z; next.lp[3] = v.w;
             if (b.old_logp) {
@@ -200,70 +257,64 @@ policy_loss_kernel(const __grid_constant__ PolicyBatch b, const float* logp, flo
                 next.ref_logp[0] = f.x; next.ref_logp[1] = f.y; next.ref_logp[2] = f.z; next.ref_logp[3] = f.w;
             }
             next.mask = b.mask ? *reinterpret_cast<const uint32_t*>(b.mask + t0) : 0xFFFFFFFFu;
-            return;
+            return next;
         }
         next.mask = 0u;
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-            if (t0 + k >= n) continue;
+            if (t0 + k >= tokens) continue;
             next.lp[k] = logp[t0 + k];
             if (b.old_logp) next.old_logp[k] = b.old_logp[t0 + k];
             if (b.ref_logp) next.ref_logp[k] = b.ref_logp[t0 + k];
             next.mask |= (b.mask ? (uint32_t)b.mask[t0 + k] : 1u) << (8 * k);
         }
+        return next;
     };
-    if (lot < end) load((lot << 7) + 4 * lane);
+    if (lot < end) next = load((lot << 7) + 4 * lane);
+    if (lot + 1 < end) later = load((lot << 7) + 128 + 4 * lane);
     RowWalk walk;
-    if (lot < end && b.rows > 0) walk.find(b.row_start, b.rows, lot << 7);
+    if (lot < end && b.rows > 0) walk.find(b, lot << 7);
     for (; lot < end; ++lot) {
         const Four four = next;
-        const long long w0 = lot << 7, t0 = w0 + 4 * lane;
-        if (lot + 1 < end) load(t0 + 128);
+        next = later;
+        const uint32_t w0 = lot << 7, t0 = w0 + 4 * lane;
+        if (lot + 2 < end) later = load(t0 + 256);
         float grad[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-        PolicyTerms<float> mine = {0.0f, 0.0f, 0.0f, 0.0f};
         if (b.rows > 0) {
-            long long until;
-            int r = walk.row_of(w0, t0, until);
-            // of the four tokens, those from skip to stop lie in a rollout
-            const int skip = (int)max(0LL, min(4LL, walk.begin - t0)), stop = (int)max(0LL, min(4LL, walk.end - t0));
-            PolicyToken k;
-            k.weight = b.weight[r];
-            k.adv = b.adv[r];
+            uint32_t counts = four.mask;
+            if (w0 < walk.begin || walk.end - w0 < 128u || w0 >= walk.end) {    // some lie in no rollout
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const long long t = t0 + j;
-                if (t >= until) {                                // into the next rollout, or past empty ones
-                    ++r;
-                    until = r + 1 < b.rows ? b.row_start[r + 1] : INT64_MAX;
-                    if (t >= until) {
-                        r = row_between(b.row_start, r, b.rows, t);
-                        until = r + 1 < b.rows ? b.row_start[r + 1] : INT64_MAX;
-                    }
-                    k.weight = b.weight[r];
-                    k.adv = b.adv[r];
-                }
-                if (j < skip || j >= stop || ((four.mask >> (8 * j)) & 0xFFu) == 0u || k.weight == 0.0f) continue;
-                k.old_logp = four.old_logp[j];
-                k.ref_logp = four.ref_logp[j];
-                PolicyTerms<float> term;
-                grad[j] = policy_token(b, k, four.lp[j], term);
-                mine.gain += term.gain;
-                mine.kl += term.kl;
-                mine.clipped += term.clipped;
-                mine.rho += term.rho;
+                for (int j = 0; j < 4; ++j)
+                    if (t0 + j < walk.begin || t0 + j >= walk.end) counts &= ~(0xFFu << (8 * j));
+            }
+            counts = __vminu4(counts, 0x01010101u);
+            float w[4], a[4];
+            if (walk.one_rollout(w0, w[0], a[0])) {
+                w[1] = w[2] = w[3] = w[0];
+                a[1] = a[2] = a[3] = a[0];
+                if (w[0] != 0.0f) four_tokens(b, four.lp, four.old_logp, four.ref_logp, w, a, counts, grad, mine);
+            } else {
+                walk.several_rollouts(w0, t0, w, a);
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    if (w[j] == 0.0f) counts &= ~(1u << (8 * j));
+                four_tokens(b, four.lp, four.old_logp, four.ref_logp, w, a, counts, grad, mine);
             }
         }
-        sum.gain += (double)mine.gain;
-        sum.kl += (double)mine.kl;
-        sum.clipped += (double)mine.clipped;
-        sum.rho += (double)mine.rho;
+        if ((lot & 3u) == 3u || lot + 1 == end) {        // fp32 over up to 16 tokens, fp64 from there on
+            sum.gain += (double)mine.gain;
+            sum.kl += (double)mine.kl;
+            sum.clipped += (double)mine.clipped;
+            sum.rho += (double)mine.rho;
+            mine = PolicyTerms<float>{0.0f, 0.0f, 0.0f, 0.0f};
+        }
         if (d_logp) {
-            if (kVec && t0 + 4 <= n) {
+            if (kVec && t0 + 4 <= tokens) {
                 *reinterpret_cast<float4*>(d_logp + t0) = make_float4(grad[0], grad[1], grad[2], grad[3]);
             } else {
 #pragma unroll
                 for (int j = 0; j < 4; ++j)
-                    if (t0 + j < n) d_logp[t0 + j] = grad[j];
+                    if (t0 + j < tokens) d_logp[t0 + j] = grad[j];
             }
         }
     }
@@ -293,9 +344,9 @@ int launch_loss_weights(const int64_t* row_start, const uint8_t* mask, int32_t n
         if (counts) SR_CUDA_TRY(cudaMemsetAsync(counts, 0, 2 * sizeof(int64_t), s));
         return SR_OK;
     }
-    // Masked batches of up to 2048 rollouts and a million tokens count in the cluster itself, in one launch: eight SMs read the
-    // mask, larger ones on all SMs in a launch of its own.
-    const bool here = mask != nullptr && rows <= 8 * kRowsOfCta && n_tokens <= 1 << 20;
+    // Masked batches of up to 2048 rollouts and 65536 tokens are counted in the cluster itself, in one launch; eight SMs would take
+    // 15 us for 770000 tokens, a launch of its own on all SMs 5.
+    const bool here = mask != nullptr && rows <= 8 * kRowsOfCta && n_tokens <= 1 << 16;
     int32_t* const tokens = mask && !here ? static_cast<int32_t*>(ws) : nullptr;
     if (tokens) {
         const int of_cta = min(kRowsOfCta, max(8, rows / (148 * 8) & ~7));
@@ -324,10 +375,10 @@ int launch_policy_loss(const PolicyBatch& b, const float* logp, int32_t n, float
     const uintptr_t at = reinterpret_cast<uintptr_t>(logp) | reinterpret_cast<uintptr_t>(d_logp) | reinterpret_cast<uintptr_t>(b.old_logp) | reinterpret_cast<uintptr_t>(b.ref_logp);
     const bool vec = (at & 15) == 0 && (reinterpret_cast<uintptr_t>(b.mask) & 3) == 0;
     if (n <= 8 * 1024 * 4) {
-        const int lots = (n + 127) / 128, ctas = max(1, min(8, (lots + 3) / 4)), threads = max(1, min(32, (lots + ctas - 1) / ctas)) * 32;
+        const int lots = (n + 127) / 128, ctas = max(1, min(8, (lots + 15) / 16)), threads = max(1, min(16, (lots + ctas - 1) / ctas)) * 32;
         return launch_as(true, ctas, "policy_loss_kernel", vec ? policy_loss_kernel<true, true> : policy_loss_kernel<false, true>, ctas, threads, 0, s, b, logp, d_logp, n, partial, loss, stats);
     }
-    const int blocks = (int)min((long long)(148 * 4), ((long long)n + 1023) / 1024);
+    const int blocks = (int)min((long long)(148 * 2), ((long long)n + 1023) / 1024);
     SR_LAUNCH("policy_loss_kernel", vec ? policy_loss_kernel<true, false> : policy_loss_kernel<false, false>, blocks, 256, 0, s, b, logp, d_logp, n, partial, loss, stats);
     SR_LAUNCH("sum_terms_kernel", sum_terms_kernel<double, true>, 1, 1024, 0, s, reinterpret_cast<const PolicyTerms<double>*>(partial), blocks, b.beta, partial, loss, stats);
     return SR_OK;

@@ -15,7 +15,7 @@ struct PolicyBatch {
     const uint8_t* mask;
     int rows;
     double clip_low, clip_high, beta;
-    float low, high;                 // 1 - clip_low, 1 + clip_high
+    float low, high, beta32;         // 1 - clip_low, 1 + clip_high, beta
 };
 // What the loss reads of one token beside its log-probability.
 struct PolicyToken {
@@ -52,57 +52,122 @@ __device__ __forceinline__ int warp_row_between(const int64_t* start, int lo, in
     return lo;
 }
 
-// The rollouts of the tokens that a warp passes through in ascending order, 128 at a time, four a lane.
+// The rollouts of the tokens that a warp passes through in ascending order, 128 at a time, four a lane: starts, weights and
+// advantages of 32 rollouts at once, a rollout a lane, so that most lots of 128 need no loads.
 struct RowWalk {
-    const int64_t* start;
-    int rows, r;                     // r: the rollout of the first token of the 128 at hand, or the one before the first
-    long long begin, end;            // tokens that lie in a rollout
+    const PolicyBatch* b;
+    uint32_t begin, end;             // tokens that lie in a rollout
+    int base;                        // the rollout before the lanes'
+    float weight, adv;               // its
+    uint32_t lane_start;             // of rollout base + 1 + lane; none: never reached
+    float lane_weight, lane_adv;
 
-    __device__ __forceinline__ void find(const int64_t* row_start, int n_rows, long long first) {
-        start = row_start;
-        rows = n_rows;
-        begin = start[0];
-        end = start[rows];
-        r = warp_row_between(start, 0, rows, first);
+    // Tokens are fewer than 2^31: where a start lies before or behind them all is enough.
+    static __device__ __forceinline__ uint32_t place(long long start) { return (uint32_t)min(max(start, 0LL), 0xFFFFFFFFLL); }
+    __device__ __forceinline__ void fill(int row) {
+        const int at = row + 1 + (threadIdx.x & 31);
+        const bool is = at < b->rows;
+        base = row;
+        lane_start = is ? place(b->row_start[at]) : 0xFFFFFFFFu;
+        lane_weight = is ? b->weight[at] : 0.0f;
+        lane_adv = lane_weight != 0.0f ? b->adv[at] : 0.0f;      // what a rollout without weight has is not used
+        weight = b->weight[row];
+        adv = weight != 0.0f ? b->adv[row] : 0.0f;
     }
-    // Row of token t0 (this lane's) of the 128 that begin at w0, and the token behind its last; moves on.  Lanes look at the
-    // next 32 starts together; where the 128 tokens have more rollouts they search for themselves.
-    __device__ __forceinline__ int row_of(long long w0, long long t0, long long& until) {
-        const int lane = threadIdx.x & 31;
-        const int at = r + 1 + lane;
-        const long long next = at < rows ? start[at] : INT64_MAX;       // start of rollout r + 1 + lane
-        const unsigned within = __ballot_sync(0xFFFFFFFFu, next <= w0 + 127);
-        int row = r;
-        if (within == 0u) {                                      // all in one rollout
-            until = INT64_MAX;
-        } else if (within != 0xFFFFFFFFu) {
-            // as many of the (ascending) starts as are not behind t0
-            int before = 0;
+    __device__ __forceinline__ void find(const PolicyBatch& batch, uint32_t first) {
+        b = &batch;
+        begin = place(b->row_start[0]);
+        end = place(b->row_start[b->rows]);
+        fill(warp_row_between(b->row_start, 0, b->rows, first));
+    }
+    // Whether the 128 tokens from w0 on lie in one rollout (or before the first, or behind the last); then w and a are its weight
+    // and advantage.
+    __device__ __forceinline__ bool one_rollout(uint32_t w0, float& w, float& a) {
+        unsigned in = __ballot_sync(0xFFFFFFFFu, lane_start <= w0 + 127);
+        if (in == 0xFFFFFFFFu) {                                 // more starts than the lanes hold: move on to the rollout of w0
+            const int passed = __popc(__ballot_sync(0xFFFFFFFFu, lane_start <= w0));
+            fill(passed < 32 ? base + passed : warp_row_between(b->row_start, base + 32, b->rows, w0));
+            in = __ballot_sync(0xFFFFFFFFu, lane_start <= w0 + 127);
+        }
+        const unsigned passed = __ballot_sync(0xFFFFFFFFu, lane_start <= w0);
+        const int last = 31 - __clz(passed);                     // starts ascend; -1: none is passed
+        w = __shfl_sync(0xFFFFFFFFu, lane_weight, last & 31);
+        a = __shfl_sync(0xFFFFFFFFu, lane_adv, last & 31);
+        if (last < 0) {
+            w = weight;
+            a = adv;
+        }
+        return passed == in;
+    }
+    // Weight and advantage of this lane's tokens t0 .. t0 + 3 where the 128 from w0 on lie in several.
+    __device__ __forceinline__ void several_rollouts(uint32_t w0, uint32_t t0, float (&w)[4], float (&a)[4]) {
+        if (__any_sync(0xFFFFFFFFu, lane_start > w0 + 127)) {
+            int before = 0;                                      // starts that are not behind t0: they ascend
 #pragma unroll
             for (int step = 16; step > 0; step >>= 1) {
-                const long long probe = __shfl_sync(0xFFFFFFFFu, next, before + step - 1);
+                const uint32_t probe = __shfl_sync(0xFFFFFFFFu, lane_start, before + step - 1);
                 if (probe <= t0) before += step;
             }
-            row = r + before;
-            until = __shfl_sync(0xFFFFFFFFu, next, before & 31);
-            r += __popc(__ballot_sync(0xFFFFFFFFu, next <= w0 + 128));
-        } else {
-            const int last = warp_row_between(start, r, rows, w0 + 128);
-            row = row_between(start, r, last + 1, t0);
-            until = row + 1 < rows ? start[row + 1] : INT64_MAX;
-            r = last;
+            uint32_t until = __shfl_sync(0xFFFFFFFFu, lane_start, before);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                while (__any_sync(0xFFFFFFFFu, until <= t0 + j)) {       // lane 31's start is behind the lot: `before` stays below 32
+                    before += until <= t0 + j;
+                    until = __shfl_sync(0xFFFFFFFFu, lane_start, before);
+                }
+                const float ws = __shfl_sync(0xFFFFFFFFu, lane_weight, (before - 1) & 31), as = __shfl_sync(0xFFFFFFFFu, lane_adv, (before - 1) & 31);
+                w[j] = before ? ws : weight;
+                a[j] = before ? as : adv;
+            }
+        } else {                                                 // 33 rollouts and more in 128 tokens
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int row = row_between(b->row_start, base, b->rows, t0 + j);
+                w[j] = b->weight[row];
+                a[j] = w[j] != 0.0f ? b->adv[row] : 0.0f;
+            }
         }
-        return row;
     }
 };
+
+static __device__ __noinline__ float far_expm1(float d) { return expm1f(d); }       // rare: kept out of the loops
+
+// e^d - 1 and e^d - 1 - d.  With d = n ln 2 + r and |r| <= ln(2) / 2, e^r - 1 = r + q with q = r^2 times the Taylor series of
+// (e^r - 1 - r) / r^2, cut where the next term is below 2^-27 of the sum; then
+//     e^d - 1 - d = 2^n q + (2^n r + (2^n - 1) - d),
+// whose second part is exactly 0 for n = 0: policies that nearly agree lose nothing.
+// For |d| <= 80.
+__device__ __forceinline__ void exp_less_line_near(float d, float& em1, float& kl) {
+    const float n = rintf(d * 1.44269504f);
+    float r = fmaf(n, -0.693359375f, d);           // ln 2 in two parts, the first with few bits: this product is exact
+    r = fmaf(n, 2.12194440054690583e-4f, r);
+    float g = 1.0f / 40320.0f;
+    g = fmaf(g, r, 1.0f / 5040.0f);
+    g = fmaf(g, r, 1.0f / 720.0f);
+    g = fmaf(g, r, 1.0f / 120.0f);
+    g = fmaf(g, r, 1.0f / 24.0f);
+    g = fmaf(g, r, 1.0f / 6.0f);
+    g = fmaf(g, r, 0.5f);
+    const float q = g * r * r;
+    const float s = __int_as_float(((int)n + 127) << 23);       // 2^n
+    kl = fmaf(s, q, (fmaf(s, r, s - 1.0f)) - d);
+    em1 = fmaf(s, r + q, s - 1.0f);
+}
+__device__ __forceinline__ void exp_less_line(float d, float& em1, float& kl) {
+    if (fabsf(d) > 80.0f) {                        // 2^n r may overflow before the sum does
+        em1 = far_expm1(d);
+        kl = em1 - d;
+    } else {
+        exp_less_line_near(d, em1, kl);
+    }
+}
 
 // Terms of a token that counts, and the gradient of its log-probability.  `lp` is fp32 where it came from memory, fp64
 // where it has just been computed.
 //
-// Two differences decide what is lost in 32 bits.  Whether rho is past a border of the clip range: rho in fp32 is off by up
-// to 2^-22 of itself, so within 2^-20 of a border the comparison is made again in fp64 (a token on the wrong side has a
-// wholly wrong gradient).  And e^d - 1 - d of policies that nearly agree: below 1/2 it is d^2 times the Taylor series of
-// (e^d - 1 - d) / d^2, cut where the next term is below 2^-29 of the sum.
+// Whether rho is past a border of the clip range would be lost in 32 bits (and a token on the wrong side has a wholly wrong
+// gradient): rho in fp32 is off by up to 2^-22 of itself, so within 2^-20 of a border the comparison is made again in fp64.
+static __device__ __noinline__ double exact_ratio(double lp, double old_logp) { return exp(lp - old_logp); }      // rare as well
 template <typename F>
 __device__ __forceinline__ float policy_token(const PolicyBatch& b, const PolicyToken& k, F lp, PolicyTerms<float>& out) {
     const float A = k.adv, w = k.weight;
@@ -114,32 +179,17 @@ __device__ __forceinline__ float policy_token(const PolicyBatch& b, const Policy
         rho = expf((float)delta);
         clipped = A > 0.0f ? rho > border : A < 0.0f && rho < border;
         if (fabsf(rho - border) <= 9.5367431640625e-7f * border) {
-            const double exact = exp((double)lp - (double)k.old_logp);
+            const double exact = exact_ratio((double)lp, (double)k.old_logp);
             clipped = A > 0.0f ? exact > 1.0 + b.clip_high : A < 0.0f && exact < 1.0 - b.clip_low;
         }
     }
     const float gain = A == 0.0f ? 0.0f : A * (clipped ? border : rho);
-    float d_lp = clipped || A == 0.0f ? 0.0f : -A * rho;
+    float d_lp = clipped || A == 0.0f ? 0.0f : -gain;
     float kl = 0.0f;
     if (b.ref_logp) {
-        const float d = (float)((F)k.ref_logp - lp);
         float em1;
-        if (fabsf(d) < 0.5f) {
-            float s = 1.0f / 362880.0f;
-            s = fmaf(s, d, 1.0f / 40320.0f);
-            s = fmaf(s, d, 1.0f / 5040.0f);
-            s = fmaf(s, d, 1.0f / 720.0f);
-            s = fmaf(s, d, 1.0f / 120.0f);
-            s = fmaf(s, d, 1.0f / 24.0f);
-            s = fmaf(s, d, 1.0f / 6.0f);
-            s = fmaf(s, d, 0.5f);
-            kl = s * d * d;
-            em1 = d + kl;
-        } else {
-            em1 = expm1f(d);
-            kl = em1 - d;
-        }
-        if (b.beta != 0.0) d_lp = fmaf(-(float)b.beta, em1, d_lp);
+        exp_less_line((float)((F)k.ref_logp - lp), em1, kl);
+        if (b.beta != 0.0) d_lp = fmaf(-b.beta32, em1, d_lp);
     }
     out.gain = w * gain;
     out.kl = w * kl;

@@ -118,7 +118,7 @@ int sr_policy_loss(const float* logp, const float* logp_old, const float* logp_r
     if (rc != SR_OK) return rc;
     if (n_tokens > 0 && logp == nullptr) return SR_ERR_NULL;
     if (short_of(workspace, workspace_bytes, kPartialBytes)) return SR_ERR_WORKSPACE;
-    const PolicyBatch b{logp_old, logp_ref, adv, weight, row_start, mask, n_rollouts, clip_low, clip_high, beta, (float)(1.0 - clip_low), (float)(1.0 + clip_high)};
+    const PolicyBatch b{logp_old, logp_ref, adv, weight, row_start, mask, n_rollouts, clip_low, clip_high, beta, (float)(1.0 - clip_low), (float)(1.0 + clip_high), (float)beta};
     return launch_policy_loss(b, logp, n_tokens, loss, d_logp, stats, static_cast<double*>(workspace), static_cast<cudaStream_t>(stream));
 }
 
@@ -138,7 +138,7 @@ int sr_policy_loss_logits(const void* logits, int32_t dtype, int32_t n_tokens, i
     rc = check_gradient(logits, dtype, n_tokens, vocab, pitch, d_logits, d_pitch);
     if (rc != SR_OK) return rc;
     if (short_of(workspace, workspace_bytes, sr_policy_loss_logits_workspace_bytes(n_tokens))) return SR_ERR_WORKSPACE;
-    const PolicyBatch b{logp_old, logp_ref, adv, weight, row_start, mask, n_rollouts, clip_low, clip_high, beta, (float)(1.0 - clip_low), (float)(1.0 + clip_high)};
+    const PolicyBatch b{logp_old, logp_ref, adv, weight, row_start, mask, n_rollouts, clip_low, clip_high, beta, (float)(1.0 - clip_low), (float)(1.0 + clip_high), (float)beta};
     StepScratch ws;
     ws.partial = static_cast<double*>(workspace);
     ws.terms = reinterpret_cast<PolicyTerms<float>*>(static_cast<char*>(workspace) + kPartialBytes);

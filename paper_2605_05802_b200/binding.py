@@ -28,7 +28,7 @@ SR_ERR_BAD_SIZE, SR_ERR_BAD_DTYPE, SR_ERR_BAD_VALUE, SR_ERR_OVERLAP = -11, -12, 
 SR_NORM_MAXLEN, SR_NORM_NONE = 0, 1
 SR_NO_ACTION = -(2 ** 31)
 SR_STATUS_NEG_LEN, SR_STATUS_STEP_OVERFLOW, SR_STATUS_BAD_STATE = 1, 2, 4
-SR_STATUS_BAD_TARGET, SR_STATUS_NONFINITE = 8, 16
+SR_STATUS_BAD_TARGET, SR_STATUS_NONFINITE, SR_STATUS_TIMEOUT = 8, 16, 32
 SR_DTYPE_F32, SR_DTYPE_BF16, SR_DTYPE_F16 = 0, 1, 2
 SR_LOSS_SUM, SR_LOSS_TOKEN_MEAN, SR_LOSS_ROLLOUT_MEAN = 0, 1, 2
 SR_MAX_N, SR_MAX_K, SR_MAX_INCR_STEPS = 32, 1024, 32

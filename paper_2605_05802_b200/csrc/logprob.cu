@@ -16,6 +16,7 @@
 #include <math_constants.h>
 
 #include "policy.cuh"
+#include "ring.cuh"
 
 namespace sr {
 namespace {
@@ -531,6 +532,273 @@ held_policy_loss_kernel(PolicyBatch b, const T* logits, int vocab, long long pit
     held.write_gradient(out, parts, at, threads, g);
 }
 
+// ---- long rows, held in shared memory
+//
+// A row of 150000 tokens does not fit the registers or the shared memory of one SM, and read twice it comes from HBM twice (the
+// second pass found 3 % of it in L2).  So a cluster holds it, a slice a CTA, in a ring of chunks: one thread has them copied in
+// (bulk copies that count their bytes at a barrier), the others add them up as they come, meet the cluster's sums, and write the
+// gradient from the same chunks, each of which is then free for the next row.  CTAs stay and take row after row: the copies never
+// wait for the sums of a row, and two CTAs an SM take turns at computing and at waiting for each other's cluster.
+// Read once, written once: bound by HBM; two exponentials an element come next (3/4 of their rate at that speed).
+constexpr int kRingThreads = 512, kRingWarps = kRingThreads / 32;
+constexpr int kChunk = kRingThreads * 16;          // bytes: a vector a thread
+constexpr int kRingSlots = 13;                     // 104 KB: two CTAs an SM
+constexpr int kRingRow = 10;                       // chunks of a slice at most; the rest is ahead
+
+struct RingPart {
+    double s;
+    float m, unused;
+};
+
+template <typename T>
+__global__ void __launch_bounds__(kRingThreads + 32, 2)
+ring_policy_loss_kernel(const __grid_constant__ PolicyBatch b, const T* logits, int vocab, long long pitch, const int32_t* targets, const int32_t* row_of, const int32_t* list,
+                        const int32_t* n_live, int n_tokens, double temperature, float c, int ctas, float* logp, PolicyTerms<float>* terms, T* d_logits, long long d_pitch,
+                        int32_t* status) {
+    constexpr int E = Vec<T>::kElems;
+    extern __shared__ __align__(128) unsigned char s_ring[];
+    __shared__ uint64_t s_full[kRingSlots], s_empty[kRingSlots], s_met[2];
+    __shared__ RingPart s_part[2][kMaxCtas * kRingWarps];
+    __shared__ RowGradient s_gradient[2];
+    __shared__ int s_gave_up;
+    const int rank = blockIdx.x % ctas, cluster_at = blockIdx.x / ctas, clusters = gridDim.x / ctas;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    if (threadIdx.x == 0) {
+        for (int k = 0; k < kRingSlots; ++k) {
+            barrier_init(&s_full[k], 1);
+            barrier_init(&s_empty[k], kRingWarps);
+        }
+        barrier_init(&s_met[0], kRingWarps * ctas);
+        barrier_init(&s_met[1], kRingWarps * ctas);
+        s_gave_up = 0;
+        barriers_ready();
+    }
+    const auto cluster = cooperative_groups::this_cluster();
+    cluster.sync();                            // barriers of every CTA are there before anyone arrives at them
+    grid_begin();
+    const int live = *n_live;
+    // this CTA's vectors of a row
+    const auto slice = [&](const RowParts<T>& parts, int& begin, int& end) {
+        begin = (int)((long long)parts.vecs * rank / ctas);
+        end = (int)((long long)parts.vecs * (rank + 1) / ctas);
+    };
+
+    volatile int* const gave_up = &s_gave_up;
+    if (warp == kRingWarps) {                  // the thread that has chunks copied in
+        uint32_t n = 0;
+        for (int q = cluster_at; lane == 0 && q < live && !*gave_up; q += clusters) {
+            const T* row = logits + (size_t)list[q] * pitch;
+            const RowParts<T> parts(row, vocab);
+            int begin, end;
+            slice(parts, begin, end);
+            const uint4* body = reinterpret_cast<const uint4*>(row + parts.head);
+            for (int v = begin; v < end; v += kRingThreads, ++n) {
+                const uint32_t slot = n % kRingSlots, use = n / kRingSlots;
+                if (use > 0) barrier_wait(&s_empty[slot], (use - 1) & 1, gave_up);
+                if (*gave_up) break;
+                const uint32_t bytes = (uint32_t)min(kRingThreads, end - v) * 16u;
+                barrier_expect(&s_full[slot], bytes);
+                bulk_load(s_ring + slot * kChunk, body + v, bytes, &s_full[slot]);
+            }
+        }
+        // no copy is in flight when the CTA ends
+        int ignored = 0;
+        for (uint32_t k = n > kRingSlots ? n - kRingSlots : 0; k < n; ++k) barrier_wait(&s_full[k % kRingSlots], (k / kRingSlots) & 1, &ignored);
+        cluster.sync();
+        return;
+    }
+
+    uint32_t n = 0;                            // chunks before this row
+    int turn = 0;
+    for (int q = cluster_at; q < live; q += clusters, ++turn) {
+        const int t = list[q];
+        const T* row = logits + (size_t)t * pitch;
+        T* out = d_logits + (size_t)t * d_pitch;
+        const RowParts<T> parts(row, vocab);
+        int begin, end;
+        slice(parts, begin, end);
+        const int chunks = (end - begin + kRingThreads - 1) / kRingThreads;
+        const int32_t y = targets[t];
+        float x_y = 0.0f, A = 0.0f, w = 0.0f;
+        if (threadIdx.x == 0) {                // before anyone writes: d_logits may be the logits
+            const int rollout = row_of[t];
+            x_y = to_float(row[y]);
+            A = b.adv[rollout];
+            w = b.weight[rollout];
+        }
+        const int single = rank == 0 && (int)threadIdx.x < parts.head + parts.tail ? parts.single(threadIdx.x) : -1;
+        const float x1 = single >= 0 ? to_float(row[single]) : minus_inf();
+
+        RowSums r = {minus_inf(), 0.0, 0.0};
+        float s[4] = {0.0f, 0.0f, 0.0f, 0.0f}, u[4];
+        for (int k = 0; k < chunks; ++k) {
+            const uint32_t slot = (n + k) % kRingSlots;
+            barrier_wait(&s_full[slot], ((n + k) / kRingSlots) & 1, gave_up);
+            if (begin + k * kRingThreads + (int)threadIdx.x < end) {
+                const uint4 v = *reinterpret_cast<const uint4*>(s_ring + slot * kChunk + threadIdx.x * 16);
+                VecMax<T> top(minus_inf());
+                top.take(v);
+                if (top.value() > r.m) {
+                    const float f = exp2_approx((r.m - top.value()) * c);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) s[j] *= f;
+                    r.s *= (double)f;
+                    r.m = top.value();
+                }
+                float x[E];
+                unpack(v, x, T());
+                add_terms<E, false>(x, r.m == minus_inf() ? 0.0f : r.m, c, s, u);
+            }
+            if (k % 4 == 3) {
+                r.s += (double)((s[0] + s[1]) + (s[2] + s[3]));
+                s[0] = s[1] = s[2] = s[3] = 0.0f;
+            }
+        }
+        r.s += (double)((s[0] + s[1]) + (s[2] + s[3]));
+        if (single >= 0) take<false>(x1, c, r);
+
+        // every warp of the cluster leaves its sums with every CTA
+        float M = r.m;
+#pragma unroll
+        for (int off = 16; off > 0; off >>= 1) M = fmaxf(M, __shfl_xor_sync(0xFFFFFFFFu, M, off));
+        rescale<false>(r, M, c);
+#pragma unroll
+        for (int off = 16; off > 0; off >>= 1) r.s += __shfl_xor_sync(0xFFFFFFFFu, r.s, off);
+        const int side = turn & 1;
+        if (lane < ctas) {
+            *cluster.map_shared_rank(&s_part[side][rank * kRingWarps + warp], lane) = RingPart{r.s, M, 0.0f};
+            barrier_arrive_at(&s_met[side], lane);
+        }
+        barrier_wait(&s_met[side], (turn >> 1) & 1, gave_up);
+        RingPart part[kMaxCtas * kRingWarps / 32];
+#pragma unroll
+        for (int k = 0; k < kMaxCtas * kRingWarps / 32; ++k)
+            part[k] = lane + 32 * k < ctas * kRingWarps ? s_part[side][lane + 32 * k] : RingPart{0.0, minus_inf(), 0.0f};
+        M = minus_inf();
+#pragma unroll
+        for (int k = 0; k < kMaxCtas * kRingWarps / 32; ++k) M = fmaxf(M, part[k].m);
+#pragma unroll
+        for (int off = 16; off > 0; off >>= 1) M = fmaxf(M, __shfl_xor_sync(0xFFFFFFFFu, M, off));
+        double S = 0.0;
+#pragma unroll
+        for (int k = 0; k < kMaxCtas * kRingWarps / 32; ++k) {
+            RowSums one = {part[k].m, part[k].s, 0.0};
+            rescale<false>(one, M, c);
+            S += one.s;
+        }
+#pragma unroll
+        for (int off = 16; off > 0; off >>= 1) S += __shfl_xor_sync(0xFFFFFFFFu, S, off);
+        if (M == minus_inf()) S = CUDART_NAN;      // no token can occur: there is no distribution
+
+        if (threadIdx.x == 0) {
+            token_gradient(b, t, x_y, A, w, M, S, temperature, rank == 0 ? logp : nullptr, terms, &s_gradient[side]);
+            if (*gave_up && rank == 0) terms[t].gain = CUDART_NAN_F;
+        }
+        asm volatile("bar.sync 1, %0;" ::"n"(kRingThreads) : "memory");
+        RowGradient g = s_gradient[side];
+        g.M = M;
+        g.c = c;
+        g.target = y;
+        uint4* to = reinterpret_cast<uint4*>(out + parts.head);
+        const int target_vec = y < parts.head ? -1 : (y - parts.head) / E;
+        for (int k = 0; k < chunks; ++k) {
+            const uint32_t slot = (n + k) % kRingSlots;
+            const int i = begin + k * kRingThreads + (int)threadIdx.x;
+            uint4 v = make_uint4(0u, 0u, 0u, 0u);
+            if (i < end) v = *reinterpret_cast<const uint4*>(s_ring + slot * kChunk + threadIdx.x * 16);
+            __syncwarp();
+            if (lane == 0) barrier_arrive(&s_empty[slot]);
+            if (i < end) {
+                float x[E];
+                unpack(v, x, T());
+#pragma unroll
+                for (int j = 0; j < E; ++j) x[j] = gradient<false>(g, x[j]);
+                if (i == target_vec) {
+                    const int at_j = (y - parts.head) % E;
+#pragma unroll
+                    for (int j = 0; j < E; ++j)
+                        if (j == at_j) x[j] += g.at_target;
+                }
+                store_once(to + i, pack(x, T()));
+            }
+        }
+        if (single >= 0) {
+            float v = gradient<false>(g, x1);
+            if (single == y) v += g.at_target;
+            out[single] = from_float<T>(v);
+        }
+        n += chunks;
+    }
+    // the rows of tokens that do not count, from the end of the list
+    for (int q = n_tokens - 1 - cluster_at; q >= live; q -= clusters) {
+        const int t = list[q];
+        write_gradient<T, false, true>(nullptr, d_logits + (size_t)t * d_pitch, vocab, rank * kRingThreads + threadIdx.x, ctas * kRingThreads, RowGradient());
+        if (rank == 0 && threadIdx.x == 0) {
+            logp[t] = 0.0f;
+            terms[t] = PolicyTerms<float>{0.0f, 0.0f, 0.0f, 0.0f};
+        }
+    }
+    if (threadIdx.x == 0 && *gave_up && status) atomicOr(status, SR_STATUS_TIMEOUT);
+    cluster.sync();                            // nobody leaves while its memory may be written to
+}
+
+// The rollout of every token that counts, -1 for the others, as token_rows_kernel; and a list of the tokens, those that count
+// from its beginning, the others from its end.  One cluster.
+constexpr int kListThreads = 1024, kListTokens = 65536;
+__global__ void __launch_bounds__(kListThreads)
+token_list_kernel(const __grid_constant__ PolicyBatch b, const int32_t* targets, int vocab, int n, int32_t* row_of, int32_t* list, int32_t* n_live, int32_t* status) {
+    grid_begin();
+    __shared__ int s_warp[32], s_cta[8];
+    const auto cluster = cooperative_groups::this_cluster();
+    const int ctas = gridDim.x, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int first = (int)((long long)n * blockIdx.x / ctas), last = (int)((long long)n * (blockIdx.x + 1) / ctas);
+    int mine = 0;
+    for (int t0 = first + 32 * warp; t0 < last; t0 += kListThreads) {          // a warp's tokens are neighbours
+        const int t = t0 + lane;
+        int r = -1;
+        if (b.rows > 0) {
+            const int r_first = warp_row_between(b.row_start, 0, b.rows, t0), r_last = warp_row_between(b.row_start, r_first, b.rows, min(t0 + 31, last - 1));
+            if (t < last && counts_as_target(targets[t], vocab, status, true) && !(b.mask && b.mask[t] == 0) && t >= b.row_start[0] && t < b.row_start[b.rows]) {
+                r = row_between(b.row_start, r_first, r_last + 1, t);
+                if (b.weight[r] == 0.0f) r = -1;
+            }
+        } else if (t < last) {
+            counts_as_target(targets[t], vocab, status, true);
+        }
+        if (t < last) row_of[t] = r;
+        mine += __popc(__ballot_sync(0xFFFFFFFFu, r >= 0));
+    }
+    if (lane == 0) s_warp[warp] = mine;
+    __syncthreads();
+    if (warp == 0) {
+        const int total = __reduce_add_sync(0xFFFFFFFFu, s_warp[lane]);
+        if (lane < ctas) *cluster.map_shared_rank(&s_cta[blockIdx.x], lane) = total;
+    }
+    cluster.sync();
+    int before = 0, all = 0;                   // tokens that count in the CTAs before this, and in all
+    for (int k = 0; k < ctas; ++k) {
+        if (k < (int)blockIdx.x) before += s_cta[k];
+        all += s_cta[k];
+    }
+    if (blockIdx.x == 0 && threadIdx.x == 0) *n_live = all;
+    for (int base = first; base < last; base += kListThreads) {
+        const int t = base + (int)threadIdx.x;
+        const bool counts = t < last && row_of[t] >= 0;         // this thread's own write, or its warp's
+        const unsigned bits = __ballot_sync(0xFFFFFFFFu, counts);
+        __syncthreads();
+        if (lane == 0) s_warp[warp] = __popc(bits);
+        __syncthreads();
+        int in_warps = 0, total = 0;
+        for (int k = 0; k < 32; ++k) {
+            if (k < warp) in_warps += s_warp[k];
+            total += s_warp[k];
+        }
+        const int at = before + in_warps + __popc(bits & low_mask(lane));       // tokens that count before t
+        if (t < last) list[counts ? at : n - 1 - (t - at)] = t;
+        before += total;
+    }
+}
+
 // How a row is held: CTAs to a row and vectors a thread, or no way to.  One CTA, or, where the rows alone do not fill the GPU, a
 // cluster as long as each thread still has a vector.
 struct Held {
@@ -588,13 +856,40 @@ int launch_backward(const LogitsArgs& a, const float* row_stats, const float* en
                   d_logp, d_entropy, a.temperature, c, parts, static_cast<T*>(d_logits), (long long)d_pitch);
 }
 
+// CTAs to a row of the ring kernel, or 0: rows too long for it, too short to be worth it, or too few to keep its CTAs busy.
+int ring_ctas(int n_tokens, int vocab, int elem) {
+    const long long vecs = ((long long)vocab * elem + 15) / 16;
+    if (n_tokens > kListTokens || vecs <= kHeldThreads * kMostVecs) return 0;
+    int ctas = 1;
+    while (ctas < kMaxCtas && vecs > (long long)ctas * kRingThreads * kRingRow) ctas *= 2;
+    if (vecs > (long long)ctas * kRingThreads * kRingRow || (long long)n_tokens * ctas < 2 * 148) return 0;
+    return ctas;
+}
+template <typename T>
+int launch_ring(const LogitsArgs& a, const PolicyBatch& b, const StepScratch& ws, int ctas, float* logp, void* d_logits, int64_t d_pitch, int32_t* status, cudaStream_t s) {
+    const float c = (float)(1.0 / (kLn2 * a.temperature));
+    const auto kernel = ring_policy_loss_kernel<T>;
+    constexpr int kBytes = kRingSlots * kChunk;
+    SR_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kBytes));
+    const int list_ctas = min(8, (a.n_tokens + kListThreads - 1) / kListThreads * 2);
+    int rc = launch_as(true, list_ctas, "token_list_kernel", token_list_kernel, list_ctas, kListThreads, 0, s, b, a.targets, a.vocab, a.n_tokens, ws.row_of, ws.list, ws.n_live, status);
+    if (rc != SR_OK) return rc;
+    const int clusters = min(a.n_tokens, 2 * 148 / ctas);
+    return launch_as(true, ctas, "ring_policy_loss_kernel", kernel, clusters * ctas, kRingThreads + 32, kBytes, s, b, static_cast<const T*>(a.logits), a.vocab, (long long)a.pitch, a.targets,
+                     ws.row_of, ws.list, ws.n_live, a.n_tokens, a.temperature, c, ctas, logp, ws.terms, static_cast<T*>(d_logits), (long long)d_pitch, status);
+}
+
+// Whether rows that are held can be written as they were read: logits and gradient lie alike against 16 bytes in every row.
+bool alike(const LogitsArgs& a, const void* d_logits, int64_t d_pitch) {
+    const uintptr_t apart = reinterpret_cast<uintptr_t>(a.logits) ^ reinterpret_cast<uintptr_t>(d_logits);
+    return (apart & 15) == 0 && (a.n_tokens == 1 || ((a.pitch - d_pitch) * dtype_bytes(a.dtype)) % 16 == 0);
+}
+
 template <typename T>
 int launch_step(const LogitsArgs& a, const PolicyBatch& b, const int32_t* row_of, float* logp, PolicyTerms<float>* terms, void* d_logits, int64_t d_pitch, cudaStream_t s) {
     const float c = (float)(1.0 / (kLn2 * a.temperature));
-    // held rows are written as they were read: both lie alike against 16 bytes
     const Held held = held_row(a.n_tokens, a.vocab, (int)sizeof(T));
-    const uintptr_t apart = reinterpret_cast<uintptr_t>(a.logits) ^ reinterpret_cast<uintptr_t>(d_logits);
-    if (held.vecs && (apart & 15) == 0 && ((a.pitch - d_pitch) * (int64_t)sizeof(T)) % 16 == 0)
+    if (held.vecs && alike(a, d_logits, d_pitch))
         return with_vecs(held.vecs, [&](auto vecs) {
             return launch_as(true, held.ctas, "held_policy_loss_kernel", held_policy_loss_kernel<T, vecs()>, a.n_tokens * held.ctas, kHeldThreads, 0, s, b, static_cast<const T*>(a.logits),
                              a.vocab, (long long)a.pitch, a.targets, row_of, a.temperature, c, held.ctas, logp, terms, static_cast<T*>(d_logits), (long long)d_pitch);
@@ -628,12 +923,20 @@ int launch_token_logprob_backward(const LogitsArgs& a, const float* row_stats, c
 int launch_policy_loss_logits(const LogitsArgs& a, const PolicyBatch& b, float* loss, float* logp, void* d_logits, int64_t d_pitch, float* stats, int32_t* status,
                               const StepScratch& ws, cudaStream_t s) {
     if (a.n_tokens > 0) {
-        SR_LAUNCH("token_rows_kernel", token_rows_kernel, (int)(((long long)a.n_tokens + 255) / 256), 256, 0, s, b, a.targets, a.vocab, a.n_tokens, ws.row_of, status);
+        const int elem = dtype_bytes(a.dtype), ring = alike(a, d_logits, d_pitch) ? ring_ctas(a.n_tokens, a.vocab, elem) : 0;
+        if (!ring)
+            SR_LAUNCH("token_rows_kernel", token_rows_kernel, (int)(((long long)a.n_tokens + 255) / 256), 256, 0, s, b, a.targets, a.vocab, a.n_tokens, ws.row_of, status);
         int rc;
         switch (a.dtype) {
-            case SR_DTYPE_F32: rc = launch_step<float>(a, b, ws.row_of, logp, ws.terms, d_logits, d_pitch, s); break;
-            case SR_DTYPE_BF16: rc = launch_step<__nv_bfloat16>(a, b, ws.row_of, logp, ws.terms, d_logits, d_pitch, s); break;
-            default: rc = launch_step<__half>(a, b, ws.row_of, logp, ws.terms, d_logits, d_pitch, s); break;
+            case SR_DTYPE_F32:
+                rc = ring ? launch_ring<float>(a, b, ws, ring, logp, d_logits, d_pitch, status, s) : launch_step<float>(a, b, ws.row_of, logp, ws.terms, d_logits, d_pitch, s);
+                break;
+            case SR_DTYPE_BF16:
+                rc = ring ? launch_ring<__nv_bfloat16>(a, b, ws, ring, logp, d_logits, d_pitch, status, s) : launch_step<__nv_bfloat16>(a, b, ws.row_of, logp, ws.terms, d_logits, d_pitch, s);
+                break;
+            default:
+                rc = ring ? launch_ring<__half>(a, b, ws, ring, logp, d_logits, d_pitch, status, s) : launch_step<__half>(a, b, ws.row_of, logp, ws.terms, d_logits, d_pitch, s);
+                break;
         }
         if (rc != SR_OK) return rc;
     }

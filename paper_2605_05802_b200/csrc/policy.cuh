@@ -249,6 +249,8 @@ struct StepScratch {
     double* partial;                 // [kMaxPartials][4]
     PolicyTerms<float>* terms;       // [n_tokens]
     int32_t* row_of;                 // [n_tokens]
+    int32_t* list;                   // [n_tokens]
+    int32_t* n_live;
 };
 int launch_policy_loss_logits(const LogitsArgs& a, const PolicyBatch& b, float* loss, float* logp, void* d_logits, int64_t d_pitch, float* stats, int32_t* status,
                               const StepScratch& ws, cudaStream_t s);

@@ -1,0 +1,68 @@
+// Barriers in shared memory, bulk copies into it and writes to the other CTAs of a cluster, with waits that end.
+#pragma once
+
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+namespace sr {
+
+__device__ __forceinline__ uint32_t shared_address(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
+
+__device__ __forceinline__ void barrier_init(uint64_t* bar, uint32_t arrivals) {
+    asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(shared_address(bar)), "r"(arrivals) : "memory");
+}
+// Makes initialised barriers known to bulk copies and to the cluster; a cluster barrier follows.
+__device__ __forceinline__ void barriers_ready() { asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory"); }
+__device__ __forceinline__ void barrier_expect(uint64_t* bar, uint32_t bytes) {
+    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(shared_address(bar)), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void barrier_arrive(uint64_t* bar) {
+    asm volatile("mbarrier.arrive.release.cta.shared::cta.b64 _, [%0];" ::"r"(shared_address(bar)) : "memory");
+}
+// Arrives at the same barrier of CTA `rank` of the cluster; what this thread wrote to that CTA's memory is there before.
+__device__ __forceinline__ void barrier_arrive_at(uint64_t* bar, uint32_t rank) {
+    asm volatile(
+        "{\n\t.reg .b32 there;\n\t"
+        "mapa.shared::cluster.u32 there, %0, %1;\n\t"
+        "mbarrier.arrive.release.cluster.shared::cluster.b64 _, [there];\n\t}" ::"r"(shared_address(bar)), "r"(rank) : "memory");
+}
+__device__ __forceinline__ bool barrier_test(uint64_t* bar, uint32_t parity) {
+    uint32_t done;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}" : "=r"(done) : "r"(shared_address(bar)), "r"(parity) : "memory");
+    return done != 0;
+}
+__device__ __forceinline__ unsigned long long nanoseconds() {
+    unsigned long long t;
+    asm volatile("mov.u64 %0, %globaltimer;" : "=l"(t));
+    return t;
+}
+constexpr unsigned long long kWaitLimit = 1000000000ull;     // a second; a wait takes microseconds
+
+// Waits for the phase with that parity.  After the limit, or where another thread of the CTA has given up, *gave_up is set and the
+// wait ends all the same: whoever reads it says so in the results.
+__device__ __noinline__ void barrier_wait_long(uint64_t* bar, uint32_t parity, volatile int* gave_up) {
+    const unsigned long long began = nanoseconds();
+    for (;;) {
+        for (int k = 0; k < 64; ++k)
+            if (barrier_test(bar, parity)) return;
+        if (*gave_up) return;
+        if (nanoseconds() - began > kWaitLimit) {
+            *gave_up = 1;
+            return;
+        }
+    }
+}
+__device__ __forceinline__ void barrier_wait(uint64_t* bar, uint32_t parity, volatile int* gave_up) {
+    if (!barrier_test(bar, parity)) barrier_wait_long(bar, parity, gave_up);
+}
+
+// Copies `bytes` (a multiple of 16, both addresses on 16 bytes) from global into this CTA's shared memory and counts them at `bar`.
+__device__ __forceinline__ void bulk_load(void* to, const void* from, uint32_t bytes, uint64_t* bar) {
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(shared_address(to)), "l"(from), "r"(bytes), "r"(shared_address(bar))
+                 : "memory");
+}
+
+}  // namespace sr

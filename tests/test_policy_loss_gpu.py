@@ -233,7 +233,8 @@ def logits(T, V, dtype, seed, pad=0):
     return x, y
 
 
-STEPS = [(1, 1), (4, 3), (7, 129), (60, 4096), (400, 4096), (3, 8200), (5, 50021), (2, 151936), (301, 1001), (3, 300000), (2, 999983), (700, 40)]
+STEPS = [(1, 1), (4, 3), (7, 129), (60, 4096), (400, 4096), (3, 8200), (5, 50021), (2, 151936), (301, 1001), (3, 300000), (2, 999983), (700, 40),
+         (1000, 21003), (160, 50021), (84, 151936)]
 
 
 @pytest.mark.parametrize("dtype", list(DTYPES))

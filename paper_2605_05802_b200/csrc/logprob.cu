@@ -40,17 +40,44 @@ struct RowSums {
     double s, u;
 };
 
-// Terms of N elements, none of them above m (or NaN, or +inf: these end up in s).
-template <int N, bool kEntropy>
-__device__ __forceinline__ void add_terms(const float (&x)[N], float m, float c, float (&s)[4], float (&u)[4]) {
+// fp32 sums of the terms of a few elements, four of each side by side.
+template <bool kEntropy>
+struct TermSums {
+    f32x2 s[2] = {0ull, 0ull}, u[2] = {0ull, 0ull};
+
+    // N (an even number of) elements, none of them above m (or NaN, or +inf: these end up in s).
+    template <int N>
+    __device__ __forceinline__ void add(const float (&x)[N], float m, float c) {
+        const f32x2 minus_m = two(-m), cc = two(c);
 #pragma unroll
-    for (int k = 0; k < N; ++k) {
-        const float t = (x[k] - m) * c;
-        const float e = exp2_approx(t);
-        s[k & 3] += e;
-        if (kEntropy) u[k & 3] = fmaf(e, fmaxf(t, -1000.0f), u[k & 3]);      // 0 * -inf is 0 here; a NaN is in s already
+        for (int k = 0; k < N; k += 2) {
+            const f32x2 t = mul2(add2(two(x[k], x[k + 1]), minus_m), cc);
+            const float t0 = low_of(t), t1 = high_of(t);
+            const f32x2 e = two(exp2_approx(t0), exp2_approx(t1));
+            s[(k >> 1) & 1] = add2(s[(k >> 1) & 1], e);
+            // 0 * -inf is to be 0 here; a NaN is in s already
+            if (kEntropy) u[(k >> 1) & 1] = fma2(e, two(fmaxf(t0, -1000.0f), fmaxf(t1, -1000.0f)), u[(k >> 1) & 1]);
+        }
     }
-}
+    __device__ __forceinline__ void scale(float f) {
+        s[0] = mul2(s[0], two(f));
+        s[1] = mul2(s[1], two(f));
+    }
+    static __device__ __forceinline__ double total(const f32x2 (&v)[2]) {
+        const f32x2 both = add2(v[0], v[1]);
+        return (double)(low_of(both) + high_of(both));
+    }
+    // Moves the sums into r.
+    __device__ __forceinline__ void flush(RowSums& r) {
+        r.s += total(s);
+        s[0] = s[1] = 0ull;
+        if (kEntropy) {
+            r.u += total(u);
+            u[0] = u[1] = 0ull;
+        }
+    }
+};
+
 // Makes `top` the maximum where it is larger.
 template <bool kEntropy>
 __device__ __forceinline__ void grow(float top, float c, RowSums& r) {
@@ -66,11 +93,9 @@ __device__ __forceinline__ void grow(float top, float c, RowSums& r) {
 template <bool kEntropy>
 __device__ __forceinline__ void take(float x, float c, RowSums& r) {
     grow<kEntropy>(x, c, r);
-    const float one[1] = {x};
-    float s[4] = {0.0f, 0.0f, 0.0f, 0.0f}, u[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-    add_terms<1, kEntropy>(one, r.m == minus_inf() ? 0.0f : r.m, c, s, u);
-    r.s += (double)s[0];
-    if (kEntropy) r.u += (double)u[0];
+    const float t = (x - (r.m == minus_inf() ? 0.0f : r.m)) * c, e = exp2_approx(t);
+    r.s += (double)e;
+    if (kEntropy) r.u += (double)(e * fmaxf(t, -1000.0f));
 }
 
 // r, seen from the maximum M of several parts.
@@ -191,15 +216,14 @@ __device__ __forceinline__ RowSums sum_row(const T* row, int vocab, int at, int 
         for (int k = 0; k < kUnroll; ++k) top.take(q[k]);
         grow<kEntropy>(top.value(), c, r);
         const float m = r.m == minus_inf() ? 0.0f : r.m;
-        float s[4] = {0.0f, 0.0f, 0.0f, 0.0f}, u[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+        TermSums<kEntropy> sums;
 #pragma unroll
         for (int k = 0; k < kUnroll; ++k) {
             float x[E];
             unpack_again(q[k], x, T());
-            add_terms<E, kEntropy>(x, m, c, s, u);
+            sums.add(x, m, c);
         }
-        r.s += (double)((s[0] + s[1]) + (s[2] + s[3]));
-        if (kEntropy) r.u += (double)((u[0] + u[1]) + (u[2] + u[3]));
+        sums.flush(r);
     }
     return r;
 }
@@ -214,6 +238,20 @@ __device__ __forceinline__ float gradient(const RowGradient& g, float x) {
     const float t = (x - g.M) * g.c;
     const float e = exp2_approx(t);
     return kEntropy ? e * fmaf(g.k1, fmaxf(t, -1000.0f), g.k0) : e * g.k0;
+}
+// Of a vector's elements, in place.
+template <bool kEntropy, int E>
+__device__ __forceinline__ void gradients(const RowGradient& g, float (&x)[E]) {
+    const f32x2 minus_m = two(-g.M), cc = two(g.c), k0 = two(g.k0), k1 = two(g.k1);
+#pragma unroll
+    for (int k = 0; k < E; k += 2) {
+        const f32x2 t = mul2(add2(two(x[k], x[k + 1]), minus_m), cc);
+        const float t0 = low_of(t), t1 = high_of(t);
+        const f32x2 e = two(exp2_approx(t0), exp2_approx(t1));
+        const f32x2 d = kEntropy ? mul2(e, fma2(k1, two(fmaxf(t0, -1000.0f), fmaxf(t1, -1000.0f)), k0)) : mul2(e, k0);
+        x[k] = low_of(d);
+        x[k + 1] = high_of(d);
+    }
 }
 // A row spread over the registers of a cluster: kVecs vectors a thread, and a single element where the row has some.  It is read
 // once, whatever is made of it, and all of a thread's loads are on their way together.
@@ -244,18 +282,13 @@ struct HeldRow {
         if (!(r.m > minus_inf())) r.m = minus_inf();           // a NaN alone is no maximum
         take<kEntropy>(x1, c, r);
         const float m = r.m == minus_inf() ? 0.0f : r.m;
-        float s[4] = {0.0f, 0.0f, 0.0f, 0.0f}, u[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+        TermSums<kEntropy> sums;
 #pragma unroll
         for (int k = 0; k < kVecs; ++k) {
             float x[E];
             unpack_again(q[k], x, T());
-            add_terms<E, kEntropy>(x, m, c, s, u);
-            if (k % 4 == 3 || k == kVecs - 1) {
-                r.s += (double)((s[0] + s[1]) + (s[2] + s[3]));
-                if (kEntropy) r.u += (double)((u[0] + u[1]) + (u[2] + u[3]));
-#pragma unroll
-                for (int j = 0; j < 4; ++j) s[j] = u[j] = 0.0f;
-            }
+            sums.add(x, m, c);
+            if (k % 4 == 3 || k == kVecs - 1) sums.flush(r);
         }
         return r;
     }
@@ -268,8 +301,7 @@ struct HeldRow {
             if (i >= parts.vecs) break;
             float x[E];
             unpack_again(q[k], x, T());
-#pragma unroll
-            for (int j = 0; j < E; ++j) x[j] = gradient<false>(g, x[j]);
+            gradients<false>(g, x);
             if (i == target_vec) {
                 const int at_j = (g.target - parts.head) % E;
 #pragma unroll
@@ -319,8 +351,7 @@ __device__ __forceinline__ void write_gradient(const T* row, T* out, int vocab, 
             if (!kZero) {
                 float x[E];
                 unpack(q[k], x, T());
-#pragma unroll
-                for (int j = 0; j < E; ++j) x[j] = gradient<kEntropy>(g, x[j]);
+                gradients<kEntropy>(g, x);
                 if (i == target_vec) {
                     const int at_j = (g.target - parts.head) % E;
 #pragma unroll
@@ -447,11 +478,11 @@ token_rows_kernel(PolicyBatch b, const int32_t* targets, int vocab, int n, int32
 
 // By one thread: the token's terms of the loss and the gradient of its row.  A function of its own, so that the registers of a
 // held row are put aside for it in that thread alone.
-__device__ __noinline__ void token_gradient(const PolicyBatch& b, int t, float x_y, float A, float w, float m, double S, double temperature, float* logp,
-                                            PolicyTerms<float>* terms, RowGradient* g) {
+__device__ __noinline__ void token_gradient(const PolicyBatch& b, const PolicyToken& k, int t, float x_y, float m, double S, double temperature, float* logp, PolicyTerms<float>* terms,
+                                            RowGradient* g) {
     const double lp = ((double)x_y - (double)m) / temperature - log(S);
     PolicyTerms<float> term;
-    const float d = policy_token(b, PolicyToken{b.old_logp ? b.old_logp[t] : 0.0f, b.ref_logp ? b.ref_logp[t] : 0.0f, A, w}, lp, term);
+    const float d = policy_token(b, k, lp, term);
     if (logp) {
         logp[t] = (float)lp;
         terms[t] = term;
@@ -459,11 +490,14 @@ __device__ __noinline__ void token_gradient(const PolicyBatch& b, int t, float x
     g->k0 = (float)(-(double)d / (S * temperature));
     g->at_target = (float)((double)d / temperature);
 }
+__device__ __forceinline__ PolicyToken load_token(const PolicyBatch& b, int t, int rollout) {
+    return PolicyToken{b.old_logp ? b.old_logp[t] : 0.0f, b.ref_logp ? b.ref_logp[t] : 0.0f, b.adv[rollout], b.weight[rollout]};
+}
 // The gradient of a row, in every thread of the CTA; `first` writes down the token's figures.
-__device__ __forceinline__ RowGradient loss_gradient(const PolicyBatch& b, int t, float x_y, int y, float A, float w, const RowSums& r, double temperature, float c,
-                                                     bool first, float* logp, PolicyTerms<float>* terms) {
+__device__ __forceinline__ RowGradient loss_gradient(const PolicyBatch& b, const PolicyToken& k, int t, float x_y, int y, const RowSums& r, double temperature, float c, bool first,
+                                                     float* logp, PolicyTerms<float>* terms) {
     __shared__ RowGradient s_g;
-    if (threadIdx.x == 0) token_gradient(b, t, x_y, A, w, r.m, r.s, temperature, first ? logp : nullptr, terms, &s_g);
+    if (threadIdx.x == 0) token_gradient(b, k, t, x_y, r.m, r.s, temperature, first ? logp : nullptr, terms, &s_g);
     __syncthreads();
     RowGradient g = s_g;
     g.M = r.m;
@@ -494,11 +528,11 @@ policy_loss_logits_kernel(PolicyBatch b, const T* logits, int vocab, long long p
     }
     const T* row = logits + (size_t)t * pitch;
     const int32_t y = targets[t];
-    const float A = b.adv[rollout], w = b.weight[rollout];
     const float x_y = to_float(row[y]);                        // before anyone writes: d_logits may be the logits
+    const PolicyToken token = threadIdx.x == 0 ? load_token(b, t, rollout) : PolicyToken{};      // on its way meanwhile
     RowSums r = sum_row<T, false, true>(row, vocab, at, threads, c);
     r = combine<false>(r, c, ctas);
-    g = loss_gradient(b, t, x_y, y, A, w, r, temperature, c, first, logp, terms);
+    g = loss_gradient(b, token, t, x_y, y, r, temperature, c, first, logp, terms);
     write_gradient<T, false, false>(row, out, vocab, at, threads, g);
 }
 
@@ -525,10 +559,10 @@ held_policy_loss_kernel(PolicyBatch b, const T* logits, int vocab, long long pit
     HeldRow<T, kVecs> held;
     held.load(row, parts, at, threads);
     const int32_t y = targets[t];
-    const float A = b.adv[rollout], w = b.weight[rollout];
     const float x_y = to_float(row[y]);                        // before anyone writes: d_logits may be the logits
+    const PolicyToken token = threadIdx.x == 0 ? load_token(b, t, rollout) : PolicyToken{};      // on its way meanwhile
     const RowSums r = combine<false>(held.template sums<false>(c), c, ctas);
-    const RowGradient g = loss_gradient(b, t, x_y, y, A, w, r, temperature, c, first, logp, terms);
+    const RowGradient g = loss_gradient(b, token, t, x_y, y, r, temperature, c, first, logp, terms);
     held.write_gradient(out, parts, at, threads, g);
 }
 
@@ -536,237 +570,335 @@ held_policy_loss_kernel(PolicyBatch b, const T* logits, int vocab, long long pit
 //
 // A row of 150000 tokens does not fit the registers or the shared memory of one SM, and read twice it comes from HBM twice (the
 // second pass found 3 % of it in L2).  So a cluster holds it, a slice a CTA, in a ring of chunks: one thread has them copied in
-// (bulk copies that count their bytes at a barrier), the others add them up as they come, meet the cluster's sums, and write the
+// (bulk copies that count their bytes at a barrier); eight warps add them up as they come and send their sums to every CTA of
+// the cluster; one warp turns these into the row's gradient and finds out about the row to come; and the eight write the
 // gradient from the same chunks, each of which is then free for the next row.  CTAs stay and take row after row: the copies never
-// wait for the sums of a row, and two CTAs an SM take turns at computing and at waiting for each other's cluster.
+// wait for the sums of a row, and two CTAs an SM take turns at computing and at waiting.
 // Read once, written once: bound by HBM; two exponentials an element come next (3/4 of their rate at that speed).
-constexpr int kRingThreads = 512, kRingWarps = kRingThreads / 32;
-constexpr int kChunk = kRingThreads * 16;          // bytes: a vector a thread
+constexpr int kRingThreads = 256, kRingWarps = kRingThreads / 32;
+constexpr int kChunkVecs = 2 * kRingThreads;       // two vectors a thread: with one, more instructions went into finding them than into the terms
+constexpr int kChunk = kChunkVecs * 16;            // bytes
 constexpr int kRingSlots = 13;                     // 104 KB: two CTAs an SM
 constexpr int kRingRow = 10;                       // chunks of a slice at most; the rest is ahead
 
+// A slot, and the parity of the phase that its use is.
+struct RingPlace {
+    uint32_t slot = 0, phase = 0;
+    __device__ __forceinline__ void step() {
+        if (++slot == kRingSlots) {
+            slot = 0;
+            phase ^= 1u;
+        }
+    }
+};
 struct RingPart {
     double s;
     float m, unused;
 };
+// A row to come.  Its target's logit stands here too: written, it has been read.
+struct RingRow {
+    int t, y;                        // t < 0: there is none
+    float x_y;
+};
+constexpr int kRingQueue = 8;        // rows that a CTA may know of
+// Counters: tokens that count; the next row of them to be taken; the next of the others.
+enum { kLive, kNextLive, kNextOther };
 
 template <typename T>
-__global__ void __launch_bounds__(kRingThreads + 32, 2)
-ring_policy_loss_kernel(const __grid_constant__ PolicyBatch b, const T* logits, int vocab, long long pitch, const int32_t* targets, const int32_t* row_of, const int32_t* list,
-                        const int32_t* n_live, int n_tokens, double temperature, float c, int ctas, float* logp, PolicyTerms<float>* terms, T* d_logits, long long d_pitch,
-                        int32_t* status) {
+__global__ void __launch_bounds__(kRingThreads + 64, 2)
+ring_policy_loss_kernel(const __grid_constant__ PolicyBatch b, const T* logits, int vocab, long long pitch, const int4* list, int32_t* counters, int n_tokens, double temperature,
+                        float c, int ctas, float* logp, PolicyTerms<float>* terms, T* d_logits, long long d_pitch, int32_t* status) {
     constexpr int E = Vec<T>::kElems;
     extern __shared__ __align__(128) unsigned char s_ring[];
-    __shared__ uint64_t s_full[kRingSlots], s_empty[kRingSlots], s_met[2];
-    __shared__ RingPart s_part[2][kMaxCtas * kRingWarps];
+    __shared__ uint64_t s_full[kRingSlots], s_empty[kRingSlots];                  // chunks that are there, and that are done with
+    __shared__ uint64_t s_got[kRingQueue], s_known[2], s_met[2], s_ready[2];      // by row: its number, what it is, the cluster's sums, the gradient
+    __shared__ __align__(16) RingPart s_part[2][kMaxCtas * kRingWarps];
+    __shared__ __align__(16) int4 s_number[kRingQueue];
+    __shared__ RingRow s_row[2];
     __shared__ RowGradient s_gradient[2];
-    __shared__ int s_gave_up;
-    const int rank = blockIdx.x % ctas, cluster_at = blockIdx.x / ctas, clusters = gridDim.x / ctas;
+    __shared__ int s_gave_up, s_other;
+    const int rank = blockIdx.x % ctas;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     if (threadIdx.x == 0) {
         for (int k = 0; k < kRingSlots; ++k) {
             barrier_init(&s_full[k], 1);
             barrier_init(&s_empty[k], kRingWarps);
         }
-        barrier_init(&s_met[0], kRingWarps * ctas);
-        barrier_init(&s_met[1], kRingWarps * ctas);
+        for (int k = 0; k < kRingQueue; ++k) barrier_init(&s_got[k], 1);
+        for (int k = 0; k < 2; ++k) {
+            barrier_init(&s_known[k], 1);
+            barrier_init(&s_met[k], 1);
+            barrier_init(&s_ready[k], 1);
+        }
         s_gave_up = 0;
         barriers_ready();
     }
     const auto cluster = cooperative_groups::this_cluster();
-    cluster.sync();                            // barriers of every CTA are there before anyone arrives at them
+    cluster.sync();                            // barriers of every CTA are there before anyone writes to it
     grid_begin();
-    const int live = *n_live;
+    volatile int* const gave_up = &s_gave_up;
+    const int live = counters[kLive];
     // this CTA's vectors of a row
     const auto slice = [&](const RowParts<T>& parts, int& begin, int& end) {
         begin = (int)((long long)parts.vecs * rank / ctas);
         end = (int)((long long)parts.vecs * (rank + 1) / ctas);
     };
+    // The list's entry of the cluster's turn-th row; none: x < 0.
+    const auto entry = [&](int turn) {
+        const int at = turn & (kRingQueue - 1);
+        barrier_wait(&s_got[at], (turn / kRingQueue) & 1, gave_up);
+        const int number = *reinterpret_cast<volatile int*>(&s_number[at].x);
+        return number < live && !*gave_up ? list[number] : make_int4(-1, 0, 0, 0);
+    };
 
-    volatile int* const gave_up = &s_gave_up;
-    if (warp == kRingWarps) {                  // the thread that has chunks copied in
+    // Rows are dealt out as clusters ask for them: some may have started late.  The first CTA's copying thread asks, and tells
+    // the others.  It is at most five rows ahead of its own consumers (a slice has three chunks at least), and those are never two
+    // ahead of anyone's: a place in the queue has been read by all long before it is used again.
+    if (warp == kRingWarps) {                  // has chunks copied in, by one thread
+        RingPlace place;
         uint32_t n = 0;
-        for (int q = cluster_at; lane == 0 && q < live && !*gave_up; q += clusters) {
-            const T* row = logits + (size_t)list[q] * pitch;
+        const auto tell = [&](int turn, int number) {
+            const int at = turn & (kRingQueue - 1);
+            for (int k = 0; k < ctas; ++k) store_at(&s_number[at], (uint32_t)number, 0ull, &s_got[at], k);
+        };
+        if (lane == 0) {
+            if (rank == 0) tell(0, atomicAdd(&counters[kNextLive], 1));
+            for (int turn = 0;; ++turn) {
+                barrier_expect(&s_got[turn & (kRingQueue - 1)], 16);
+                const int4 row_of = entry(turn);
+                if (row_of.x < 0) break;
+                int number = 0;
+                if (rank == 0) number = atomicAdd(&counters[kNextLive], 1);
+                const T* row = logits + (size_t)row_of.x * pitch;
+                const RowParts<T> parts(row, vocab);
+                int begin, end;
+                slice(parts, begin, end);
+                const uint4* body = reinterpret_cast<const uint4*>(row + parts.head);
+                for (int v = begin; v < end; v += kChunkVecs, ++n) {
+                    if (n >= kRingSlots) barrier_wait(&s_empty[place.slot], place.phase ^ 1u, gave_up);
+                    if (*gave_up) break;
+                    const uint32_t bytes = (uint32_t)min(kChunkVecs, end - v) * 16u;
+                    barrier_expect(&s_full[place.slot], bytes);
+                    bulk_load(s_ring + place.slot * kChunk, body + v, bytes, &s_full[place.slot]);
+                    place.step();
+                }
+                if (rank == 0) tell(turn + 1, number);
+            }
+            // no copy is in flight when the CTA ends
+            int ignored = 0;
+            for (uint32_t k = n > kRingSlots ? n - kRingSlots : 0; k < n; ++k) barrier_wait(&s_full[k % kRingSlots], (k / kRingSlots) & 1, &ignored);
+        }
+    } else if (warp == kRingWarps + 1) {       // says which row comes next, and turns the cluster's sums into its gradient
+        PolicyToken token = {};
+        float x_y = 0.0f;
+        const auto announce = [&](int side, const int4& row) {   // its target's logit is read before anyone can write: d_logits may be the logits
+            if (row.x >= 0) {
+                x_y = to_float(logits[(size_t)row.x * pitch + row.y]);
+                token = load_token(b, row.x, row.z);
+            }
+            if (lane == 0) {
+                s_row[side] = RingRow{row.x, row.y, x_y};
+                barrier_arrive(&s_known[side]);
+            }
+        };
+        int4 row = entry(0);
+        announce(0, row);
+        for (int turn = 0; row.x >= 0; ++turn) {
+            const int side = turn & 1;
+            if (lane == 0) barrier_expect(&s_met[side], (uint32_t)(sizeof(RingPart) * kRingWarps) * (uint32_t)ctas);
+            const int4 next = entry(turn + 1); // on its way while this row is summed up
+            barrier_wait(&s_met[side], (turn >> 1) & 1, gave_up);
+            RingPart part[kMaxCtas * kRingWarps / 32];
+            float M = minus_inf();
+#pragma unroll
+            for (int k = 0; k < kMaxCtas * kRingWarps / 32; ++k) {
+                part[k] = lane + 32 * k < ctas * kRingWarps ? s_part[side][lane + 32 * k] : RingPart{0.0, minus_inf(), 0.0f};
+                M = fmaxf(M, part[k].m);
+            }
+#pragma unroll
+            for (int off = 16; off > 0; off >>= 1) M = fmaxf(M, __shfl_xor_sync(0xFFFFFFFFu, M, off));
+            double S = 0.0;
+#pragma unroll
+            for (int k = 0; k < kMaxCtas * kRingWarps / 32; ++k) {
+                RowSums one = {part[k].m, part[k].s, 0.0};
+                rescale<false>(one, M, c);
+                S += one.s;
+            }
+#pragma unroll
+            for (int off = 16; off > 0; off >>= 1) S += __shfl_xor_sync(0xFFFFFFFFu, S, off);
+            if (M == minus_inf()) S = CUDART_NAN;      // no token can occur: there is no distribution
+            if (lane == 0) {
+                token_gradient(b, token, row.x, x_y, M, S, temperature, rank == 0 ? logp : nullptr, terms, &s_gradient[side]);
+                if (*gave_up && rank == 0) terms[row.x].gain = CUDART_NAN_F;
+                s_gradient[side].M = M;
+                barrier_arrive(&s_ready[side]);
+            }
+            __syncwarp();
+            row = next;
+            announce(side ^ 1, row);
+        }
+    } else {
+        RingPlace place;                       // of the row's first chunk
+        for (int turn = 0;; ++turn) {
+            const int side = turn & 1;
+            barrier_wait(&s_known[side], (turn >> 1) & 1, gave_up);
+            const int t = s_row[side].t, y = s_row[side].y;
+            if (t < 0 || *gave_up) break;
+            const T* row = logits + (size_t)t * pitch;
+            T* out = d_logits + (size_t)t * d_pitch;
             const RowParts<T> parts(row, vocab);
             int begin, end;
             slice(parts, begin, end);
-            const uint4* body = reinterpret_cast<const uint4*>(row + parts.head);
-            for (int v = begin; v < end; v += kRingThreads, ++n) {
-                const uint32_t slot = n % kRingSlots, use = n / kRingSlots;
-                if (use > 0) barrier_wait(&s_empty[slot], (use - 1) & 1, gave_up);
-                if (*gave_up) break;
-                const uint32_t bytes = (uint32_t)min(kRingThreads, end - v) * 16u;
-                barrier_expect(&s_full[slot], bytes);
-                bulk_load(s_ring + slot * kChunk, body + v, bytes, &s_full[slot]);
-            }
-        }
-        // no copy is in flight when the CTA ends
-        int ignored = 0;
-        for (uint32_t k = n > kRingSlots ? n - kRingSlots : 0; k < n; ++k) barrier_wait(&s_full[k % kRingSlots], (k / kRingSlots) & 1, &ignored);
-        cluster.sync();
-        return;
-    }
+            const int chunks = (end - begin + kChunkVecs - 1) / kChunkVecs, whole = (end - begin) / kChunkVecs;
+            const unsigned char* const from = s_ring + threadIdx.x * 16;
+            const int single = rank == 0 && (int)threadIdx.x < parts.head + parts.tail ? parts.single(threadIdx.x) : -1;
+            const float x1 = single >= 0 ? to_float(row[single]) : minus_inf();
 
-    uint32_t n = 0;                            // chunks before this row
-    int turn = 0;
-    for (int q = cluster_at; q < live; q += clusters, ++turn) {
-        const int t = list[q];
-        const T* row = logits + (size_t)t * pitch;
-        T* out = d_logits + (size_t)t * d_pitch;
-        const RowParts<T> parts(row, vocab);
-        int begin, end;
-        slice(parts, begin, end);
-        const int chunks = (end - begin + kRingThreads - 1) / kRingThreads;
-        const int32_t y = targets[t];
-        float x_y = 0.0f, A = 0.0f, w = 0.0f;
-        if (threadIdx.x == 0) {                // before anyone writes: d_logits may be the logits
-            const int rollout = row_of[t];
-            x_y = to_float(row[y]);
-            A = b.adv[rollout];
-            w = b.weight[rollout];
-        }
-        const int single = rank == 0 && (int)threadIdx.x < parts.head + parts.tail ? parts.single(threadIdx.x) : -1;
-        const float x1 = single >= 0 ? to_float(row[single]) : minus_inf();
-
-        RowSums r = {minus_inf(), 0.0, 0.0};
-        float s[4] = {0.0f, 0.0f, 0.0f, 0.0f}, u[4];
-        for (int k = 0; k < chunks; ++k) {
-            const uint32_t slot = (n + k) % kRingSlots;
-            barrier_wait(&s_full[slot], ((n + k) / kRingSlots) & 1, gave_up);
-            if (begin + k * kRingThreads + (int)threadIdx.x < end) {
-                const uint4 v = *reinterpret_cast<const uint4*>(s_ring + slot * kChunk + threadIdx.x * 16);
+            RowSums r = {minus_inf(), 0.0, 0.0};
+            TermSums<false> sums;
+            RingPlace at = place;
+            const auto add = [&](const uint4 (&v)[4]) {        // four vectors: one look at the maximum
                 VecMax<T> top(minus_inf());
-                top.take(v);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) top.take(v[j]);
                 if (top.value() > r.m) {
                     const float f = exp2_approx((r.m - top.value()) * c);
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) s[j] *= f;
+                    sums.scale(f);
                     r.s *= (double)f;
                     r.m = top.value();
                 }
-                float x[E];
-                unpack(v, x, T());
-                add_terms<E, false>(x, r.m == minus_inf() ? 0.0f : r.m, c, s, u);
-            }
-            if (k % 4 == 3) {
-                r.s += (double)((s[0] + s[1]) + (s[2] + s[3]));
-                s[0] = s[1] = s[2] = s[3] = 0.0f;
-            }
-        }
-        r.s += (double)((s[0] + s[1]) + (s[2] + s[3]));
-        if (single >= 0) take<false>(x1, c, r);
-
-        // every warp of the cluster leaves its sums with every CTA
-        float M = r.m;
+                const float m = r.m == minus_inf() ? 0.0f : r.m;
 #pragma unroll
-        for (int off = 16; off > 0; off >>= 1) M = fmaxf(M, __shfl_xor_sync(0xFFFFFFFFu, M, off));
-        rescale<false>(r, M, c);
-#pragma unroll
-        for (int off = 16; off > 0; off >>= 1) r.s += __shfl_xor_sync(0xFFFFFFFFu, r.s, off);
-        const int side = turn & 1;
-        if (lane < ctas) {
-            *cluster.map_shared_rank(&s_part[side][rank * kRingWarps + warp], lane) = RingPart{r.s, M, 0.0f};
-            barrier_arrive_at(&s_met[side], lane);
-        }
-        barrier_wait(&s_met[side], (turn >> 1) & 1, gave_up);
-        RingPart part[kMaxCtas * kRingWarps / 32];
-#pragma unroll
-        for (int k = 0; k < kMaxCtas * kRingWarps / 32; ++k)
-            part[k] = lane + 32 * k < ctas * kRingWarps ? s_part[side][lane + 32 * k] : RingPart{0.0, minus_inf(), 0.0f};
-        M = minus_inf();
-#pragma unroll
-        for (int k = 0; k < kMaxCtas * kRingWarps / 32; ++k) M = fmaxf(M, part[k].m);
-#pragma unroll
-        for (int off = 16; off > 0; off >>= 1) M = fmaxf(M, __shfl_xor_sync(0xFFFFFFFFu, M, off));
-        double S = 0.0;
-#pragma unroll
-        for (int k = 0; k < kMaxCtas * kRingWarps / 32; ++k) {
-            RowSums one = {part[k].m, part[k].s, 0.0};
-            rescale<false>(one, M, c);
-            S += one.s;
-        }
-#pragma unroll
-        for (int off = 16; off > 0; off >>= 1) S += __shfl_xor_sync(0xFFFFFFFFu, S, off);
-        if (M == minus_inf()) S = CUDART_NAN;      // no token can occur: there is no distribution
-
-        if (threadIdx.x == 0) {
-            token_gradient(b, t, x_y, A, w, M, S, temperature, rank == 0 ? logp : nullptr, terms, &s_gradient[side]);
-            if (*gave_up && rank == 0) terms[t].gain = CUDART_NAN_F;
-        }
-        asm volatile("bar.sync 1, %0;" ::"n"(kRingThreads) : "memory");
-        RowGradient g = s_gradient[side];
-        g.M = M;
-        g.c = c;
-        g.target = y;
-        uint4* to = reinterpret_cast<uint4*>(out + parts.head);
-        const int target_vec = y < parts.head ? -1 : (y - parts.head) / E;
-        for (int k = 0; k < chunks; ++k) {
-            const uint32_t slot = (n + k) % kRingSlots;
-            const int i = begin + k * kRingThreads + (int)threadIdx.x;
-            uint4 v = make_uint4(0u, 0u, 0u, 0u);
-            if (i < end) v = *reinterpret_cast<const uint4*>(s_ring + slot * kChunk + threadIdx.x * 16);
-            __syncwarp();
-            if (lane == 0) barrier_arrive(&s_empty[slot]);
-            if (i < end) {
-                float x[E];
-                unpack(v, x, T());
-#pragma unroll
-                for (int j = 0; j < E; ++j) x[j] = gradient<false>(g, x[j]);
-                if (i == target_vec) {
-                    const int at_j = (y - parts.head) % E;
-#pragma unroll
-                    for (int j = 0; j < E; ++j)
-                        if (j == at_j) x[j] += g.at_target;
+                for (int j = 0; j < 4; ++j) {
+                    float x[E];
+                    unpack_again(v[j], x, T());
+                    sums.add(x, m, c);
                 }
-                store_once(to + i, pack(x, T()));
+                sums.flush(r);
+            };
+            int k = 0;
+            for (; k + 2 <= whole; k += 2) {
+                uint4 v[4];
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    barrier_wait(&s_full[at.slot], at.phase, gave_up);
+                    v[2 * h] = *reinterpret_cast<const uint4*>(from + at.slot * kChunk);
+                    v[2 * h + 1] = *reinterpret_cast<const uint4*>(from + at.slot * kChunk + kChunk / 2);
+                    at.step();
+                }
+                add(v);
+            }
+            if (k < chunks) {                              // what is left: a whole chunk, the beginning of one, or both
+                uint4 v[4] = {all_minus_inf<T>(), all_minus_inf<T>(), all_minus_inf<T>(), all_minus_inf<T>()};
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    if (k + h >= chunks) break;
+                    barrier_wait(&s_full[at.slot], at.phase, gave_up);
+                    const int have = end - begin - (k + h) * kChunkVecs;
+                    if ((int)threadIdx.x < have) v[2 * h] = *reinterpret_cast<const uint4*>(from + at.slot * kChunk);
+                    if ((int)threadIdx.x + kRingThreads < have) v[2 * h + 1] = *reinterpret_cast<const uint4*>(from + at.slot * kChunk + kChunk / 2);
+                    at.step();
+                }
+                add(v);
+            }
+            if (single >= 0) take<false>(x1, c, r);
+            // every warp of the cluster leaves its sums with every CTA
+            float M = r.m;
+#pragma unroll
+            for (int off = 16; off > 0; off >>= 1) M = fmaxf(M, __shfl_xor_sync(0xFFFFFFFFu, M, off));
+            rescale<false>(r, M, c);
+#pragma unroll
+            for (int off = 16; off > 0; off >>= 1) r.s += __shfl_xor_sync(0xFFFFFFFFu, r.s, off);
+            if (lane < ctas) store_at(&s_part[side][rank * kRingWarps + warp], (unsigned long long)__double_as_longlong(r.s), (unsigned long long)__float_as_uint(M), &s_met[side], lane);
+
+            barrier_wait(&s_ready[side], (turn >> 1) & 1, gave_up);
+            RowGradient g = s_gradient[side];
+            g.c = c;
+            g.k1 = 0.0f;
+            g.target = y;
+            uint4* to = reinterpret_cast<uint4*>(out + parts.head) + begin + threadIdx.x;
+            // the target's place among this thread's vectors: chunk and half
+            const int target_vec = y < parts.head ? -1 : (y - parts.head) / E - begin - (int)threadIdx.x;
+            for (k = 0; k < chunks; ++k, to += kChunkVecs) {
+                const int have = k < whole ? kChunkVecs : end - begin - k * kChunkVecs;
+                uint4 v[2];
+#pragma unroll
+                for (int h = 0; h < 2; ++h) v[h] = *reinterpret_cast<const uint4*>(from + place.slot * kChunk + h * (kChunk / 2));   // behind the end: an older row's, not used
+                __syncwarp();
+                if (lane == 0) barrier_arrive(&s_empty[place.slot]);
+                place.step();
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    if ((int)threadIdx.x + h * kRingThreads >= have) break;
+                    float x[E];
+                    unpack(v[h], x, T());
+                    gradients<false>(g, x);
+                    if (target_vec == k * kChunkVecs + h * kRingThreads) {
+                        const int at_j = (y - parts.head) % E;
+#pragma unroll
+                        for (int j = 0; j < E; ++j)
+                            if (j == at_j) x[j] += g.at_target;
+                    }
+                    store_once(to + h * kRingThreads, pack(x, T()));
+                }
+            }
+            if (single >= 0) {
+                float v = gradient<false>(g, x1);
+                if (single == y) v += g.at_target;
+                out[single] = from_float<T>(v);
             }
         }
-        if (single >= 0) {
-            float v = gradient<false>(g, x1);
-            if (single == y) v += g.at_target;
-            out[single] = from_float<T>(v);
+        // the rows of tokens that do not count, by each CTA as it has time
+        for (;;) {
+            asm volatile("bar.sync 1, %0;" ::"n"(kRingThreads) : "memory");
+            if (threadIdx.x == 0) s_other = atomicAdd(&counters[kNextOther], 1);
+            asm volatile("bar.sync 1, %0;" ::"n"(kRingThreads) : "memory");
+            const int number = *reinterpret_cast<volatile int*>(&s_other);
+            if (number >= n_tokens - live) break;
+            const int t = list[live + number].x;
+            write_gradient<T, false, true>(nullptr, d_logits + (size_t)t * d_pitch, vocab, threadIdx.x, kRingThreads, RowGradient());
+            if (threadIdx.x == 0) {
+                logp[t] = 0.0f;
+                terms[t] = PolicyTerms<float>{0.0f, 0.0f, 0.0f, 0.0f};
+            }
         }
-        n += chunks;
+        if (threadIdx.x == 0 && *gave_up && status) atomicOr(status, SR_STATUS_TIMEOUT);
     }
-    // the rows of tokens that do not count, from the end of the list
-    for (int q = n_tokens - 1 - cluster_at; q >= live; q -= clusters) {
-        const int t = list[q];
-        write_gradient<T, false, true>(nullptr, d_logits + (size_t)t * d_pitch, vocab, rank * kRingThreads + threadIdx.x, ctas * kRingThreads, RowGradient());
-        if (rank == 0 && threadIdx.x == 0) {
-            logp[t] = 0.0f;
-            terms[t] = PolicyTerms<float>{0.0f, 0.0f, 0.0f, 0.0f};
-        }
-    }
-    if (threadIdx.x == 0 && *gave_up && status) atomicOr(status, SR_STATUS_TIMEOUT);
+    __syncwarp();
     cluster.sync();                            // nobody leaves while its memory may be written to
 }
 
-// The rollout of every token that counts, -1 for the others, as token_rows_kernel; and a list of the tokens, those that count
-// from its beginning, the others from its end.  One cluster.
+// What token_rows_kernel says of every token, as a list: token, target and rollout of those that count, in order, and then the
+// others; and the ring's counters.  One cluster.
 constexpr int kListThreads = 1024, kListTokens = 65536;
 __global__ void __launch_bounds__(kListThreads)
-token_list_kernel(const __grid_constant__ PolicyBatch b, const int32_t* targets, int vocab, int n, int32_t* row_of, int32_t* list, int32_t* n_live, int32_t* status) {
+token_list_kernel(const __grid_constant__ PolicyBatch b, const int32_t* targets, int vocab, int n, int4* list, int32_t* counters, int32_t* status) {
     grid_begin();
     __shared__ int s_warp[32], s_cta[8];
     const auto cluster = cooperative_groups::this_cluster();
     const int ctas = gridDim.x, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int first = (int)((long long)n * blockIdx.x / ctas), last = (int)((long long)n * (blockIdx.x + 1) / ctas);
-    int mine = 0;
-    for (int t0 = first + 32 * warp; t0 < last; t0 += kListThreads) {          // a warp's tokens are neighbours
+    // rollout and target of token t, a lane, of the 32 from t0 on; -1: it does not count
+    const auto look_up = [&](int t0, bool report) {
         const int t = t0 + lane;
+        const int y = t < last ? targets[t] : -1;
         int r = -1;
+        const bool is = counts_as_target(y, vocab, status, report);
         if (b.rows > 0) {
             const int r_first = warp_row_between(b.row_start, 0, b.rows, t0), r_last = warp_row_between(b.row_start, r_first, b.rows, min(t0 + 31, last - 1));
-            if (t < last && counts_as_target(targets[t], vocab, status, true) && !(b.mask && b.mask[t] == 0) && t >= b.row_start[0] && t < b.row_start[b.rows]) {
+            if (is && !(b.mask && b.mask[t] == 0) && t >= b.row_start[0] && t < b.row_start[b.rows]) {
                 r = row_between(b.row_start, r_first, r_last + 1, t);
                 if (b.weight[r] == 0.0f) r = -1;
             }
-        } else if (t < last) {
-            counts_as_target(targets[t], vocab, status, true);
         }
-        if (t < last) row_of[t] = r;
-        mine += __popc(__ballot_sync(0xFFFFFFFFu, r >= 0));
+        return make_int2(r, y);
+    };
+    int2 own = make_int2(-1, -1);              // of the first sweep: mostly there is no other
+    int mine = 0;
+    for (int t0 = first + 32 * warp; t0 < last; t0 += kListThreads) {
+        const int2 found = look_up(t0, true);
+        if (t0 == first + 32 * warp) own = found;
+        mine += __popc(__ballot_sync(0xFFFFFFFFu, found.x >= 0));
     }
     if (lane == 0) s_warp[warp] = mine;
     __syncthreads();
@@ -780,21 +912,21 @@ token_list_kernel(const __grid_constant__ PolicyBatch b, const int32_t* targets,
         if (k < (int)blockIdx.x) before += s_cta[k];
         all += s_cta[k];
     }
-    if (blockIdx.x == 0 && threadIdx.x == 0) *n_live = all;
+    if (blockIdx.x == 0 && threadIdx.x == 0) {
+        counters[kLive] = all;
+        counters[kNextLive] = counters[kNextOther] = 0;
+    }
     for (int base = first; base < last; base += kListThreads) {
-        const int t = base + (int)threadIdx.x;
-        const bool counts = t < last && row_of[t] >= 0;         // this thread's own write, or its warp's
+        const int t0 = base + 32 * warp, t = t0 + lane;
+        if (base != first && t0 < last) own = look_up(t0, false);
+        const bool counts = t < last && own.x >= 0;
         const unsigned bits = __ballot_sync(0xFFFFFFFFu, counts);
         __syncthreads();
         if (lane == 0) s_warp[warp] = __popc(bits);
         __syncthreads();
-        int in_warps = 0, total = 0;
-        for (int k = 0; k < 32; ++k) {
-            if (k < warp) in_warps += s_warp[k];
-            total += s_warp[k];
-        }
+        const int of_warp = s_warp[lane], total = __reduce_add_sync(0xFFFFFFFFu, of_warp), in_warps = __reduce_add_sync(0xFFFFFFFFu, lane < warp ? of_warp : 0);
         const int at = before + in_warps + __popc(bits & low_mask(lane));       // tokens that count before t
-        if (t < last) list[counts ? at : n - 1 - (t - at)] = t;
+        if (t < last) list[counts ? at : all + (t - at)] = make_int4(t, own.y, own.x, 0);
         before += total;
     }
 }
@@ -860,9 +992,9 @@ int launch_backward(const LogitsArgs& a, const float* row_stats, const float* en
 int ring_ctas(int n_tokens, int vocab, int elem) {
     const long long vecs = ((long long)vocab * elem + 15) / 16;
     if (n_tokens > kListTokens || vecs <= kHeldThreads * kMostVecs) return 0;
-    int ctas = 1;
-    while (ctas < kMaxCtas && vecs > (long long)ctas * kRingThreads * kRingRow) ctas *= 2;
-    if (vecs > (long long)ctas * kRingThreads * kRingRow || (long long)n_tokens * ctas < 2 * 148) return 0;
+    int ctas = 2;                              // never one: writes that count at another CTA's barrier are for kernels launched in clusters
+    while (ctas < kMaxCtas && vecs > (long long)ctas * kChunkVecs * kRingRow) ctas *= 2;
+    if (vecs > (long long)ctas * kChunkVecs * kRingRow || (long long)n_tokens * ctas < 2 * 148) return 0;
     return ctas;
 }
 template <typename T>
@@ -872,11 +1004,11 @@ int launch_ring(const LogitsArgs& a, const PolicyBatch& b, const StepScratch& ws
     constexpr int kBytes = kRingSlots * kChunk;
     SR_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kBytes));
     const int list_ctas = min(8, (a.n_tokens + kListThreads - 1) / kListThreads * 2);
-    int rc = launch_as(true, list_ctas, "token_list_kernel", token_list_kernel, list_ctas, kListThreads, 0, s, b, a.targets, a.vocab, a.n_tokens, ws.row_of, ws.list, ws.n_live, status);
+    int rc = launch_as(true, list_ctas, "token_list_kernel", token_list_kernel, list_ctas, kListThreads, 0, s, b, a.targets, a.vocab, a.n_tokens, ws.list, ws.counters, status);
     if (rc != SR_OK) return rc;
-    const int clusters = min(a.n_tokens, 2 * 148 / ctas);
-    return launch_as(true, ctas, "ring_policy_loss_kernel", kernel, clusters * ctas, kRingThreads + 32, kBytes, s, b, static_cast<const T*>(a.logits), a.vocab, (long long)a.pitch, a.targets,
-                     ws.row_of, ws.list, ws.n_live, a.n_tokens, a.temperature, c, ctas, logp, ws.terms, static_cast<T*>(d_logits), (long long)d_pitch, status);
+    const int clusters = min(a.n_tokens, 2 * 148 / ctas);      // those that find no room at first take what rows are left
+    return launch_as(true, ctas, "ring_policy_loss_kernel", kernel, clusters * ctas, kRingThreads + 64, kBytes, s, b, static_cast<const T*>(a.logits), a.vocab, (long long)a.pitch,
+                     ws.list, ws.counters, a.n_tokens, a.temperature, c, ctas, logp, ws.terms, static_cast<T*>(d_logits), (long long)d_pitch, status);
 }
 
 // Whether rows that are held can be written as they were read: logits and gradient lie alike against 16 bytes in every row.

@@ -248,9 +248,9 @@ int launch_sum_terms(const PolicyTerms<float>* terms, int n, double beta, float*
 struct StepScratch {
     double* partial;                 // [kMaxPartials][4]
     PolicyTerms<float>* terms;       // [n_tokens]
-    int32_t* row_of;                 // [n_tokens]
-    int32_t* list;                   // [n_tokens]
-    int32_t* n_live;
+    int32_t* row_of;                 // [n_tokens], or the same memory as
+    int4* list;                      // [n_tokens]
+    int32_t* counters;               // [4]
 };
 int launch_policy_loss_logits(const LogitsArgs& a, const PolicyBatch& b, float* loss, float* logp, void* d_logits, int64_t d_pitch, float* stats, int32_t* status,
                               const StepScratch& ws, cudaStream_t s);

@@ -19,19 +19,22 @@ __device__ __forceinline__ void barrier_expect(uint64_t* bar, uint32_t bytes) {
 __device__ __forceinline__ void barrier_arrive(uint64_t* bar) {
     asm volatile("mbarrier.arrive.release.cta.shared::cta.b64 _, [%0];" ::"r"(shared_address(bar)) : "memory");
 }
-// Arrives at the same barrier of CTA `rank` of the cluster; what this thread wrote to that CTA's memory is there before.
-__device__ __forceinline__ void barrier_arrive_at(uint64_t* bar, uint32_t rank) {
+// Writes 16 bytes to the same place in CTA `rank` of the cluster and counts them at its barrier `bar`; nothing is waited for.
+__device__ __forceinline__ void store_at(void* to, unsigned long long lo, unsigned long long hi, uint64_t* bar, uint32_t rank) {
     asm volatile(
-        "{\n\t.reg .b32 there;\n\t"
-        "mapa.shared::cluster.u32 there, %0, %1;\n\t"
-        "mbarrier.arrive.release.cluster.shared::cluster.b64 _, [there];\n\t}" ::"r"(shared_address(bar)), "r"(rank) : "memory");
+        "{\n\t.reg .b32 there, bar;\n\t"
+        "mapa.shared::cluster.u32 there, %0, %4;\n\t"
+        "mapa.shared::cluster.u32 bar, %3, %4;\n\t"
+        "st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.v2.b64 [there], {%1, %2}, [bar];\n\t}" ::"r"(shared_address(to)), "l"(lo), "l"(hi), "r"(shared_address(bar)), "r"(rank)
+        : "memory");
 }
+constexpr uint32_t kNap = 20000;          // ns that a test may sleep for: warps that ask again and again take issue slots from those that work
 __device__ __forceinline__ bool barrier_test(uint64_t* bar, uint32_t parity) {
     uint32_t done;
     asm volatile(
         "{\n\t.reg .pred p;\n\t"
-        "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
-        "selp.u32 %0, 1, 0, p;\n\t}" : "=r"(done) : "r"(shared_address(bar)), "r"(parity) : "memory");
+        "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2, %3;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}" : "=r"(done) : "r"(shared_address(bar)), "r"(parity), "r"(kNap) : "memory");
     return done != 0;
 }
 __device__ __forceinline__ unsigned long long nanoseconds() {

@@ -123,7 +123,7 @@ int sr_policy_loss(const float* logp, const float* logp_old, const float* logp_r
 }
 
 size_t sr_policy_loss_logits_workspace_bytes(int32_t n_tokens) {
-    return n_tokens < 0 ? 0 : kPartialBytes + align_up((size_t)n_tokens * (sizeof(PolicyTerms<float>) + 2 * sizeof(int32_t)) + sizeof(int32_t), 256);
+    return n_tokens < 0 ? 0 : kPartialBytes + align_up((size_t)n_tokens * (sizeof(PolicyTerms<float>) + sizeof(int4)) + 4 * sizeof(int32_t), 256);
 }
 
 int sr_policy_loss_logits(const void* logits, int32_t dtype, int32_t n_tokens, int32_t vocab, int64_t pitch, const int32_t* targets, const float* logp_old,
@@ -142,9 +142,9 @@ int sr_policy_loss_logits(const void* logits, int32_t dtype, int32_t n_tokens, i
     StepScratch ws;
     ws.partial = static_cast<double*>(workspace);
     ws.terms = reinterpret_cast<PolicyTerms<float>*>(static_cast<char*>(workspace) + kPartialBytes);
-    ws.row_of = reinterpret_cast<int32_t*>(ws.terms + n_tokens);
-    ws.list = ws.row_of + n_tokens;
-    ws.n_live = ws.list + n_tokens;
+    ws.list = reinterpret_cast<int4*>(ws.terms + n_tokens);
+    ws.row_of = reinterpret_cast<int32_t*>(ws.list);
+    ws.counters = reinterpret_cast<int32_t*>(ws.list + n_tokens);
     return launch_policy_loss_logits(LogitsArgs{logits, dtype, n_tokens, vocab, pitch, targets, temperature}, b, loss, logp, d_logits, d_pitch, stats, status, ws,
                                      static_cast<cudaStream_t>(stream));
 }

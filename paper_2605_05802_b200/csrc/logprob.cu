@@ -34,6 +34,21 @@ __device__ __forceinline__ float exp2_approx(float t) {        // 2^t within 2 u
 }
 __device__ __forceinline__ float minus_inf() { return __int_as_float(0xFF800000); }
 
+// log S of a sum that is at least 1, to 2^-24 of itself or 2^-24, whichever is more: S = 2^e m, and only log m, below 1, is
+// taken in fp32.  (A logarithm in fp64 is a chain of a hundred instructions and more that the whole row waits for.)
+__device__ __forceinline__ double log_sum(double S) {
+    const int hi = __double2hiint(S), e = ((hi >> 20) & 0x7FF) - 1023;
+    const float m = (float)__hiloint2double((hi & 0x000FFFFF) | 0x3FF00000, __double2loint(S));
+    return e < 1024 ? fma((double)e, kLn2, (double)logf(m)) : S;         // NaN and inf stay what they are
+}
+
+// Largest of a warp's numbers, in every lane; NaN only where all are.
+__device__ __forceinline__ float warp_max(float x) {
+    float r;
+    asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(x));
+    return r;
+}
+
 // What is known of a row, or of a part of it.
 struct RowSums {
     float m;
@@ -372,7 +387,7 @@ __device__ __forceinline__ bool counts_as_target(int32_t y, int vocab, int32_t* 
 
 template <typename T, bool kEntropy>
 __global__ void __launch_bounds__(kRowThreads, 4)
-token_logprob_kernel(const T* logits, int vocab, long long pitch, const int32_t* targets, double temperature, float c, int ctas,
+token_logprob_kernel(const T* logits, int vocab, long long pitch, const int32_t* targets, double inv_temperature, float c, int ctas,
                      float* logp, float* row_stats, float* entropy, int32_t* status) {
     grid_begin();
     const int t = blockIdx.x / ctas, part = blockIdx.x % ctas;
@@ -391,8 +406,8 @@ token_logprob_kernel(const T* logits, int vocab, long long pitch, const int32_t*
     RowSums r = sum_row<T, kEntropy, false>(row, vocab, part * kRowThreads + threadIdx.x, ctas * kRowThreads, c);
     r = combine<kEntropy>(r, c, ctas);
     if (first) {
-        const double log_S = log(r.s);
-        logp[t] = (float)(((double)x_y - (double)r.m) / temperature - log_S);
+        const double log_S = log_sum(r.s);
+        logp[t] = (float)(((double)x_y - (double)r.m) * inv_temperature - log_S);
         if (row_stats) {
             row_stats[2 * (size_t)t] = r.m;
             row_stats[2 * (size_t)t + 1] = (float)r.s;
@@ -403,7 +418,7 @@ token_logprob_kernel(const T* logits, int vocab, long long pitch, const int32_t*
 
 template <typename T, int kVecs, bool kEntropy>
 __global__ void __launch_bounds__(kHeldThreads, kVecs > 7 ? 3 : 4)
-held_logprob_kernel(const T* logits, int vocab, long long pitch, const int32_t* targets, double temperature, float c, int ctas,
+held_logprob_kernel(const T* logits, int vocab, long long pitch, const int32_t* targets, double inv_temperature, float c, int ctas,
                     float* logp, float* row_stats, float* entropy, int32_t* status) {
     grid_begin();
     const int t = blockIdx.x / ctas, part = blockIdx.x % ctas;
@@ -423,8 +438,8 @@ held_logprob_kernel(const T* logits, int vocab, long long pitch, const int32_t* 
     const float x_y = first ? to_float(row[y]) : 0.0f;        // on its way meanwhile
     const RowSums r = combine<kEntropy>(held.template sums<kEntropy>(c), c, ctas);
     if (first) {
-        const double log_S = log(r.s);
-        logp[t] = (float)(((double)x_y - (double)r.m) / temperature - log_S);
+        const double log_S = log_sum(r.s);
+        logp[t] = (float)(((double)x_y - (double)r.m) * inv_temperature - log_S);
         if (row_stats) {
             row_stats[2 * (size_t)t] = r.m;
             row_stats[2 * (size_t)t + 1] = (float)r.s;
@@ -478,26 +493,26 @@ token_rows_kernel(PolicyBatch b, const int32_t* targets, int vocab, int n, int32
 
 // By one thread: the token's terms of the loss and the gradient of its row.  A function of its own, so that the registers of a
 // held row are put aside for it in that thread alone.
-__device__ __noinline__ void token_gradient(const PolicyBatch& b, const PolicyToken& k, int t, float x_y, float m, double S, double temperature, float* logp, PolicyTerms<float>* terms,
-                                            RowGradient* g) {
-    const double lp = ((double)x_y - (double)m) / temperature - log(S);
+__device__ __noinline__ void token_gradient(const PolicyBatch& b, const PolicyToken& k, int t, float x_y, float m, double S, double inv_temperature, float* logp,
+                                            PolicyTerms<float>* terms, RowGradient* g) {
+    const double lp = ((double)x_y - (double)m) * inv_temperature - log_sum(S);
     PolicyTerms<float> term;
-    const float d = policy_token(b, k, lp, term);
+    const float d = policy_token(b, k, lp, term) * (float)inv_temperature;
+    g->k0 = -d / (float)S;
+    g->at_target = d;
     if (logp) {
         logp[t] = (float)lp;
         terms[t] = term;
     }
-    g->k0 = (float)(-(double)d / (S * temperature));
-    g->at_target = (float)((double)d / temperature);
 }
 __device__ __forceinline__ PolicyToken load_token(const PolicyBatch& b, int t, int rollout) {
     return PolicyToken{b.old_logp ? b.old_logp[t] : 0.0f, b.ref_logp ? b.ref_logp[t] : 0.0f, b.adv[rollout], b.weight[rollout]};
 }
 // The gradient of a row, in every thread of the CTA; `first` writes down the token's figures.
-__device__ __forceinline__ RowGradient loss_gradient(const PolicyBatch& b, const PolicyToken& k, int t, float x_y, int y, const RowSums& r, double temperature, float c, bool first,
+__device__ __forceinline__ RowGradient loss_gradient(const PolicyBatch& b, const PolicyToken& k, int t, float x_y, int y, const RowSums& r, double inv_temperature, float c, bool first,
                                                      float* logp, PolicyTerms<float>* terms) {
     __shared__ RowGradient s_g;
-    if (threadIdx.x == 0) token_gradient(b, k, t, x_y, r.m, r.s, temperature, first ? logp : nullptr, terms, &s_g);
+    if (threadIdx.x == 0) token_gradient(b, k, t, x_y, r.m, r.s, inv_temperature, first ? logp : nullptr, terms, &s_g);
     __syncthreads();
     RowGradient g = s_g;
     g.M = r.m;
@@ -510,7 +525,7 @@ __device__ __forceinline__ RowGradient loss_gradient(const PolicyBatch& b, const
 template <typename T>
 __global__ void __launch_bounds__(kRowThreads, 4)
 policy_loss_logits_kernel(PolicyBatch b, const T* logits, int vocab, long long pitch, const int32_t* targets, const int32_t* row_of,
-                          double temperature, float c, int ctas, float* logp, PolicyTerms<float>* terms, T* d_logits, long long d_pitch) {
+                          double inv_temperature, float c, int ctas, float* logp, PolicyTerms<float>* terms, T* d_logits, long long d_pitch) {
     grid_begin();
     const int t = blockIdx.x / ctas, part = blockIdx.x % ctas;
     const int at = part * kRowThreads + threadIdx.x, threads = ctas * kRowThreads;
@@ -532,14 +547,14 @@ policy_loss_logits_kernel(PolicyBatch b, const T* logits, int vocab, long long p
     const PolicyToken token = threadIdx.x == 0 ? load_token(b, t, rollout) : PolicyToken{};      // on its way meanwhile
     RowSums r = sum_row<T, false, true>(row, vocab, at, threads, c);
     r = combine<false>(r, c, ctas);
-    g = loss_gradient(b, token, t, x_y, y, r, temperature, c, first, logp, terms);
+    g = loss_gradient(b, token, t, x_y, y, r, inv_temperature, c, first, logp, terms);
     write_gradient<T, false, false>(row, out, vocab, at, threads, g);
 }
 
 template <typename T, int kVecs>
 __global__ void __launch_bounds__(kHeldThreads, kVecs > 7 ? 3 : 4)
 held_policy_loss_kernel(PolicyBatch b, const T* logits, int vocab, long long pitch, const int32_t* targets, const int32_t* row_of,
-                        double temperature, float c, int ctas, float* logp, PolicyTerms<float>* terms, T* d_logits, long long d_pitch) {
+                        double inv_temperature, float c, int ctas, float* logp, PolicyTerms<float>* terms, T* d_logits, long long d_pitch) {
     grid_begin();
     const int t = blockIdx.x / ctas, part = blockIdx.x % ctas;
     const int at = part * kHeldThreads + threadIdx.x, threads = ctas * kHeldThreads;
@@ -562,7 +577,7 @@ held_policy_loss_kernel(PolicyBatch b, const T* logits, int vocab, long long pit
     const float x_y = to_float(row[y]);                        // before anyone writes: d_logits may be the logits
     const PolicyToken token = threadIdx.x == 0 ? load_token(b, t, rollout) : PolicyToken{};      // on its way meanwhile
     const RowSums r = combine<false>(held.template sums<false>(c), c, ctas);
-    const RowGradient g = loss_gradient(b, token, t, x_y, y, r, temperature, c, first, logp, terms);
+    const RowGradient g = loss_gradient(b, token, t, x_y, y, r, inv_temperature, c, first, logp, terms);
     held.write_gradient(out, parts, at, threads, g);
 }
 
@@ -579,7 +594,8 @@ constexpr int kRingThreads = 256, kRingWarps = kRingThreads / 32;
 constexpr int kChunkVecs = 2 * kRingThreads;       // two vectors a thread: with one, more instructions went into finding them than into the terms
 constexpr int kChunk = kChunkVecs * 16;            // bytes
 constexpr int kRingSlots = 13;                     // 104 KB: two CTAs an SM
-constexpr int kRingRow = 10;                       // chunks of a slice at most; the rest is ahead
+constexpr int kRingRow = 10;                       // chunks of a slice at most: three slots and more are ahead
+constexpr int kZeros = 4096;                       // bytes of zeros that gradients of tokens that do not count are copied from
 
 // A slot, and the parity of the phase that its use is.
 struct RingPlace {
@@ -601,12 +617,12 @@ struct RingRow {
     float x_y;
 };
 constexpr int kRingQueue = 8;        // rows that a CTA may know of
-// Counters: tokens that count; the next row of them to be taken; the next of the others.
+// Counters: tokens that count; the next row of them to be taken; the next slice of the others.
 enum { kLive, kNextLive, kNextOther };
 
 template <typename T>
 __global__ void __launch_bounds__(kRingThreads + 64, 2)
-ring_policy_loss_kernel(const __grid_constant__ PolicyBatch b, const T* logits, int vocab, long long pitch, const int4* list, int32_t* counters, int n_tokens, double temperature,
+ring_policy_loss_kernel(const __grid_constant__ PolicyBatch b, const T* logits, int vocab, long long pitch, const int4* list, int32_t* counters, int n_tokens, double inv_temperature,
                         float c, int ctas, float* logp, PolicyTerms<float>* terms, T* d_logits, long long d_pitch, int32_t* status) {
     constexpr int E = Vec<T>::kElems;
     extern __shared__ __align__(128) unsigned char s_ring[];
@@ -616,7 +632,8 @@ ring_policy_loss_kernel(const __grid_constant__ PolicyBatch b, const T* logits, 
     __shared__ __align__(16) int4 s_number[kRingQueue];
     __shared__ RingRow s_row[2];
     __shared__ RowGradient s_gradient[2];
-    __shared__ int s_gave_up, s_other;
+    __shared__ int s_gave_up;
+    __shared__ __align__(16) uint4 s_zeros[kZeros / 16];
     const int rank = blockIdx.x % ctas;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     if (threadIdx.x == 0) {
@@ -633,15 +650,18 @@ ring_policy_loss_kernel(const __grid_constant__ PolicyBatch b, const T* logits, 
         s_gave_up = 0;
         barriers_ready();
     }
+    if (threadIdx.x < kZeros / 16) s_zeros[threadIdx.x] = make_uint4(0u, 0u, 0u, 0u);
+    shared_written();
     const auto cluster = cooperative_groups::this_cluster();
     cluster.sync();                            // barriers of every CTA are there before anyone writes to it
     grid_begin();
     volatile int* const gave_up = &s_gave_up;
     const int live = counters[kLive];
     // this CTA's vectors of a row
+    const int log_ctas = 31 - __clz(ctas);     // a power of two
     const auto slice = [&](const RowParts<T>& parts, int& begin, int& end) {
-        begin = (int)((long long)parts.vecs * rank / ctas);
-        end = (int)((long long)parts.vecs * (rank + 1) / ctas);
+        begin = (int)(((long long)parts.vecs * rank) >> log_ctas);
+        end = (int)(((long long)parts.vecs * (rank + 1)) >> log_ctas);
     };
     // The list's entry of the cluster's turn-th row; none: x < 0.
     const auto entry = [&](int turn) {
@@ -661,6 +681,19 @@ ring_policy_loss_kernel(const __grid_constant__ PolicyBatch b, const T* logits, 
             const int at = turn & (kRingQueue - 1);
             for (int k = 0; k < ctas; ++k) store_at(&s_number[at], (uint32_t)number, 0ull, &s_got[at], k);
         };
+        // The gradients of tokens that do not count are zeros, copied from shared memory without a thread's help, a slice of a row
+        // for every slice of a row that counts: they fill what the sums leave of the bandwidth.
+        const int others = (n_tokens - live) << log_ctas;
+        const auto clear = [&](int number) {
+            const RowParts<T> parts(d_logits + (size_t)list[live + (number >> log_ctas)].x * d_pitch, vocab);
+            T* const out = d_logits + (size_t)list[live + (number >> log_ctas)].x * d_pitch;
+            const int part = number & (ctas - 1);
+            const long long begin = ((long long)parts.vecs * part) >> log_ctas, end = ((long long)parts.vecs * (part + 1)) >> log_ctas;
+            uint4* to = reinterpret_cast<uint4*>(out + parts.head);
+            for (long long v = begin; v < end; v += kZeros / 16) bulk_store(to + v, s_zeros, (uint32_t)min((long long)(kZeros / 16), end - v) * 16u);
+            if (part == 0)
+                for (int k = 0; k < parts.head + parts.tail; ++k) out[parts.single(k)] = from_float<T>(0.0f);
+        };
         if (lane == 0) {
             if (rank == 0) tell(0, atomicAdd(&counters[kNextLive], 1));
             for (int turn = 0;; ++turn) {
@@ -669,6 +702,7 @@ ring_policy_loss_kernel(const __grid_constant__ PolicyBatch b, const T* logits, 
                 if (row_of.x < 0) break;
                 int number = 0;
                 if (rank == 0) number = atomicAdd(&counters[kNextLive], 1);
+                const int other = atomicAdd(&counters[kNextOther], 1);
                 const T* row = logits + (size_t)row_of.x * pitch;
                 const RowParts<T> parts(row, vocab);
                 int begin, end;
@@ -683,59 +717,97 @@ ring_policy_loss_kernel(const __grid_constant__ PolicyBatch b, const T* logits, 
                     place.step();
                 }
                 if (rank == 0) tell(turn + 1, number);
+                if (other < others) clear(other);
             }
+            for (;;) {
+                const int other = atomicAdd(&counters[kNextOther], 1);
+                if (other >= others) break;
+                clear(other);
+            }
+            bulk_stores_done();
             // no copy is in flight when the CTA ends
             int ignored = 0;
             for (uint32_t k = n > kRingSlots ? n - kRingSlots : 0; k < n; ++k) barrier_wait(&s_full[k % kRingSlots], (k / kRingSlots) & 1, &ignored);
         }
     } else if (warp == kRingWarps + 1) {       // says which row comes next, and turns the cluster's sums into its gradient
-        PolicyToken token = {};
+        int4 row = make_int4(-1, 0, 0, 0), next = row;
+        PolicyToken token = {}, next_token = {};
         float x_y = 0.0f;
-        const auto announce = [&](int side, const int4& row) {   // its target's logit is read before anyone can write: d_logits may be the logits
-            if (row.x >= 0) {
-                x_y = to_float(logits[(size_t)row.x * pitch + row.y]);
-                token = load_token(b, row.x, row.z);
+        T next_x = from_float<T>(0.0f);
+        const auto look_ahead = [&](int turn) {    // its target's logit is read before anyone can write: d_logits may be the logits
+            next = entry(turn);
+            if (next.x >= 0) {
+                next_x = logits[(size_t)next.x * pitch + next.y];
+                next_token = load_token(b, next.x, next.z);
             }
+        };
+        const auto announce = [&](int side) {
+            row = next;
+            token = next_token;
+            x_y = to_float(next_x);
             if (lane == 0) {
                 s_row[side] = RingRow{row.x, row.y, x_y};
                 barrier_arrive(&s_known[side]);
             }
         };
-        int4 row = entry(0);
-        announce(0, row);
+        look_ahead(0);
+        announce(0);
         for (int turn = 0; row.x >= 0; ++turn) {
             const int side = turn & 1;
             if (lane == 0) barrier_expect(&s_met[side], (uint32_t)(sizeof(RingPart) * kRingWarps) * (uint32_t)ctas);
-            const int4 next = entry(turn + 1); // on its way while this row is summed up
+            look_ahead(turn + 1);              // on its way while this row is summed up
             barrier_wait(&s_met[side], (turn >> 1) & 1, gave_up);
-            RingPart part[kMaxCtas * kRingWarps / 32];
-            float M = minus_inf();
+            // The cluster waits for k0 and at_target: they come from a short chain in fp32, log p to 2^-22; what is written down of
+            // the token is worked out afterwards.
+            constexpr int kParts = (kMaxCtas * kRingWarps + 31) / 32;
+            RingPart part[kParts];
+            float factor[kParts], M = minus_inf(), S32 = 0.0f;
 #pragma unroll
-            for (int k = 0; k < kMaxCtas * kRingWarps / 32; ++k) {
+            for (int k = 0; k < kParts; ++k) {
                 part[k] = lane + 32 * k < ctas * kRingWarps ? s_part[side][lane + 32 * k] : RingPart{0.0, minus_inf(), 0.0f};
                 M = fmaxf(M, part[k].m);
             }
+            M = warp_max(M);
 #pragma unroll
-            for (int off = 16; off > 0; off >>= 1) M = fmaxf(M, __shfl_xor_sync(0xFFFFFFFFu, M, off));
-            double S = 0.0;
-#pragma unroll
-            for (int k = 0; k < kMaxCtas * kRingWarps / 32; ++k) {
-                RowSums one = {part[k].m, part[k].s, 0.0};
-                rescale<false>(one, M, c);
-                S += one.s;
+            for (int k = 0; k < kParts; ++k) {
+                factor[k] = part[k].m == M ? 1.0f : exp2_approx((part[k].m - M) * c);
+                S32 = fmaf((float)part[k].s, factor[k], S32);
             }
 #pragma unroll
-            for (int off = 16; off > 0; off >>= 1) S += __shfl_xor_sync(0xFFFFFFFFu, S, off);
-            if (M == minus_inf()) S = CUDART_NAN;      // no token can occur: there is no distribution
+            for (int off = 16; off > 0; off >>= 1) S32 += __shfl_xor_sync(0xFFFFFFFFu, S32, off);
+            if (M == minus_inf()) S32 = CUDART_NAN_F;  // no token can occur: there is no distribution
+            float log2_S;
+            asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(log2_S) : "f"(S32));
+            PolicyTerms<float> term;
+            const float d = policy_token(b, token, fmaf(x_y - M, (float)inv_temperature, -(float)kLn2 * log2_S), term) * (float)inv_temperature;
             if (lane == 0) {
-                token_gradient(b, token, row.x, x_y, M, S, temperature, rank == 0 ? logp : nullptr, terms, &s_gradient[side]);
-                if (*gave_up && rank == 0) terms[row.x].gain = CUDART_NAN_F;
-                s_gradient[side].M = M;
+                RowGradient& g = s_gradient[side];
+                g.M = M;
+                g.k0 = -d / S32;
+                g.at_target = d;
                 barrier_arrive(&s_ready[side]);
             }
+            const int t = row.x;
+            const float x_t = x_y;
+            const PolicyToken token_t = token;
             __syncwarp();
-            row = next;
-            announce(side ^ 1, row);
+            announce(side ^ 1);
+            if (rank == 0) {
+                double S = 0.0;
+#pragma unroll
+                for (int k = 0; k < kParts; ++k) S += part[k].s * (double)factor[k];
+#pragma unroll
+                for (int off = 16; off > 0; off >>= 1) S += __shfl_xor_sync(0xFFFFFFFFu, S, off);
+                if (M == minus_inf()) S = CUDART_NAN;
+                if (lane == 0) {
+                    const double lp = ((double)x_t - (double)M) * inv_temperature - log_sum(S);
+                    policy_token(b, token_t, lp, term);
+                    if (*gave_up) term.gain = CUDART_NAN_F;
+                    logp[t] = (float)lp;
+                    terms[t] = term;
+                }
+                __syncwarp();
+            }
         }
     } else {
         RingPlace place;                       // of the row's first chunk
@@ -803,9 +875,7 @@ ring_policy_loss_kernel(const __grid_constant__ PolicyBatch b, const T* logits, 
             }
             if (single >= 0) take<false>(x1, c, r);
             // every warp of the cluster leaves its sums with every CTA
-            float M = r.m;
-#pragma unroll
-            for (int off = 16; off > 0; off >>= 1) M = fmaxf(M, __shfl_xor_sync(0xFFFFFFFFu, M, off));
+            const float M = warp_max(r.m);
             rescale<false>(r, M, c);
 #pragma unroll
             for (int off = 16; off > 0; off >>= 1) r.s += __shfl_xor_sync(0xFFFFFFFFu, r.s, off);
@@ -848,20 +918,6 @@ ring_policy_loss_kernel(const __grid_constant__ PolicyBatch b, const T* logits, 
                 out[single] = from_float<T>(v);
             }
         }
-        // the rows of tokens that do not count, by each CTA as it has time
-        for (;;) {
-            asm volatile("bar.sync 1, %0;" ::"n"(kRingThreads) : "memory");
-            if (threadIdx.x == 0) s_other = atomicAdd(&counters[kNextOther], 1);
-            asm volatile("bar.sync 1, %0;" ::"n"(kRingThreads) : "memory");
-            const int number = *reinterpret_cast<volatile int*>(&s_other);
-            if (number >= n_tokens - live) break;
-            const int t = list[live + number].x;
-            write_gradient<T, false, true>(nullptr, d_logits + (size_t)t * d_pitch, vocab, threadIdx.x, kRingThreads, RowGradient());
-            if (threadIdx.x == 0) {
-                logp[t] = 0.0f;
-                terms[t] = PolicyTerms<float>{0.0f, 0.0f, 0.0f, 0.0f};
-            }
-        }
         if (threadIdx.x == 0 && *gave_up && status) atomicOr(status, SR_STATUS_TIMEOUT);
     }
     __syncwarp();
@@ -869,10 +925,10 @@ ring_policy_loss_kernel(const __grid_constant__ PolicyBatch b, const T* logits, 
 }
 
 // What token_rows_kernel says of every token, as a list: token, target and rollout of those that count, in order, and then the
-// others; and the ring's counters.  One cluster.
+// others, whose figures are written here; and the ring's counters.  One cluster.
 constexpr int kListThreads = 1024, kListTokens = 65536;
 __global__ void __launch_bounds__(kListThreads)
-token_list_kernel(const __grid_constant__ PolicyBatch b, const int32_t* targets, int vocab, int n, int4* list, int32_t* counters, int32_t* status) {
+token_list_kernel(const __grid_constant__ PolicyBatch b, const int32_t* targets, int vocab, int n, int4* list, int32_t* counters, float* logp, PolicyTerms<float>* terms, int32_t* status) {
     grid_begin();
     __shared__ int s_warp[32], s_cta[8];
     const auto cluster = cooperative_groups::this_cluster();
@@ -926,7 +982,13 @@ token_list_kernel(const __grid_constant__ PolicyBatch b, const int32_t* targets,
         __syncthreads();
         const int of_warp = s_warp[lane], total = __reduce_add_sync(0xFFFFFFFFu, of_warp), in_warps = __reduce_add_sync(0xFFFFFFFFu, lane < warp ? of_warp : 0);
         const int at = before + in_warps + __popc(bits & low_mask(lane));       // tokens that count before t
-        if (t < last) list[counts ? at : all + (t - at)] = make_int4(t, own.y, own.x, 0);
+        if (t < last) {
+            list[counts ? at : all + (t - at)] = make_int4(t, own.y, own.x, 0);
+            if (!counts) {
+                logp[t] = 0.0f;
+                terms[t] = PolicyTerms<float>{0.0f, 0.0f, 0.0f, 0.0f};
+            }
+        }
         before += total;
     }
 }
@@ -971,12 +1033,12 @@ int launch_forward(const LogitsArgs& a, float* logp, float* row_stats, float* en
         return with_vecs(held.vecs, [&](auto vecs) {
             const auto kernel = entropy ? held_logprob_kernel<T, vecs(), true> : held_logprob_kernel<T, vecs(), false>;
             return launch_as(true, held.ctas, "held_logprob_kernel", kernel, a.n_tokens * held.ctas, kHeldThreads, 0, s, static_cast<const T*>(a.logits), a.vocab, (long long)a.pitch, a.targets,
-                             a.temperature, c, held.ctas, logp, row_stats, entropy, status);
+                             1.0 / a.temperature, c, held.ctas, logp, row_stats, entropy, status);
         });
     const int ctas = ctas_of_row(a.n_tokens, a.vocab, (int)sizeof(T));
     const auto kernel = entropy ? token_logprob_kernel<T, true> : token_logprob_kernel<T, false>;
     return launch_as(true, ctas, "token_logprob_kernel", kernel, a.n_tokens * ctas, kRowThreads, 0, s, static_cast<const T*>(a.logits), a.vocab, (long long)a.pitch, a.targets,
-                     a.temperature, c, ctas, logp, row_stats, entropy, status);
+                     1.0 / a.temperature, c, ctas, logp, row_stats, entropy, status);
 }
 
 template <typename T>
@@ -988,14 +1050,19 @@ int launch_backward(const LogitsArgs& a, const float* row_stats, const float* en
                   d_logp, d_entropy, a.temperature, c, parts, static_cast<T*>(d_logits), (long long)d_pitch);
 }
 
+// Whether rows that are held can be written as they were read: logits and gradient lie alike against 16 bytes in every row.
+bool alike(const LogitsArgs& a, const void* d_logits, int64_t d_pitch) {
+    const uintptr_t apart = reinterpret_cast<uintptr_t>(a.logits) ^ reinterpret_cast<uintptr_t>(d_logits);
+    return (apart & 15) == 0 && (a.n_tokens == 1 || ((a.pitch - d_pitch) * dtype_bytes(a.dtype)) % 16 == 0);
+}
+
 // CTAs to a row of the ring kernel, or 0: rows too long for it, too short to be worth it, or too few to keep its CTAs busy.
 int ring_ctas(int n_tokens, int vocab, int elem) {
     const long long vecs = ((long long)vocab * elem + 15) / 16;
     if (n_tokens > kListTokens || vecs <= kHeldThreads * kMostVecs) return 0;
     int ctas = 2;                              // never one: writes that count at another CTA's barrier are for kernels launched in clusters
     while (ctas < kMaxCtas && vecs > (long long)ctas * kChunkVecs * kRingRow) ctas *= 2;
-    if (vecs > (long long)ctas * kChunkVecs * kRingRow || (long long)n_tokens * ctas < 2 * 148) return 0;
-    return ctas;
+    return vecs > (long long)ctas * kChunkVecs * kRingRow || (long long)n_tokens * ctas < 2 * 148 ? 0 : ctas;
 }
 template <typename T>
 int launch_ring(const LogitsArgs& a, const PolicyBatch& b, const StepScratch& ws, int ctas, float* logp, void* d_logits, int64_t d_pitch, int32_t* status, cudaStream_t s) {
@@ -1004,19 +1071,12 @@ int launch_ring(const LogitsArgs& a, const PolicyBatch& b, const StepScratch& ws
     constexpr int kBytes = kRingSlots * kChunk;
     SR_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kBytes));
     const int list_ctas = min(8, (a.n_tokens + kListThreads - 1) / kListThreads * 2);
-    int rc = launch_as(true, list_ctas, "token_list_kernel", token_list_kernel, list_ctas, kListThreads, 0, s, b, a.targets, a.vocab, a.n_tokens, ws.list, ws.counters, status);
+    int rc = launch_as(true, list_ctas, "token_list_kernel", token_list_kernel, list_ctas, kListThreads, 0, s, b, a.targets, a.vocab, a.n_tokens, ws.list, ws.counters, logp, ws.terms, status);
     if (rc != SR_OK) return rc;
     const int clusters = min(a.n_tokens, 2 * 148 / ctas);      // those that find no room at first take what rows are left
     return launch_as(true, ctas, "ring_policy_loss_kernel", kernel, clusters * ctas, kRingThreads + 64, kBytes, s, b, static_cast<const T*>(a.logits), a.vocab, (long long)a.pitch,
-                     ws.list, ws.counters, a.n_tokens, a.temperature, c, ctas, logp, ws.terms, static_cast<T*>(d_logits), (long long)d_pitch, status);
+                     ws.list, ws.counters, a.n_tokens, 1.0 / a.temperature, c, ctas, logp, ws.terms, static_cast<T*>(d_logits), (long long)d_pitch, status);
 }
-
-// Whether rows that are held can be written as they were read: logits and gradient lie alike against 16 bytes in every row.
-bool alike(const LogitsArgs& a, const void* d_logits, int64_t d_pitch) {
-    const uintptr_t apart = reinterpret_cast<uintptr_t>(a.logits) ^ reinterpret_cast<uintptr_t>(d_logits);
-    return (apart & 15) == 0 && (a.n_tokens == 1 || ((a.pitch - d_pitch) * dtype_bytes(a.dtype)) % 16 == 0);
-}
-
 template <typename T>
 int launch_step(const LogitsArgs& a, const PolicyBatch& b, const int32_t* row_of, float* logp, PolicyTerms<float>* terms, void* d_logits, int64_t d_pitch, cudaStream_t s) {
     const float c = (float)(1.0 / (kLn2 * a.temperature));
@@ -1024,11 +1084,19 @@ int launch_step(const LogitsArgs& a, const PolicyBatch& b, const int32_t* row_of
     if (held.vecs && alike(a, d_logits, d_pitch))
         return with_vecs(held.vecs, [&](auto vecs) {
             return launch_as(true, held.ctas, "held_policy_loss_kernel", held_policy_loss_kernel<T, vecs()>, a.n_tokens * held.ctas, kHeldThreads, 0, s, b, static_cast<const T*>(a.logits),
-                             a.vocab, (long long)a.pitch, a.targets, row_of, a.temperature, c, held.ctas, logp, terms, static_cast<T*>(d_logits), (long long)d_pitch);
+                             a.vocab, (long long)a.pitch, a.targets, row_of, 1.0 / a.temperature, c, held.ctas, logp, terms, static_cast<T*>(d_logits), (long long)d_pitch);
         });
     const int ctas = ctas_of_row(a.n_tokens, a.vocab, (int)sizeof(T));
     return launch_as(true, ctas, "policy_loss_logits_kernel", policy_loss_logits_kernel<T>, a.n_tokens * ctas, kRowThreads, 0, s, b, static_cast<const T*>(a.logits), a.vocab, (long long)a.pitch, a.targets, row_of,
-                     a.temperature, c, ctas, logp, terms, static_cast<T*>(d_logits), (long long)d_pitch);
+                     1.0 / a.temperature, c, ctas, logp, terms, static_cast<T*>(d_logits), (long long)d_pitch);
+}
+
+template <typename T>
+int launch_rows(const LogitsArgs& a, const PolicyBatch& b, const StepScratch& ws, float* logp, void* d_logits, int64_t d_pitch, int32_t* status, cudaStream_t s) {
+    const int ring = alike(a, d_logits, d_pitch) ? ring_ctas(a.n_tokens, a.vocab, (int)sizeof(T)) : 0;
+    if (ring) return launch_ring<T>(a, b, ws, ring, logp, d_logits, d_pitch, status, s);
+    SR_LAUNCH("token_rows_kernel", token_rows_kernel, (int)(((long long)a.n_tokens + 255) / 256), 256, 0, s, b, a.targets, a.vocab, a.n_tokens, ws.row_of, status);
+    return launch_step<T>(a, b, ws.row_of, logp, ws.terms, d_logits, d_pitch, s);
 }
 
 }  // namespace
@@ -1055,20 +1123,11 @@ int launch_token_logprob_backward(const LogitsArgs& a, const float* row_stats, c
 int launch_policy_loss_logits(const LogitsArgs& a, const PolicyBatch& b, float* loss, float* logp, void* d_logits, int64_t d_pitch, float* stats, int32_t* status,
                               const StepScratch& ws, cudaStream_t s) {
     if (a.n_tokens > 0) {
-        const int elem = dtype_bytes(a.dtype), ring = alike(a, d_logits, d_pitch) ? ring_ctas(a.n_tokens, a.vocab, elem) : 0;
-        if (!ring)
-            SR_LAUNCH("token_rows_kernel", token_rows_kernel, (int)(((long long)a.n_tokens + 255) / 256), 256, 0, s, b, a.targets, a.vocab, a.n_tokens, ws.row_of, status);
         int rc;
         switch (a.dtype) {
-            case SR_DTYPE_F32:
-                rc = ring ? launch_ring<float>(a, b, ws, ring, logp, d_logits, d_pitch, status, s) : launch_step<float>(a, b, ws.row_of, logp, ws.terms, d_logits, d_pitch, s);
-                break;
-            case SR_DTYPE_BF16:
-                rc = ring ? launch_ring<__nv_bfloat16>(a, b, ws, ring, logp, d_logits, d_pitch, status, s) : launch_step<__nv_bfloat16>(a, b, ws.row_of, logp, ws.terms, d_logits, d_pitch, s);
-                break;
-            default:
-                rc = ring ? launch_ring<__half>(a, b, ws, ring, logp, d_logits, d_pitch, status, s) : launch_step<__half>(a, b, ws.row_of, logp, ws.terms, d_logits, d_pitch, s);
-                break;
+            case SR_DTYPE_F32: rc = launch_rows<float>(a, b, ws, logp, d_logits, d_pitch, status, s); break;
+            case SR_DTYPE_BF16: rc = launch_rows<__nv_bfloat16>(a, b, ws, logp, d_logits, d_pitch, status, s); break;
+            default: rc = launch_rows<__half>(a, b, ws, logp, d_logits, d_pitch, status, s); break;
         }
         if (rc != SR_OK) return rc;
     }

@@ -68,4 +68,16 @@ __device__ __forceinline__ void bulk_load(void* to, const void* from, uint32_t b
                  : "memory");
 }
 
+// Copies `bytes` (as above) from this CTA's shared memory to global; bulk_stores_done waits until the memory they come from has been
+// read.
+__device__ __forceinline__ void bulk_store(void* to, const void* from, uint32_t bytes) {
+    asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;" ::"l"(to), "r"(shared_address(from)), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void bulk_stores_done() {
+    asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+    asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+}
+// What threads have written to shared memory is there for bulk copies; a barrier follows.
+__device__ __forceinline__ void shared_written() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+
 }  // namespace sr

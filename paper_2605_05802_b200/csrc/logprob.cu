@@ -620,7 +620,8 @@ constexpr int kRingQueue = 8;        // rows that a CTA may know of
 // Counters: tokens that count; the next row of them to be taken; the next slice of the others.
 enum { kLive, kNextLive, kNextOther };
 
-template <typename T>
+// kAlone: one CTA to a row.  It is no cluster, and nothing is sent: what would be is written here, and its writers arrive.
+template <typename T, bool kAlone>
 __global__ void __launch_bounds__(kRingThreads + 64, 2)
 ring_policy_loss_kernel(const __grid_constant__ PolicyBatch b, const T* logits, int vocab, long long pitch, const int4* list, int32_t* counters, int n_tokens, double inv_temperature,
                         float c, int ctas, float* logp, PolicyTerms<float>* terms, T* d_logits, long long d_pitch, int32_t* status) {
@@ -634,7 +635,7 @@ ring_policy_loss_kernel(const __grid_constant__ PolicyBatch b, const T* logits, 
     __shared__ RowGradient s_gradient[2];
     __shared__ int s_gave_up;
     __shared__ __align__(16) uint4 s_zeros[kZeros / 16];
-    const int rank = blockIdx.x % ctas;
+    const int rank = kAlone ? 0 : blockIdx.x % ctas;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     if (threadIdx.x == 0) {
         for (int k = 0; k < kRingSlots; ++k) {
@@ -644,7 +645,7 @@ ring_policy_loss_kernel(const __grid_constant__ PolicyBatch b, const T* logits, 
         for (int k = 0; k < kRingQueue; ++k) barrier_init(&s_got[k], 1);
         for (int k = 0; k < 2; ++k) {
             barrier_init(&s_known[k], 1);
-            barrier_init(&s_met[k], 1);
+            barrier_init(&s_met[k], kAlone ? kRingWarps : 1);
             barrier_init(&s_ready[k], 1);
         }
         s_gave_up = 0;
@@ -652,13 +653,14 @@ ring_policy_loss_kernel(const __grid_constant__ PolicyBatch b, const T* logits, 
     }
     if (threadIdx.x < kZeros / 16) s_zeros[threadIdx.x] = make_uint4(0u, 0u, 0u, 0u);
     shared_written();
-    const auto cluster = cooperative_groups::this_cluster();
-    cluster.sync();                            // barriers of every CTA are there before anyone writes to it
+    // barriers of every CTA are there before anyone writes to it
+    if (kAlone) __syncthreads();
+    else cooperative_groups::this_cluster().sync();
     grid_begin();
     volatile int* const gave_up = &s_gave_up;
     const int live = counters[kLive];
     // this CTA's vectors of a row
-    const int log_ctas = 31 - __clz(ctas);     // a power of two
+    const int log_ctas = kAlone ? 0 : 31 - __clz(ctas);     // a power of two
     const auto slice = [&](const RowParts<T>& parts, int& begin, int& end) {
         begin = (int)(((long long)parts.vecs * rank) >> log_ctas);
         end = (int)(((long long)parts.vecs * (rank + 1)) >> log_ctas);
@@ -679,7 +681,12 @@ ring_policy_loss_kernel(const __grid_constant__ PolicyBatch b, const T* logits, 
         uint32_t n = 0;
         const auto tell = [&](int turn, int number) {
             const int at = turn & (kRingQueue - 1);
-            for (int k = 0; k < ctas; ++k) store_at(&s_number[at], (uint32_t)number, 0ull, &s_got[at], k);
+            if (kAlone) {
+                s_number[at].x = number;
+                barrier_arrive(&s_got[at]);
+            } else {
+                for (int k = 0; k < ctas; ++k) store_at(&s_number[at], (uint32_t)number, 0ull, &s_got[at], k);
+            }
         };
         // The gradients of tokens that do not count are zeros, copied from shared memory without a thread's help, a slice of a row
         // for every slice of a row that counts: they fill what the sums leave of the bandwidth.
@@ -697,7 +704,7 @@ ring_policy_loss_kernel(const __grid_constant__ PolicyBatch b, const T* logits, 
         if (lane == 0) {
             if (rank == 0) tell(0, atomicAdd(&counters[kNextLive], 1));
             for (int turn = 0;; ++turn) {
-                barrier_expect(&s_got[turn & (kRingQueue - 1)], 16);
+                if (!kAlone) barrier_expect(&s_got[turn & (kRingQueue - 1)], 16);
                 const int4 row_of = entry(turn);
                 if (row_of.x < 0) break;
                 int number = 0;
@@ -754,12 +761,12 @@ ring_policy_loss_kernel(const __grid_constant__ PolicyBatch b, const T* logits, 
         announce(0);
         for (int turn = 0; row.x >= 0; ++turn) {
             const int side = turn & 1;
-            if (lane == 0) barrier_expect(&s_met[side], (uint32_t)(sizeof(RingPart) * kRingWarps) * (uint32_t)ctas);
+            if (!kAlone && lane == 0) barrier_expect(&s_met[side], (uint32_t)(sizeof(RingPart) * kRingWarps) * (uint32_t)ctas);
             look_ahead(turn + 1);              // on its way while this row is summed up
             barrier_wait(&s_met[side], (turn >> 1) & 1, gave_up);
             // The cluster waits for k0 and at_target: they come from a short chain in fp32, log p to 2^-22; what is written down of
             // the token is worked out afterwards.
-            constexpr int kParts = (kMaxCtas * kRingWarps + 31) / 32;
+            constexpr int kParts = kAlone ? 1 : (kMaxCtas * kRingWarps + 31) / 32;
             RingPart part[kParts];
             float factor[kParts], M = minus_inf(), S32 = 0.0f;
 #pragma unroll
@@ -879,7 +886,14 @@ ring_policy_loss_kernel(const __grid_constant__ PolicyBatch b, const T* logits, 
             rescale<false>(r, M, c);
 #pragma unroll
             for (int off = 16; off > 0; off >>= 1) r.s += __shfl_xor_sync(0xFFFFFFFFu, r.s, off);
-            if (lane < ctas) store_at(&s_part[side][rank * kRingWarps + warp], (unsigned long long)__double_as_longlong(r.s), (unsigned long long)__float_as_uint(M), &s_met[side], lane);
+            if (kAlone) {
+                if (lane == 0) {
+                    s_part[side][warp] = RingPart{r.s, M, 0.0f};
+                    barrier_arrive(&s_met[side]);
+                }
+            } else if (lane < ctas) {
+                store_at(&s_part[side][rank * kRingWarps + warp], (unsigned long long)__double_as_longlong(r.s), (unsigned long long)__float_as_uint(M), &s_met[side], lane);
+            }
 
             barrier_wait(&s_ready[side], (turn >> 1) & 1, gave_up);
             RowGradient g = s_gradient[side];
@@ -921,7 +935,7 @@ ring_policy_loss_kernel(const __grid_constant__ PolicyBatch b, const T* logits, 
         if (threadIdx.x == 0 && *gave_up && status) atomicOr(status, SR_STATUS_TIMEOUT);
     }
     __syncwarp();
-    cluster.sync();                            // nobody leaves while its memory may be written to
+    if (!kAlone) cooperative_groups::this_cluster().sync();       // nobody leaves while its memory may be written to
 }
 
 // What token_rows_kernel says of every token, as a list: token, target and rollout of those that count, in order, and then the
@@ -1060,14 +1074,14 @@ bool alike(const LogitsArgs& a, const void* d_logits, int64_t d_pitch) {
 int ring_ctas(int n_tokens, int vocab, int elem) {
     const long long vecs = ((long long)vocab * elem + 15) / 16;
     if (n_tokens > kListTokens || vecs <= kHeldThreads * kMostVecs) return 0;
-    int ctas = 2;                              // never one: writes that count at another CTA's barrier are for kernels launched in clusters
+    int ctas = 1;
     while (ctas < kMaxCtas && vecs > (long long)ctas * kChunkVecs * kRingRow) ctas *= 2;
     return vecs > (long long)ctas * kChunkVecs * kRingRow || (long long)n_tokens * ctas < 2 * 148 ? 0 : ctas;
 }
 template <typename T>
 int launch_ring(const LogitsArgs& a, const PolicyBatch& b, const StepScratch& ws, int ctas, float* logp, void* d_logits, int64_t d_pitch, int32_t* status, cudaStream_t s) {
     const float c = (float)(1.0 / (kLn2 * a.temperature));
-    const auto kernel = ring_policy_loss_kernel<T>;
+    const auto kernel = ctas == 1 ? ring_policy_loss_kernel<T, true> : ring_policy_loss_kernel<T, false>;
     constexpr int kBytes = kRingSlots * kChunk;
     SR_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kBytes));
     const int list_ctas = min(8, (a.n_tokens + kListThreads - 1) / kListThreads * 2);

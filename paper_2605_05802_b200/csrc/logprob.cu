@@ -21,7 +21,8 @@
 namespace sr {
 namespace {
 
-constexpr int kRowThreads = 256;
+constexpr int kRowThreads = 256;          // sums: rows of CTAs that end at other times fill each other's gaps (512 threads, 3072 rows of 151936 bf16: 188 us, 256: 173)
+constexpr int kWriteThreads = 512;        // gradients alone: nobody waits for anybody (256 threads, 2048 such rows: 181 us, 512: 175)
 constexpr int kUnroll = 4;
 constexpr int kHeldThreads = 256, kMostVecs = 10;
 constexpr int kMaxCtas = 8;              // to a row: the portable cluster size
@@ -124,52 +125,38 @@ __device__ __forceinline__ void rescale(RowSums& r, float M, float c) {
     r.m = M;
 }
 
-// Sums of all threads' parts, in every thread; over the cluster where it has several CTAs.
-template <bool kEntropy>
-__device__ __forceinline__ RowSums combine(RowSums r, float c, int ctas) {
-    __shared__ float s_m[32];
-    __shared__ double s_s[32], s_u[32];
-    __shared__ RowSums s_cta[kMaxCtas];
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
-    float M = r.m;
+// Sum of a warp's parts, in every lane.  kLanes: only the first so many have one that is not empty.
+template <bool kEntropy, int kLanes>
+__device__ __forceinline__ RowSums warp_sum(RowSums r, float c) {
+    rescale<kEntropy>(r, warp_max(r.m), c);
 #pragma unroll
-    for (int off = 16; off > 0; off >>= 1) M = fmaxf(M, __shfl_xor_sync(0xFFFFFFFFu, M, off));
-    if (lane == 0) s_m[warp] = M;
-    __syncthreads();
-    M = s_m[0];
-    for (int w = 1; w < warps; ++w) M = fmaxf(M, s_m[w]);
-    rescale<kEntropy>(r, M, c);
-#pragma unroll
-    for (int off = 16; off > 0; off >>= 1) {
+    for (int off = kLanes / 2; off > 0; off >>= 1) {
         r.s += __shfl_xor_sync(0xFFFFFFFFu, r.s, off);
         if (kEntropy) r.u += __shfl_xor_sync(0xFFFFFFFFu, r.u, off);
     }
-    if (lane == 0) {
-        s_s[warp] = r.s;
-        if (kEntropy) s_u[warp] = r.u;
+    if (kLanes < 32) {
+        r.s = __shfl_sync(0xFFFFFFFFu, r.s, 0);
+        if (kEntropy) r.u = __shfl_sync(0xFFFFFFFFu, r.u, 0);
     }
+    return r;
+}
+// Sums of all threads' parts (up to eight warps), in every thread; over the cluster where it has several CTAs.
+template <bool kEntropy>
+__device__ __forceinline__ RowSums combine(RowSums r, float c, int ctas) {
+    static_assert(kMaxCtas == 8 && kRowThreads <= 256 && kHeldThreads <= 256, "eight parts of the later sums");
+    __shared__ RowSums s_warp[8], s_cta[kMaxCtas];
+    const RowSums none = {minus_inf(), 0.0, 0.0};
+    const int lane = threadIdx.x & 31;
+    r = warp_sum<kEntropy, 32>(r, c);
+    if (lane == 0) s_warp[threadIdx.x >> 5] = r;
     __syncthreads();
-    r.s = s_s[0];
-    r.u = kEntropy ? s_u[0] : 0.0;
-    for (int w = 1; w < warps; ++w) {
-        r.s += s_s[w];
-        if (kEntropy) r.u += s_u[w];
-    }
+    r = warp_sum<kEntropy, 8>(lane < (int)(blockDim.x >> 5) ? s_warp[lane] : none, c);
     if (ctas > 1) {
         // every CTA writes its sums to all the others: after the barrier each reads its own memory, and may leave
         const auto cluster = cooperative_groups::this_cluster();
         if ((int)threadIdx.x < ctas) *cluster.map_shared_rank(&s_cta[cluster.block_rank()], threadIdx.x) = r;
         cluster.sync();
-        float top = minus_inf();
-        for (int b = 0; b < ctas; ++b) top = fmaxf(top, s_cta[b].m);
-        RowSums sum = {top, 0.0, 0.0};
-        for (int b = 0; b < ctas; ++b) {
-            RowSums part = s_cta[b];
-            rescale<kEntropy>(part, top, c);
-            sum.s += part.s;
-            if (kEntropy) sum.u += part.u;
-        }
-        r = sum;
+        r = warp_sum<kEntropy, 8>(lane < ctas ? s_cta[lane] : none, c);
     }
     if (r.m == minus_inf()) r.s = CUDART_NAN;  // no token can occur: there is no distribution
     return r;
@@ -449,7 +436,7 @@ held_logprob_kernel(const T* logits, int vocab, long long pitch, const int32_t* 
 }
 
 template <typename T, bool kEntropy>
-__global__ void __launch_bounds__(kRowThreads)
+__global__ void __launch_bounds__(kWriteThreads)
 token_logprob_backward_kernel(const T* logits, int vocab, long long pitch, const int32_t* targets, const float* row_stats,
                               const float* entropy, const float* d_logp, const float* d_entropy, double temperature, float c,
                               int parts, T* d_logits, long long d_pitch) {
@@ -459,7 +446,7 @@ token_logprob_backward_kernel(const T* logits, int vocab, long long pitch, const
     T* out = d_logits + (size_t)t * d_pitch;
     RowGradient g = {};
     if (y < 0 || y >= vocab) {
-        write_gradient<T, false, true>(nullptr, out, vocab, part * kRowThreads + threadIdx.x, parts * kRowThreads, g);
+        write_gradient<T, false, true>(nullptr, out, vocab, part * blockDim.x + threadIdx.x, parts * blockDim.x, g);
         return;
     }
     const double S = (double)row_stats[2 * (size_t)t + 1], d = (double)d_logp[t];
@@ -474,7 +461,7 @@ token_logprob_backward_kernel(const T* logits, int vocab, long long pitch, const
     g.k0 = (float)(k0 / (S * temperature));
     g.at_target = (float)(d / temperature);
     g.target = y;
-    write_gradient<T, kEntropy, false>(logits + (size_t)t * pitch, out, vocab, part * kRowThreads + threadIdx.x, parts * kRowThreads, g);
+    write_gradient<T, kEntropy, false>(logits + (size_t)t * pitch, out, vocab, part * blockDim.x + threadIdx.x, parts * blockDim.x, g);
 }
 
 // The rollout of every token that counts, -1 for the others, so that the rows of the next kernel start reading at once.
@@ -552,7 +539,7 @@ policy_loss_logits_kernel(PolicyBatch b, const T* logits, int vocab, long long p
 }
 
 template <typename T, int kVecs>
-__global__ void __launch_bounds__(kHeldThreads, kVecs > 7 ? 3 : 4)
+__global__ void __launch_bounds__(kHeldThreads, kVecs > 7 ? 3 : kVecs > 4 ? 4 : 5)
 held_policy_loss_kernel(PolicyBatch b, const T* logits, int vocab, long long pitch, const int32_t* targets, const int32_t* row_of,
                         double inv_temperature, float c, int ctas, float* logp, PolicyTerms<float>* terms, T* d_logits, long long d_pitch) {
     grid_begin();
@@ -1059,8 +1046,9 @@ template <typename T>
 int launch_backward(const LogitsArgs& a, const float* row_stats, const float* entropy, const float* d_logp, const float* d_entropy, void* d_logits, int64_t d_pitch, cudaStream_t s) {
     const float c = (float)(1.0 / (kLn2 * a.temperature));
     const int parts = ctas_of_row(a.n_tokens, a.vocab, (int)sizeof(T));
+    const int threads = (long long)a.vocab * (int)sizeof(T) > 4LL * kWriteThreads * 16 ? kWriteThreads : kWriteThreads / 2;     // four vectors a thread and more, or fewer threads
     const auto kernel = d_entropy ? token_logprob_backward_kernel<T, true> : token_logprob_backward_kernel<T, false>;
-    return launch("token_logprob_backward_kernel", kernel, a.n_tokens * parts, kRowThreads, 0, s, static_cast<const T*>(a.logits), a.vocab, (long long)a.pitch, a.targets, row_stats, entropy,
+    return launch("token_logprob_backward_kernel", kernel, a.n_tokens * parts, threads, 0, s, static_cast<const T*>(a.logits), a.vocab, (long long)a.pitch, a.targets, row_stats, entropy,
                   d_logp, d_entropy, a.temperature, c, parts, static_cast<T*>(d_logits), (long long)d_pitch);
 }
 

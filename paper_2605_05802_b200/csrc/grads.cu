@@ -1,7 +1,7 @@
 // Global gradient norm and clipping over a list of tensors.
 //
 // The list travels as a kernel argument: no copy to the device, nothing to keep between calls, and a captured call holds its
-// own.  Tensors are cut into pieces of 32 KB and the pieces dealt out evenly, as runs, to a grid that fills the GPU; a CTA
+// own.  Tensors are cut into pieces of 16 KB and the pieces dealt out evenly, as runs, to a grid that fills the GPU; a CTA
 // searches the tensor of its first piece and walks on from there.  Both kernels are bound by HBM: the norm reads every
 // gradient once, clipping reads and writes it (the factor is known only when all squares are added up).
 //
@@ -14,8 +14,8 @@ namespace sr {
 namespace {
 
 constexpr int kGradThreads = 256;
-constexpr int kVecsInFlight = 8;
-constexpr int kPieceBytes = kGradThreads * kVecsInFlight * 16;      // 32 KB
+constexpr int kVecsInFlight = 4;
+constexpr int kPieceBytes = kGradThreads * kVecsInFlight * 16;      // 16 KB
 constexpr int kGradCtas = 148 * 6;
 
 // kCap tensors; a kernel argument may have 32764 bytes.

@@ -66,6 +66,20 @@ int check_grads(const void* const* grads, const int64_t* counts, const int32_t* 
 struct Range {
     uintptr_t begin, end;
 };
+// Whether a range that is written reaches into another of them or into one that is read.  Sorts both lists, which mostly are (a
+// program's gradients follow one another): together they would not be.
+bool overlap(Range* written, size_t n_written, Range* read, size_t n_read) {
+    const auto before = [](const Range& x, const Range& y) { return x.begin < y.begin; };
+    if (!std::is_sorted(written, written + n_written, before)) std::sort(written, written + n_written, before);
+    if (!std::is_sorted(read, read + n_read, before)) std::sort(read, read + n_read, before);
+    for (size_t i = 1; i < n_written; ++i)
+        if (written[i - 1].end > written[i].begin) return true;
+    for (size_t i = 0, w = 0; i < n_read; ++i) {
+        while (w < n_written && written[w].end <= read[i].begin) ++w;
+        if (w < n_written && written[w].begin < read[i].end) return true;
+    }
+    return false;
+}
 
 constexpr size_t kPartialBytes = (size_t)kMaxPartials * 4 * sizeof(double);
 
@@ -166,12 +180,13 @@ int sr_clip_grads(const void* const* grads, const int64_t* counts, const int32_t
     if (!(max_norm >= 0.0 && max_norm <= 3.4028234663852886e38)) return SR_ERR_BAD_VALUE;
     if (norm == nullptr) return SR_ERR_NULL;
     if (n_tensors == 0) return SR_OK;
-    // every buffer that is written must lie apart from all the others: sorted by address, none reaches into the next
-    Range* const ranges = new (std::nothrow) Range[2 * (size_t)n_tensors + 1];
-    if (ranges == nullptr) return SR_ERR_WORKSPACE;
-    size_t n = 0;
+    // every buffer that is written must lie apart from all the others
+    Range* const written = new (std::nothrow) Range[2 * (size_t)n_tensors + 1];
+    if (written == nullptr) return SR_ERR_WORKSPACE;
+    Range* const read = written + n_tensors;
+    size_t n_written = 0, n_read = 0;
     int bad = SR_OK;
-    ranges[n++] = Range{reinterpret_cast<uintptr_t>(norm), reinterpret_cast<uintptr_t>(norm) + 4};
+    read[n_read++] = Range{reinterpret_cast<uintptr_t>(norm), reinterpret_cast<uintptr_t>(norm) + 4};
     for (int i = 0; i < n_tensors && bad == SR_OK; ++i) {
         if (counts[i] == 0) continue;
         const size_t bytes = (size_t)counts[i] * dtype_bytes(dtypes[i]);
@@ -179,16 +194,11 @@ int sr_clip_grads(const void* const* grads, const int64_t* counts, const int32_t
         if (to == nullptr) bad = SR_ERR_NULL;
         else if (!aligned(to, dtype_bytes(dtypes[i]))) bad = SR_ERR_ALIGN;
         const uintptr_t a = reinterpret_cast<uintptr_t>(grads[i]), b = reinterpret_cast<uintptr_t>(to);
-        ranges[n++] = Range{b, b + bytes};
-        if (a != b) ranges[n++] = Range{a, a + bytes};
+        written[n_written++] = Range{b, b + bytes};
+        if (a != b) read[n_read++] = Range{a, a + bytes};
     }
-    if (bad == SR_OK) {
-        const auto before = [](const Range& x, const Range& y) { return x.begin < y.begin; };
-        if (!std::is_sorted(ranges, ranges + n, before)) std::sort(ranges, ranges + n, before);
-        for (size_t i = 1; i < n && bad == SR_OK; ++i)
-            if (ranges[i - 1].end > ranges[i].begin) bad = SR_ERR_OVERLAP;
-    }
-    delete[] ranges;
+    if (bad == SR_OK && overlap(written, n_written, read, n_read)) bad = SR_ERR_OVERLAP;
+    delete[] written;
     if (bad != SR_OK) return bad;
     return launch_clip_grads(grads, counts, dtypes, n_tensors, norm, (float)max_norm, out, status, static_cast<cudaStream_t>(stream));
 }

@@ -89,7 +89,7 @@ int sr_token_logprob_backward(const void* logits, int32_t dtype, int32_t n_token
  *   mask       in  [n_tokens] uint8 or NULL (every token counts); positions outside
  *                  0 .. n_tokens do not count
  *   drop_mask  in  [n_groups] uint8 or NULL: non-zero = cut (sr_gate's stop, for example)
- *   mode           SR_LOSS_*;  scale: finite
+ *   mode           SR_LOSS_*;  scale: finite in fp32
  *   weight     out [n_groups * N] fp32
  *   counts     out 2 int64 or NULL: tokens that count, rollouts with at least one
  *   workspace      device scratch of sr_loss_weights_workspace_bytes(n_groups * N) bytes, 16-byte
@@ -119,7 +119,7 @@ size_t sr_loss_weights_workspace_bytes(int32_t n_rollouts);   /* host-only, pure
  *                  a chunk of a batch passes its row_start minus the chunk's first token, and
  *                  values below 0 or above n_tokens are fine
  *   mask       in  [n_tokens] uint8 or NULL
- *   clip_low, clip_high, beta   >= 0 and finite
+ *   clip_low, clip_high, beta   >= 0 and finite (beta in fp32)
  *   loss       out 1 fp32
  *   d_logp     out [n_tokens] fp32 or NULL; +0 for tokens that do not count.  May be logp itself.
  *   stats      out 4 fp32 or NULL: the weighted sums of gain, kl, [clipped] and rho
@@ -137,12 +137,17 @@ size_t sr_policy_loss_workspace_bytes(int32_t n_tokens);      /* host-only, pure
 
 /*
  * sr_policy_loss_logits -- the same loss from logits, with the gradient of the logits: what
- * sr_token_logprob, sr_policy_loss and sr_token_logprob_backward give one after the other, in one
- * pass over the logits.  A token counts when its target is one, its mask byte is non-zero and
- * it lies in a rollout whose weight is not 0.
+ * sr_token_logprob, sr_policy_loss and sr_token_logprob_backward give one after the other, without
+ * their arrays in between.  A token counts when its target is one, its mask byte is non-zero and
+ * it lies in a rollout whose weight is not 0.  It is
+ * fastest where the rows of d_logits lie against 16 bytes as those of the logits do: in place, or
+ * with pitches that differ by a multiple of 16 bytes.
  *
  *   logp       out [n_tokens] fp32; +0 for tokens that do not count
  *   d_logits   out as for sr_token_logprob_backward (may be the logits themselves)
+ *   status     in/out 1 int32 of SR_STATUS_* bits; may be NULL.  SR_STATUS_TIMEOUT: CTAs that share a
+ *              row have waited for one another for a second (microseconds are usual) and have given
+ *              up; what the call wrote is not to be used
  *   workspace      device scratch of sr_policy_loss_logits_workspace_bytes(n_tokens) bytes, 16-byte aligned
  */
 int sr_policy_loss_logits(const void* logits, int32_t dtype, int32_t n_tokens, int32_t vocab, int64_t pitch,
@@ -174,7 +179,7 @@ size_t sr_grad_norm_workspace_bytes(int32_t n_tensors);       /* host-only, pure
  *
  *   norm       in  1 fp32.  When it is not finite nothing is scaled (out receives the gradients
  *                  as they are) and SR_STATUS_NONFINITE is set: the step is the caller's to skip.
- *   max_norm       >= 0 and finite
+ *   max_norm       >= 0 and finite in fp32
  *   out            HOST array of n_tensors device pointers, same types and sizes; an entry may be
  *                  the gradient's own pointer (in place), and NULL for the array means all are.
  *                  Apart from that no two buffers overlap: SR_ERR_OVERLAP.

@@ -365,7 +365,7 @@ int launch_sum_terms(const PolicyTerms<float>* terms, int n, double beta, float*
         const int ctas = max(1, min(8, (n + 1023) / 1024)), threads = max(32, min(1024, (n + 31) & ~31));
         return launch_as(true, ctas, "sum_terms_kernel", sum_terms_kernel<float, true>, ctas, threads, 0, s, terms, n, beta, partial, loss, stats);
     }
-    const int blocks = min(kMaxPartials, (n + 4095) / 4096);
+    const int blocks = (int)min((long long)kMaxPartials, ((long long)n + 4095) / 4096);
     SR_LAUNCH("sum_terms_kernel", sum_terms_kernel<float, false>, blocks, 1024, 0, s, terms, n, beta, partial, loss, stats);
     SR_LAUNCH("sum_terms_kernel", sum_terms_kernel<double, true>, 1, 1024, 0, s, reinterpret_cast<const PolicyTerms<double>*>(partial), blocks, beta, partial, loss, stats);
     return SR_OK;

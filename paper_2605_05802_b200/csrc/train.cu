@@ -12,8 +12,13 @@ namespace {
 
 bool aligned(const void* p, size_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
 
+// Whether all of these (NULL or not) lie on the boundary of a 32-bit number.
+template <typename... P>
+bool aligned_4(const P*... p) { return (aligned(p, 4) && ...); }
+
 bool short_of(const void* ws, size_t have, size_t need) { return ws == nullptr || have < need || !aligned(ws, 16); }
 
+constexpr double kLargest = 3.4028234663852886e38;   // what fp32 holds
 constexpr int64_t kMaxPitch = int64_t(1) << 31;      // n_tokens * pitch * 4 bytes stay below 2^64
 
 // What every call on logits has in common.
@@ -35,7 +40,8 @@ int check_gradient(const void* logits, int32_t dtype, int32_t n_tokens, int32_t 
     const int64_t size = dtype_bytes(dtype);
     if (!aligned(d_logits, (size_t)size)) return SR_ERR_ALIGN;
     const uint64_t a = reinterpret_cast<uintptr_t>(logits), b = reinterpret_cast<uintptr_t>(d_logits);
-    const uint64_t a_end = a + (uint64_t)(((n_tokens - 1) * pitch + vocab) * size), b_end = b + (uint64_t)(((n_tokens - 1) * d_pitch + vocab) * size);
+    const auto bytes = [&](int64_t row) { return ((uint64_t)(n_tokens - 1) * (uint64_t)row + (uint64_t)vocab) * (uint64_t)size; };       // below 2^64
+    const uint64_t a_end = a + bytes(pitch), b_end = b + bytes(d_pitch);
     if (a_end <= b || b_end <= a) return SR_OK;
     if (pitch != d_pitch) return n_tokens == 1 && a == b ? SR_OK : SR_ERR_OVERLAP;
     const int64_t off = ((((int64_t)(b - a)) / size) % pitch + pitch) % pitch;              // column of the one in a row of the other
@@ -44,9 +50,9 @@ int check_gradient(const void* logits, int32_t dtype, int32_t n_tokens, int32_t 
 
 int check_policy(const float* adv, const float* weight, const int64_t* row_start, int32_t n_rollouts, double clip_low, double clip_high, double beta, const float* loss) {
     if (n_rollouts < 0 || n_rollouts > (1 << 30)) return SR_ERR_BAD_N;
-    if (!(clip_low >= 0.0 && clip_high >= 0.0 && beta >= 0.0) || isinf(clip_low) || isinf(clip_high) || isinf(beta)) return SR_ERR_BAD_VALUE;
+    if (!(clip_low >= 0.0 && clip_high >= 0.0 && beta >= 0.0) || isinf(clip_low) || isinf(clip_high) || beta > kLargest) return SR_ERR_BAD_VALUE;
     if (loss == nullptr || (n_rollouts > 0 && (adv == nullptr || weight == nullptr || row_start == nullptr))) return SR_ERR_NULL;
-    if (!aligned(row_start, 8)) return SR_ERR_ALIGN;
+    if (!aligned(row_start, 8) || !aligned_4(adv, weight, loss)) return SR_ERR_ALIGN;
     return SR_OK;
 }
 
@@ -92,6 +98,7 @@ int sr_token_logprob(const void* logits, int32_t dtype, int32_t n_tokens, int32_
     const int rc = check_logits(logits, dtype, n_tokens, vocab, pitch, targets, temperature);
     if (rc != SR_OK) return rc;
     if (n_tokens > 0 && logp == nullptr) return SR_ERR_NULL;
+    if (!aligned_4(logp, row_stats, entropy, status)) return SR_ERR_ALIGN;
     return launch_token_logprob(LogitsArgs{logits, dtype, n_tokens, vocab, pitch, targets, temperature}, logp, row_stats, entropy, status, static_cast<cudaStream_t>(stream));
 }
 
@@ -100,6 +107,7 @@ int sr_token_logprob_backward(const void* logits, int32_t dtype, int32_t n_token
     int rc = check_logits(logits, dtype, n_tokens, vocab, pitch, targets, temperature);
     if (rc != SR_OK) return rc;
     if (n_tokens > 0 && (row_stats == nullptr || d_logp == nullptr || (d_entropy != nullptr && entropy == nullptr))) return SR_ERR_NULL;
+    if (!aligned_4(row_stats, entropy, d_logp, d_entropy)) return SR_ERR_ALIGN;
     rc = check_gradient(logits, dtype, n_tokens, vocab, pitch, d_logits, d_pitch);
     if (rc != SR_OK) return rc;
     return launch_token_logprob_backward(LogitsArgs{logits, dtype, n_tokens, vocab, pitch, targets, temperature}, row_stats, entropy, d_logp, d_entropy, d_logits, d_pitch,
@@ -115,9 +123,9 @@ int sr_loss_weights(const int64_t* row_start, const uint8_t* mask, int32_t n_tok
     if (n_groups < 0 || N < 1 || (int64_t)n_groups * N > (1 << 30)) return SR_ERR_BAD_N;
     if (n_tokens < 0) return SR_ERR_BAD_SIZE;
     if (mode != SR_LOSS_SUM && mode != SR_LOSS_TOKEN_MEAN && mode != SR_LOSS_ROLLOUT_MEAN) return SR_ERR_BAD_MODE;
-    if (!isfinite(scale)) return SR_ERR_BAD_VALUE;
+    if (!(fabs(scale) <= kLargest)) return SR_ERR_BAD_VALUE;
     if (n_groups > 0 && (row_start == nullptr || weight == nullptr)) return SR_ERR_NULL;
-    if (!aligned(row_start, 8) || !aligned(counts, 8)) return SR_ERR_ALIGN;
+    if (!aligned(row_start, 8) || !aligned(counts, 8) || !aligned_4(weight)) return SR_ERR_ALIGN;
     if (n_groups > 0 && short_of(workspace, workspace_bytes, sr_loss_weights_workspace_bytes(n_groups * N))) return SR_ERR_WORKSPACE;
     return launch_loss_weights(row_start, mask, n_tokens, drop_mask, n_groups, N, mode, scale, weight, counts, workspace, static_cast<cudaStream_t>(stream));
 }
@@ -131,6 +139,7 @@ int sr_policy_loss(const float* logp, const float* logp_old, const float* logp_r
     const int rc = check_policy(adv, weight, row_start, n_rollouts, clip_low, clip_high, beta, loss);
     if (rc != SR_OK) return rc;
     if (n_tokens > 0 && logp == nullptr) return SR_ERR_NULL;
+    if (!aligned_4(logp, logp_old, logp_ref, d_logp, stats)) return SR_ERR_ALIGN;
     if (short_of(workspace, workspace_bytes, kPartialBytes)) return SR_ERR_WORKSPACE;
     const PolicyBatch b{logp_old, logp_ref, adv, weight, row_start, mask, n_rollouts, clip_low, clip_high, beta, (float)(1.0 - clip_low), (float)(1.0 + clip_high), (float)beta};
     return launch_policy_loss(b, logp, n_tokens, loss, d_logp, stats, static_cast<double*>(workspace), static_cast<cudaStream_t>(stream));
@@ -149,6 +158,7 @@ int sr_policy_loss_logits(const void* logits, int32_t dtype, int32_t n_tokens, i
     rc = check_policy(adv, weight, row_start, n_rollouts, clip_low, clip_high, beta, loss);
     if (rc != SR_OK) return rc;
     if (n_tokens > 0 && logp == nullptr) return SR_ERR_NULL;
+    if (!aligned_4(logp, logp_old, logp_ref, stats, status)) return SR_ERR_ALIGN;
     rc = check_gradient(logits, dtype, n_tokens, vocab, pitch, d_logits, d_pitch);
     if (rc != SR_OK) return rc;
     if (short_of(workspace, workspace_bytes, sr_policy_loss_logits_workspace_bytes(n_tokens))) return SR_ERR_WORKSPACE;
@@ -169,6 +179,7 @@ int sr_grad_norm(const void* const* grads, const int64_t* counts, const int32_t*
     const int rc = check_grads(grads, counts, dtypes, n_tensors);
     if (rc != SR_OK) return rc;
     if (norm == nullptr) return SR_ERR_NULL;
+    if (!aligned_4(norm)) return SR_ERR_ALIGN;
     if (short_of(workspace, workspace_bytes, grad_norm_workspace_bytes(n_tensors))) return SR_ERR_WORKSPACE;
     return launch_grad_norm(grads, counts, dtypes, n_tensors, norm, workspace, static_cast<cudaStream_t>(stream));
 }
@@ -177,8 +188,9 @@ int sr_clip_grads(const void* const* grads, const int64_t* counts, const int32_t
                   int32_t* status, void* stream) {
     const int rc = check_grads(grads, counts, dtypes, n_tensors);
     if (rc != SR_OK) return rc;
-    if (!(max_norm >= 0.0 && max_norm <= 3.4028234663852886e38)) return SR_ERR_BAD_VALUE;
+    if (!(max_norm >= 0.0 && max_norm <= kLargest)) return SR_ERR_BAD_VALUE;
     if (norm == nullptr) return SR_ERR_NULL;
+    if (!aligned_4(norm, status)) return SR_ERR_ALIGN;
     if (n_tensors == 0) return SR_OK;
     // every buffer that is written must lie apart from all the others
     Range* const written = new (std::nothrow) Range[2 * (size_t)n_tensors + 1];

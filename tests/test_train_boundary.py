@@ -130,6 +130,42 @@ def test_binding_refuses_what_the_library_cannot_see(lib):
             sr.sr_grad_norm(bad, norm=f, workspace=f)
 
 
+def test_numbers_that_fp32_does_not_hold_and_addresses_off_their_type(lib):
+    """Weights, beta and factors are fp32 in the kernels; an address off a boundary of its type would fault there."""
+    def weights(scale=1.0, w=FAKE):
+        return lib.sr_loss_weights(FAKE, None, 10, None, 2, 3, 1, scale, w, None, FAKE, 1 << 20, None)
+
+    def policy(lp=FAKE, old=None, ref=None, adv=FAKE, w=FAKE, beta=0.0, loss=FAKE, d=None, stats=None):
+        return lib.sr_policy_loss(lp, old, ref, adv, w, FAKE, 3, None, 10, 0.2, 0.2, beta, loss, d, stats, FAKE, 1 << 20, None)
+
+    def step(lp=FAKE, old=None, ref=None, beta=0.0, stats=None, status=None):
+        return lib.sr_policy_loss_logits(FAKE, 0, 4, 100, 100, FAKE, old, ref, FAKE, FAKE, FAKE, 3, None, 0.2, 0.2, beta, 1.0, FAKE, lp, 2 * FAKE, 100, stats, status, FAKE, 1 << 20, None)
+
+    def logprob(lp=FAKE, st=None, H=None, status=None):
+        return lib.sr_token_logprob(FAKE, 0, 4, 100, 100, FAKE, 1.0, lp, st, H, status, None)
+
+    def backward(st=FAKE, H=FAKE, d=FAKE, dH=None):
+        return lib.sr_token_logprob_backward(FAKE, 0, 4, 100, 100, FAKE, st, H, d, dH, 1.0, 2 * FAKE, 100, None)
+
+    for bad in (1e39, -1e39):
+        assert weights(scale=bad) == sr.SR_ERR_BAD_VALUE
+    assert policy(beta=1e39) == sr.SR_ERR_BAD_VALUE and step(beta=1e39) == sr.SR_ERR_BAD_VALUE
+    odd = FAKE + 2
+    assert weights(w=odd) == sr.SR_ERR_ALIGN
+    for name in ("lp", "old", "ref", "adv", "w", "loss", "d", "stats"):
+        assert policy(**{name: odd}) == sr.SR_ERR_ALIGN, name
+    for name in ("lp", "old", "ref", "stats", "status"):
+        assert step(**{name: odd}) == sr.SR_ERR_ALIGN, name
+    for name in ("lp", "st", "H", "status"):
+        assert logprob(**{name: odd}) == sr.SR_ERR_ALIGN, name
+    for name in ("st", "H", "d", "dH"):
+        assert backward(**{name: odd}) == sr.SR_ERR_ALIGN, name
+    one = (ctypes.c_void_p * 1)(FAKE), (ctypes.c_int64 * 1)(10), (ctypes.c_int32 * 1)(0)
+    assert lib.sr_grad_norm(*one, 1, odd, FAKE, 1 << 20, None) == sr.SR_ERR_ALIGN
+    assert lib.sr_clip_grads(*one, 1, odd, 1.0, None, None, None) == sr.SR_ERR_ALIGN
+    assert lib.sr_clip_grads(*one, 1, 3 * FAKE, 1.0, None, odd, None) == sr.SR_ERR_ALIGN
+
+
 @pytest.mark.gpu
 def test_binding_refuses_tensors_of_another_type_or_size():
     d = torch.device("cuda:0")

@@ -75,10 +75,6 @@ struct TermSums {
             if (kEntropy) u[(k >> 1) & 1] = fma2(e, two(fmaxf(t0, -1000.0f), fmaxf(t1, -1000.0f)), u[(k >> 1) & 1]);
         }
     }
-    __device__ __forceinline__ void scale(float f) {
-        s[0] = mul2(s[0], two(f));
-        s[1] = mul2(s[1], two(f));
-    }
     static __device__ __forceinline__ double total(const f32x2 (&v)[2]) {
         const f32x2 both = add2(v[0], v[1]);
         return (double)(low_of(both) + high_of(both));
@@ -190,43 +186,65 @@ __device__ __forceinline__ uint4 all_minus_inf() {
     return make_uint4(w, w, w, w);
 }
 
-// Sums over the part of a row that thread `at` of `threads` has.  kAgain: it is read again soon, and may stay in L2.
-template <typename T, bool kEntropy, bool kAgain>
-__device__ __forceinline__ RowSums sum_row(const T* row, int vocab, int at, int threads, float c) {
-    constexpr int E = Vec<T>::kElems;
+// Takes the elements of N vectors.
+template <typename T, bool kEntropy, int N>
+__device__ __forceinline__ void take_vectors(const uint4 (&q)[N], float c, RowSums& r) {
+    VecMax<T> top(minus_inf());
+#pragma unroll
+    for (int k = 0; k < N; ++k) top.take(q[k]);
+    grow<kEntropy>(top.value(), c, r);
+    const float m = r.m == minus_inf() ? 0.0f : r.m;
+    TermSums<kEntropy> sums;
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+        float x[Vec<T>::kElems];
+        unpack_again(q[k], x, T());
+        sums.add(x, m, c);
+    }
+    sums.flush(r);
+}
+
+// Sums over the part of a row that thread `at` of `threads` has.  kThreads: their number where it is known, or 0.  kAgain: the row is
+// read again soon, and may stay in L2.
+template <typename T, bool kEntropy, bool kAgain, int kThreads>
+__device__ __forceinline__ RowSums sum_row(const T* row, int vocab, int at, int some_threads, float c) {
+    const int threads = kThreads ? kThreads : some_threads;
     const RowParts<T> parts(row, vocab);
     RowSums r = {minus_inf(), 0.0, 0.0};
     if (at < parts.head + parts.tail) take<kEntropy>(to_float(row[parts.single(at)]), c, r);
-    const uint4* body = reinterpret_cast<const uint4*>(row + parts.head);
-    uint4 next[kUnroll];                       // the batch after the one at hand is on its way while that is summed up
-    auto load = [&](long long v) {
+    // The batch after the one at hand is on its way while that is summed up.  Batches that are whole are told apart: looking at the
+    // end of the row for every vector takes a sixth of all instructions.
+    const uint4* body = reinterpret_cast<const uint4*>(row + parts.head) + at;
+    int left = parts.vecs - at;                // vectors from `body` on, this thread's at 0, threads, 2 threads, ...
+    const int step = threads * kUnroll, whole = step - threads;
+    uint4 next[kUnroll];
+    const auto load = [&](const uint4* from) {
 #pragma unroll
-        for (int k = 0; k < kUnroll; ++k) {
-            const long long i = v + (long long)k * threads;
-            next[k] = i >= parts.vecs ? all_minus_inf<T>() : kAgain ? body[i] : load_once(body + i);
-        }
+        for (int k = 0; k < kUnroll; ++k) next[k] = kAgain ? from[k * threads] : load_once(from + k * threads);
     };
-    const long long step = (long long)threads * kUnroll;
-    if (at < parts.vecs) load(at);
-    for (long long v = at; v < parts.vecs; v += step) {
+    const auto load_rest = [&](const uint4* from, int have) {
+#pragma unroll
+        for (int k = 0; k < kUnroll; ++k) next[k] = k * threads >= have ? all_minus_inf<T>() : kAgain ? from[k * threads] : load_once(from + k * threads);
+    };
+    const auto take_next = [&](auto load_more) {
         uint4 q[kUnroll];
 #pragma unroll
         for (int k = 0; k < kUnroll; ++k) q[k] = next[k];
-        if (v + step < parts.vecs) load(v + step);
-        VecMax<T> top(minus_inf());
-#pragma unroll
-        for (int k = 0; k < kUnroll; ++k) top.take(q[k]);
-        grow<kEntropy>(top.value(), c, r);
-        const float m = r.m == minus_inf() ? 0.0f : r.m;
-        TermSums<kEntropy> sums;
-#pragma unroll
-        for (int k = 0; k < kUnroll; ++k) {
-            float x[E];
-            unpack_again(q[k], x, T());
-            sums.add(x, m, c);
-        }
-        sums.flush(r);
+        load_more();
+        take_vectors<T, kEntropy>(q, c, r);
+        body += step;
+        left -= step;
+    };
+    if (left > whole) {
+        load(body);
+        while (left > step + whole) take_next([&] { load(body + step); });
+        take_next([&] {
+            if (left > step) load_rest(body + step, left - step);
+        });
+    } else if (left > 0) {
+        load_rest(body, left);
     }
+    if (left > 0) take_next([] {});
     return r;
 }
 
@@ -372,12 +390,13 @@ __device__ __forceinline__ bool counts_as_target(int32_t y, int vocab, int32_t* 
     return y >= 0 && y < vocab;
 }
 
-template <typename T, bool kEntropy>
+// kAlone: one CTA to a row.
+template <typename T, bool kEntropy, bool kAlone>
 __global__ void __launch_bounds__(kRowThreads, 4)
-token_logprob_kernel(const T* logits, int vocab, long long pitch, const int32_t* targets, double inv_temperature, float c, int ctas,
+token_logprob_kernel(const T* logits, int vocab, long long pitch, const int32_t* targets, double inv_temperature, float c, int some_ctas,
                      float* logp, float* row_stats, float* entropy, int32_t* status) {
     grid_begin();
-    const int t = blockIdx.x / ctas, part = blockIdx.x % ctas;
+    const int ctas = kAlone ? 1 : some_ctas, t = blockIdx.x / ctas, part = blockIdx.x % ctas;
     const int32_t y = targets[t];
     const bool first = part == 0 && threadIdx.x == 0;
     if (!counts_as_target(y, vocab, status, first)) {
@@ -390,7 +409,7 @@ token_logprob_kernel(const T* logits, int vocab, long long pitch, const int32_t*
     }
     const T* row = logits + (size_t)t * pitch;
     const float x_y = first ? to_float(row[y]) : 0.0f;        // on its way meanwhile
-    RowSums r = sum_row<T, kEntropy, false>(row, vocab, part * kRowThreads + threadIdx.x, ctas * kRowThreads, c);
+    RowSums r = sum_row<T, kEntropy, false, kAlone ? kRowThreads : 0>(row, vocab, part * kRowThreads + threadIdx.x, ctas * kRowThreads, c);
     r = combine<kEntropy>(r, c, ctas);
     if (first) {
         const double log_S = log_sum(r.s);
@@ -532,7 +551,7 @@ policy_loss_logits_kernel(PolicyBatch b, const T* logits, int vocab, long long p
     const int32_t y = targets[t];
     const float x_y = to_float(row[y]);                        // before anyone writes: d_logits may be the logits
     const PolicyToken token = threadIdx.x == 0 ? load_token(b, t, rollout) : PolicyToken{};      // on its way meanwhile
-    RowSums r = sum_row<T, false, true>(row, vocab, at, threads, c);
+    RowSums r = sum_row<T, false, true, 0>(row, vocab, at, threads, c);
     r = combine<false>(r, c, ctas);
     g = loss_gradient(b, token, t, x_y, y, r, inv_temperature, c, first, logp, terms);
     write_gradient<T, false, false>(row, out, vocab, at, threads, g);
@@ -821,27 +840,7 @@ ring_policy_loss_kernel(const __grid_constant__ PolicyBatch b, const T* logits, 
             const float x1 = single >= 0 ? to_float(row[single]) : minus_inf();
 
             RowSums r = {minus_inf(), 0.0, 0.0};
-            TermSums<false> sums;
             RingPlace at = place;
-            const auto add = [&](const uint4 (&v)[4]) {        // four vectors: one look at the maximum
-                VecMax<T> top(minus_inf());
-#pragma unroll
-                for (int j = 0; j < 4; ++j) top.take(v[j]);
-                if (top.value() > r.m) {
-                    const float f = exp2_approx((r.m - top.value()) * c);
-                    sums.scale(f);
-                    r.s *= (double)f;
-                    r.m = top.value();
-                }
-                const float m = r.m == minus_inf() ? 0.0f : r.m;
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    float x[E];
-                    unpack_again(v[j], x, T());
-                    sums.add(x, m, c);
-                }
-                sums.flush(r);
-            };
             int k = 0;
             for (; k + 2 <= whole; k += 2) {
                 uint4 v[4];
@@ -852,7 +851,7 @@ ring_policy_loss_kernel(const __grid_constant__ PolicyBatch b, const T* logits, 
                     v[2 * h + 1] = *reinterpret_cast<const uint4*>(from + at.slot * kChunk + kChunk / 2);
                     at.step();
                 }
-                add(v);
+                take_vectors<T, false>(v, c, r);
             }
             if (k < chunks) {                              // what is left: a whole chunk, the beginning of one, or both
                 uint4 v[4] = {all_minus_inf<T>(), all_minus_inf<T>(), all_minus_inf<T>(), all_minus_inf<T>()};
@@ -865,7 +864,7 @@ ring_policy_loss_kernel(const __grid_constant__ PolicyBatch b, const T* logits, 
                     if ((int)threadIdx.x + kRingThreads < have) v[2 * h + 1] = *reinterpret_cast<const uint4*>(from + at.slot * kChunk + kChunk / 2);
                     at.step();
                 }
-                add(v);
+                take_vectors<T, false>(v, c, r);
             }
             if (single >= 0) take<false>(x1, c, r);
             // every warp of the cluster leaves its sums with every CTA
@@ -1037,7 +1036,8 @@ int launch_forward(const LogitsArgs& a, float* logp, float* row_stats, float* en
                              1.0 / a.temperature, c, held.ctas, logp, row_stats, entropy, status);
         });
     const int ctas = ctas_of_row(a.n_tokens, a.vocab, (int)sizeof(T));
-    const auto kernel = entropy ? token_logprob_kernel<T, true> : token_logprob_kernel<T, false>;
+    const auto kernel = ctas == 1 ? (entropy ? token_logprob_kernel<T, true, true> : token_logprob_kernel<T, false, true>)
+                                  : (entropy ? token_logprob_kernel<T, true, false> : token_logprob_kernel<T, false, false>);
     return launch_as(true, ctas, "token_logprob_kernel", kernel, a.n_tokens * ctas, kRowThreads, 0, s, static_cast<const T*>(a.logits), a.vocab, (long long)a.pitch, a.targets,
                      1.0 / a.temperature, c, ctas, logp, row_stats, entropy, status);
 }

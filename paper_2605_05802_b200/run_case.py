@@ -9,7 +9,9 @@ Cases: c1, c2, c2x128 (65536 groups x N=8, K=15), c3 (4096 groups x N=16), c3x16
 (65536 groups), c4 (token level), c4s (256 groups), c4d (token level through sr_gate_decide at --threshold), c5 (streaming, --groups to
 shrink), adv (advantages, 4M groups), orr (OR rule, 4M groups), bstats (batch
 statistics, 4M groups), keep (kept-group index list, 4M groups), sig (Appendix-B
-signals, 65536 groups x N=16), packed (token level from packed host input, 256 groups).
+signals, 65536 groups x N=16), packed (token level from packed host input, 256 groups),
+train (the trainer's operators: bf16 logits of --tokens x 151936, losses of 8192
+rollouts, 300M bf16 gradients in 128 tensors).
 """
 from __future__ import annotations
 
@@ -28,6 +30,7 @@ def main():
     ap.add_argument("--reps", type=int, default=5)
     ap.add_argument("--groups", type=int, default=0)
     ap.add_argument("--threshold", type=float, default=0.3)
+    ap.add_argument("--tokens", type=int, default=1024)
     args = ap.parse_args()
     dev = torch.device("cuda:0")
     flush = torch.empty(256 << 20, dtype=torch.uint8, device=dev)
@@ -139,6 +142,39 @@ def main():
             timed(lambda: sr.sr_gate_host_packed(h_sym, h_rs, N, stride, w.K, w.threshold, w.norm_mode,
                                                  stop=h_stop, arena=arena))
         print(f"packed host input: {G} groups x N={N}: median {statistics.median(times):.1f} us")
+    elif args.case == "train":
+        f32 = dict(dtype=torch.float32, device=dev)
+        T, V, rows, length = args.tokens, 151936, 8192, 640
+        x = torch.randn(T, V, device=dev).mul_(2.0).to(torch.bfloat16)
+        y = torch.randint(0, V, (T,), dtype=torch.int32, device=dev)
+        lp, st, d, dx = torch.empty(T, **f32), torch.empty(T, 2, **f32), torch.randn(T, **f32), torch.empty_like(x)
+        start = torch.linspace(0, T, 9, device=dev).long()
+        one = torch.ones(8, **f32)
+        n = rows * length
+        starts = torch.arange(0, n + 1, length, dtype=torch.int64, device=dev)
+        mask = (torch.rand(n, device=dev) < 0.75).to(torch.uint8)
+        lps = -torch.rand(n, device=dev)
+        old, ref = lps + 0.1 * torch.randn(n, device=dev), lps + 0.2 * torch.randn(n, device=dev)
+        adv, weight, d_lps = torch.randn(rows, **f32), torch.empty(rows, **f32), torch.empty(n, **f32)
+        grads = list(torch.randn(128, 300_000_000 // 128 // 8 * 8, device=dev).mul_(1e-3).to(torch.bfloat16))
+        loss, norm = torch.empty(1, **f32), torch.empty(1, **f32)
+        ws = torch.empty(max(sr.sr_policy_loss_logits_workspace_bytes(T), sr.sr_policy_loss_workspace_bytes(n),
+                             sr.sr_loss_weights_workspace_bytes(rows), sr.sr_grad_norm_workspace_bytes(len(grads))),
+                         dtype=torch.uint8, device=dev)
+        ops = {"sr_token_logprob": lambda: sr.sr_token_logprob(x, y, logp=lp, row_stats=st),
+               "sr_token_logprob_backward": lambda: sr.sr_token_logprob_backward(x, y, st, None, d, None, d_logits=dx),
+               "sr_policy_loss_logits": lambda: sr.sr_policy_loss_logits(
+                   x, y, None, None, one, one, start, None, 0.2, 0.28, 0.0, loss=loss, logp=lp, d_logits=dx, workspace=ws),
+               "sr_loss_weights": lambda: sr.sr_loss_weights(starts, mask, None, 8, weight=weight, workspace=ws),
+               "sr_policy_loss": lambda: sr.sr_policy_loss(lps, old, ref, adv, weight, starts, mask, 0.2, 0.28, 0.02,
+                                                           loss=loss, d_logp=d_lps, workspace=ws),
+               "sr_grad_norm": lambda: sr.sr_grad_norm(grads, norm=norm, workspace=ws),
+               "sr_clip_grads": lambda: sr.sr_clip_grads(grads, norm, 1.0)}
+        for name, fn in ops.items():
+            times.clear()
+            for _ in range(args.reps):
+                timed(fn)
+            print(f"{name}: median {statistics.median(times):.1f} us")
     else:
         raise SystemExit(f"unknown case {args.case}")
 

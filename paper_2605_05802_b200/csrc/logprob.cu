@@ -887,10 +887,33 @@ ring_policy_loss_kernel(const __grid_constant__ PolicyBatch b, const T* logits, 
             g.k1 = 0.0f;
             g.target = y;
             uint4* to = reinterpret_cast<uint4*>(out + parts.head) + begin + threadIdx.x;
-            // the target's place among this thread's vectors: chunk and half
-            const int target_vec = y < parts.head ? -1 : (y - parts.head) / E - begin - (int)threadIdx.x;
-            for (k = 0; k < chunks; ++k, to += kChunkVecs) {
-                const int have = k < whole ? kChunkVecs : end - begin - k * kChunkVecs;
+            const auto write = [&](uint4 v, uint4* at) {
+                float x[E];
+                unpack(v, x, T());
+                gradients<false>(g, x);
+                store_once(at, pack(x, T()));
+            };
+            for (k = 0; k + 2 <= whole; k += 2, to += 2 * kChunkVecs) {
+                uint4 v[4];
+                RingPlace second = place;
+                second.step();
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    v[h] = *reinterpret_cast<const uint4*>(from + place.slot * kChunk + h * (kChunk / 2));
+                    v[2 + h] = *reinterpret_cast<const uint4*>(from + second.slot * kChunk + h * (kChunk / 2));
+                }
+                __syncwarp();
+                if (lane == 0) {
+                    barrier_arrive(&s_empty[place.slot]);
+                    barrier_arrive(&s_empty[second.slot]);
+                }
+                place = second;
+                place.step();
+#pragma unroll
+                for (int h = 0; h < 4; ++h) write(v[h], to + h * kRingThreads);
+            }
+            for (; k < chunks; ++k, to += kChunkVecs) {
+                const int have = end - begin - k * kChunkVecs;
                 uint4 v[2];
 #pragma unroll
                 for (int h = 0; h < 2; ++h) v[h] = *reinterpret_cast<const uint4*>(from + place.slot * kChunk + h * (kChunk / 2));   // behind the end: an older row's, not used
@@ -898,20 +921,12 @@ ring_policy_loss_kernel(const __grid_constant__ PolicyBatch b, const T* logits, 
                 if (lane == 0) barrier_arrive(&s_empty[place.slot]);
                 place.step();
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    if ((int)threadIdx.x + h * kRingThreads >= have) break;
-                    float x[E];
-                    unpack(v[h], x, T());
-                    gradients<false>(g, x);
-                    if (target_vec == k * kChunkVecs + h * kRingThreads) {
-                        const int at_j = (y - parts.head) % E;
-#pragma unroll
-                        for (int j = 0; j < E; ++j)
-                            if (j == at_j) x[j] += g.at_target;
-                    }
-                    store_once(to + h * kRingThreads, pack(x, T()));
-                }
+                for (int h = 0; h < 2; ++h)
+                    if ((int)threadIdx.x + h * kRingThreads < have) write(v[h], to + h * kRingThreads);
             }
+            // The target once more, by the thread that has just written it: looking for it in every vector costs more.
+            const int target_vec = y < parts.head ? -1 : (y - parts.head) / E - begin;
+            if (target_vec >= 0 && target_vec < end - begin && target_vec % kRingThreads == (int)threadIdx.x) out[y] = from_float<T>(gradient<false>(g, s_row[side].x_y) + g.at_target);
             if (single >= 0) {
                 float v = gradient<false>(g, x1);
                 if (single == y) v += g.at_target;

@@ -9,9 +9,14 @@
 // fp64, so that the many small terms beside a large one are not rounded off against it.  (x - M) is taken before the product
 // with c: rows masked with the type's lowest value would overflow the other way round.
 //
-// A CTA takes a row, or, where there are too few rows for the GPU, a cluster of CTAs does and their sums meet in shared
-// memory.  Loads are 16-byte vectors, four in flight a thread; elements before the first boundary of 16 bytes and behind the
-// last are taken one by one.
+// How a row is taken, by its length and by how many there are (held_row, ctas_of_row, ring_ctas):
+//   - up to 40 KB a CTA it is held in registers: all loads on their way together, nothing rescaled, and the loss writes the gradient
+//     from them (1200 rows of 4096 fp32: 11 us of a step's 18.7, 39 MB);
+//   - longer, it streams through the registers, a batch ahead (3072 rows of 151936 bf16: 152 to 163 us, 5.7 to 6.1 TB/s);
+//   - the loss, which needs it twice, holds it in the shared memory of a cluster (the ring below: 3072 such rows and 1024 of zeros
+//     405 us, 2.2 GB; from memory twice 536).
+// Where rows alone do not fill the GPU (fewer than two CTAs an SM), a cluster takes one and its sums meet in shared memory: 8 rows
+// of 151936 take 4.4 us.  Where they do, more CTAs a row cost more than the shorter last wave gives (4096 rows, two a row: 189 us).
 #include <cooperative_groups.h>
 #include <math_constants.h>
 
@@ -454,6 +459,7 @@ held_logprob_kernel(const T* logits, int vocab, long long pitch, const int32_t* 
     }
 }
 
+// Element by element: as many CTAs as there are, nobody waits (2048 rows of 151936 bf16, a quarter zeros: 176 us, 6.2 TB/s).
 template <typename T, bool kEntropy>
 __global__ void __launch_bounds__(kWriteThreads)
 token_logprob_backward_kernel(const T* logits, int vocab, long long pitch, const int32_t* targets, const float* row_stats,
@@ -528,6 +534,8 @@ __device__ __forceinline__ RowGradient loss_gradient(const PolicyBatch& b, const
     return g;
 }
 
+// Rows that are read twice: those that lie differently in logits and gradient, too long or too few for the ring, and batches of
+// more tokens than its list has.
 template <typename T>
 __global__ void __launch_bounds__(kRowThreads, 4)
 policy_loss_logits_kernel(PolicyBatch b, const T* logits, int vocab, long long pitch, const int32_t* targets, const int32_t* row_of,
@@ -595,7 +603,8 @@ held_policy_loss_kernel(PolicyBatch b, const T* logits, int vocab, long long pit
 // the cluster; one warp turns these into the row's gradient and finds out about the row to come; and the eight write the
 // gradient from the same chunks, each of which is then free for the next row.  CTAs stay and take row after row: the copies never
 // wait for the sums of a row, and two CTAs an SM take turns at computing and at waiting.
-// Read once, written once: bound by HBM; two exponentials an element come next (3/4 of their rate at that speed).
+// Read once, written once, but not at the rate of a copy (2048 rows of 32000 bf16 61 us, 4.3 TB/s; fp32 93, 5.6): 15 instructions an
+// element (55 % of the issue slots), two of them ex2 (65 % of its rate), and two microseconds a row in which its sums meet.
 constexpr int kRingThreads = 256, kRingWarps = kRingThreads / 32;
 constexpr int kChunkVecs = 2 * kRingThreads;       // two vectors a thread: with one, more instructions went into finding them than into the terms
 constexpr int kChunk = kChunkVecs * 16;            // bytes
@@ -770,8 +779,8 @@ ring_policy_loss_kernel(const __grid_constant__ PolicyBatch b, const T* logits, 
             if (!kAlone && lane == 0) barrier_expect(&s_met[side], (uint32_t)(sizeof(RingPart) * kRingWarps) * (uint32_t)ctas);
             look_ahead(turn + 1);              // on its way while this row is summed up
             barrier_wait(&s_met[side], (turn >> 1) & 1, gave_up);
-            // The cluster waits for k0 and at_target: they come from a short chain in fp32, log p to 2^-22; what is written down of
-            // the token is worked out afterwards.
+            // The cluster waits for k0 and at_target: they come from a short chain in fp32, log p to 2^-18 (lg2.approx is off by up to
+            // 2^-22 of a logarithm below 18); what is written down of the token is worked out afterwards, in fp64.
             constexpr int kParts = kAlone ? 1 : (kMaxCtas * kRingWarps + 31) / 32;
             RingPart part[kParts];
             float factor[kParts], M = minus_inf(), S32 = 0.0f;

@@ -175,58 +175,89 @@ __device__ __forceinline__ void leave_sum(PolicyTerms<double> sum, double beta, 
 __device__ __noinline__ float one_token(const PolicyBatch& b, float old_logp, float ref_logp, float adv, float weight, float lp, PolicyTerms<float>& out) {
     return policy_token(b, PolicyToken{old_logp, ref_logp, adv, weight}, lp, out);
 }
-// policy_token of four tokens side by side, without branches: one that does not count (bit 8 j of `counts`) has weight 0 and
-// policies that agree.  What needs another look (a ratio at a border of the clip range, numbers near overflow) gets it afterwards.
+// policy_token of four tokens side by side, two to an instruction and without branches: one that does not count (bit 8 j of
+// `counts`) has policies that agree.  Lanes that need another look (a ratio at a border of the clip range, numbers near overflow) take
+// their tokens one by one.  kOne: they lie in one rollout, w[0] and a[0] are its.
+template <bool kOne>
 __device__ __forceinline__ void four_tokens(const PolicyBatch& b, const float (&lp)[4], const float (&old_logp)[4], const float (&ref_logp)[4], const float (&w)[4],
                                             const float (&a)[4], uint32_t counts, float (&grad)[4], PolicyTerms<float>& sum) {
-    bool again = false;
-    float gain[4], kl[4], rho[4], past[4];
+    bool again = false, is[4], past[4];
+    float A[4], rho[4], gain[4], kl[4] = {0.0f, 0.0f, 0.0f, 0.0f}, delta[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-        const bool is = (counts >> (8 * j)) & 1u;
-        const float A = a[j], border = A > 0.0f ? b.high : b.low, side = A > 0.0f ? 1.0f : A < 0.0f ? -1.0f : 0.0f;
-        float delta = b.old_logp ? lp[j] - old_logp[j] : lp[j] - lp[j];          // a NaN stays one
-        if (!b.old_logp && isinf(lp[j])) delta = 0.0f;
-        delta = is ? delta : 0.0f;
-        rho[j] = expf(delta);
+        is[j] = (counts >> (8 * j)) & 1u;
+        A[j] = kOne ? a[0] : a[j];
+        rho[j] = is[j] && !(lp[j] == lp[j]) ? lp[j] : 1.0f;     // a NaN stays one
+    }
+    if (b.old_logp) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {          // off by 2^-22 and |delta| 2^-23 of itself, and 0 below 2^-126
+            if (is[j]) delta[j] = lp[j] - old_logp[j];
+            again |= delta[j] > 80.0f;
+            asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(rho[j]) : "f"(delta[j] * 1.44269504f));
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const float border = A[j] > 0.0f ? b.high : b.low, side = A[j] > 0.0f ? 1.0f : A[j] < 0.0f ? -1.0f : 0.0f;
         const float over = rho[j] - border;
-        past[j] = over * side > 0.0f ? 1.0f : 0.0f;
-        gain[j] = A * (over * side > 0.0f ? border : rho[j]);
-        grad[j] = over * side > 0.0f ? 0.0f : -gain[j];
-        kl[j] = 0.0f;
-        again |= is && (fabsf(over) <= 9.5367431640625e-7f * border || delta > 80.0f);
+        past[j] = over * side > 0.0f;
+        gain[j] = A[j] * (past[j] ? border : rho[j]);
+        grad[j] = past[j] ? 0.0f : -gain[j];
+        again |= is[j] && fabsf(over) <= ratio_margin(delta[j]) * border;
     }
     if (b.ref_logp) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const float d = (counts >> (8 * j)) & 1u ? ref_logp[j] - lp[j] : 0.0f;
-            float em1;
-            exp_less_line_near(d, em1, kl[j]);
-            grad[j] = fmaf(-b.beta32, em1, grad[j]);
-            again |= fabsf(d) > 80.0f;
+        for (int j = 0; j < 4; j += 2) {
+            const float d0 = is[j] ? ref_logp[j] - lp[j] : 0.0f, d1 = is[j + 1] ? ref_logp[j + 1] - lp[j + 1] : 0.0f;
+            again |= fabsf(d0) > 80.0f || fabsf(d1) > 80.0f;
+            f32x2 em1, both;
+            exp_less_line_near(two(d0, d1), em1, both);
+            kl[j] = low_of(both);
+            kl[j + 1] = high_of(both);
+            grad[j] = fmaf(-b.beta32, low_of(em1), grad[j]);
+            grad[j + 1] = fmaf(-b.beta32, high_of(em1), grad[j + 1]);
         }
-    }
-    PolicyTerms<float> term[4];
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        const bool is = (counts >> (8 * j)) & 1u;
-        const float weight = is ? w[j] : 0.0f;
-        term[j] = PolicyTerms<float>{weight * gain[j], weight * kl[j], weight * past[j], weight * rho[j]};
-        grad[j] = is ? weight * grad[j] : 0.0f;
     }
     if (again) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-            if ((counts >> (8 * j)) & 1u) grad[j] = one_token(b, old_logp[j], ref_logp[j], a[j], w[j], lp[j], term[j]);
+        for (int j = 0; j < 4; ++j) {
+            PolicyTerms<float> term = {0.0f, 0.0f, 0.0f, 0.0f};
+            grad[j] = is[j] ? one_token(b, old_logp[j], ref_logp[j], A[j], kOne ? w[0] : w[j], lp[j], term) : 0.0f;
+            sum.gain += term.gain;
+            sum.kl += term.kl;
+            sum.clipped += term.clipped;
+            sum.rho += term.rho;
+        }
+        return;
     }
-    sum.gain += (term[0].gain + term[1].gain) + (term[2].gain + term[3].gain);
-    sum.kl += (term[0].kl + term[1].kl) + (term[2].kl + term[3].kl);
-    sum.clipped += (term[0].clipped + term[1].clipped) + (term[2].clipped + term[3].clipped);
-    sum.rho += (term[0].rho + term[1].rho) + (term[2].rho + term[3].rho);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const float weight = kOne ? w[0] : w[j];
+        gain[j] = is[j] ? gain[j] : 0.0f;
+        rho[j] = is[j] ? rho[j] : 0.0f;
+        grad[j] = is[j] ? weight * grad[j] : 0.0f;
+    }
+    const auto of = [&](int j) { return is[j] && past[j] ? 1.0f : 0.0f; };
+    if (kOne) {
+        sum.gain = fmaf(w[0], (gain[0] + gain[1]) + (gain[2] + gain[3]), sum.gain);
+        sum.kl = fmaf(w[0], (kl[0] + kl[1]) + (kl[2] + kl[3]), sum.kl);
+        sum.clipped = fmaf(w[0], (of(0) + of(1)) + (of(2) + of(3)), sum.clipped);
+        sum.rho = fmaf(w[0], (rho[0] + rho[1]) + (rho[2] + rho[3]), sum.rho);
+    } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const float weight = is[j] ? w[j] : 0.0f;
+            sum.gain = fmaf(weight, gain[j], sum.gain);
+            sum.kl = fmaf(weight, kl[j], sum.kl);
+            sum.clipped = fmaf(weight, of(j), sum.clipped);
+            sum.rho = fmaf(weight, rho[j], sum.rho);
+        }
+    }
 }
 
-// kCluster: one launch, see leave_sum.  A warp has a run of tokens, 128 at a time; the next two lots are on their way while it works
-// on one.
+// kCluster: one launch, see leave_sum.  A warp has a run of tokens, 128 at a time; the next lot is on its way while it works on
+// one.
 template <bool kVec, bool kCluster>
 __global__ void __launch_bounds__(kCluster ? 512 : 256, kCluster ? 1 : 2)
 policy_loss_kernel(const __grid_constant__ PolicyBatch b, const float* logp, float* d_logp, int n, double* partial, float* loss,
@@ -243,7 +274,7 @@ policy_loss_kernel(const __grid_constant__ PolicyBatch b, const float* logp, flo
     struct Four {
         float lp[4], old_logp[4], ref_logp[4];
         uint32_t mask;
-    } next, later;
+    } next;
     auto load = [&](uint32_t t0) {
         Four next;
         if (kVec && t0 + 4 <= tokens) {
@@ -272,14 +303,12 @@ policy_loss_kernel(const __grid_constant__ PolicyBatch b, const float* logp, flo
         return next;
     };
     if (lot < end) next = load((lot << 7) + 4 * lane);
-    if (lot + 1 < end) later = load((lot << 7) + 128 + 4 * lane);
     RowWalk walk;
     if (lot < end && b.rows > 0) walk.find(b, lot << 7);
     for (; lot < end; ++lot) {
         const Four four = next;
-        next = later;
         const uint32_t w0 = lot << 7, t0 = w0 + 4 * lane;
-        if (lot + 2 < end) later = load(t0 + 256);
+        if (lot + 1 < end) next = load(t0 + 128);
         float grad[4] = {0.0f, 0.0f, 0.0f, 0.0f};
         if (b.rows > 0) {
             uint32_t counts = four.mask;
@@ -291,15 +320,13 @@ policy_loss_kernel(const __grid_constant__ PolicyBatch b, const float* logp, flo
             counts = __vminu4(counts, 0x01010101u);
             float w[4], a[4];
             if (walk.one_rollout(w0, w[0], a[0])) {
-                w[1] = w[2] = w[3] = w[0];
-                a[1] = a[2] = a[3] = a[0];
-                if (w[0] != 0.0f) four_tokens(b, four.lp, four.old_logp, four.ref_logp, w, a, counts, grad, mine);
+                if (w[0] != 0.0f) four_tokens<true>(b, four.lp, four.old_logp, four.ref_logp, w, a, counts, grad, mine);
             } else {
                 walk.several_rollouts(w0, t0, w, a);
 #pragma unroll
                 for (int j = 0; j < 4; ++j)
                     if (w[j] == 0.0f) counts &= ~(1u << (8 * j));
-                four_tokens(b, four.lp, four.old_logp, four.ref_logp, w, a, counts, grad, mine);
+                four_tokens<false>(b, four.lp, four.old_logp, four.ref_logp, w, a, counts, grad, mine);
             }
         }
         if ((lot & 3u) == 3u || lot + 1 == end) {        // fp32 over up to 16 tokens, fp64 from there on

@@ -61,6 +61,8 @@ struct RowWalk {
     float weight, adv;               // its
     uint32_t lane_start;             // of rollout base + 1 + lane; none: never reached
     float lane_weight, lane_adv;
+    uint32_t until;                  // the rollout at hand goes on up to there: its
+    float here_weight, here_adv;
 
     // Tokens are fewer than 2^31: where a start lies before or behind them all is enough.
     static __device__ __forceinline__ uint32_t place(long long start) { return (uint32_t)min(max(start, 0LL), 0xFFFFFFFFLL); }
@@ -73,6 +75,7 @@ struct RowWalk {
         lane_adv = lane_weight != 0.0f ? b->adv[at] : 0.0f;      // what a rollout without weight has is not used
         weight = b->weight[row];
         adv = weight != 0.0f ? b->adv[row] : 0.0f;
+        until = 0;
     }
     __device__ __forceinline__ void find(const PolicyBatch& batch, uint32_t first) {
         b = &batch;
@@ -83,6 +86,9 @@ struct RowWalk {
     // Whether the 128 tokens from w0 on lie in one rollout (or before the first, or behind the last); then w and a are its weight
     // and advantage.
     __device__ __forceinline__ bool one_rollout(uint32_t w0, float& w, float& a) {
+        w = here_weight;
+        a = here_adv;
+        if (w0 + 127 < until) return true;
         unsigned in = __ballot_sync(0xFFFFFFFFu, lane_start <= w0 + 127);
         if (in == 0xFFFFFFFFu) {                                 // more starts than the lanes hold: move on to the rollout of w0
             const int passed = __popc(__ballot_sync(0xFFFFFFFFu, lane_start <= w0));
@@ -97,6 +103,9 @@ struct RowWalk {
             w = weight;
             a = adv;
         }
+        here_weight = w;
+        here_adv = a;
+        until = last < 31 ? __shfl_sync(0xFFFFFFFFu, lane_start, last + 1) : 0;
         return passed == in;
     }
     // Weight and advantage of this lane's tokens t0 .. t0 + 3 where the 128 from w0 on lie in several.
@@ -136,29 +145,39 @@ static __device__ __noinline__ float far_expm1(float d) { return expm1f(d); }   
 // (e^r - 1 - r) / r^2, cut where the next term is below 2^-27 of the sum; then
 //     e^d - 1 - d = 2^n q + (2^n r + (2^n - 1) - d),
 // whose second part is exactly 0 for n = 0: policies that nearly agree lose nothing.
-// For |d| <= 80.
-__device__ __forceinline__ void exp_less_line_near(float d, float& em1, float& kl) {
-    const float n = rintf(d * 1.44269504f);
-    float r = fmaf(n, -0.693359375f, d);           // ln 2 in two parts, the first with few bits: this product is exact
-    r = fmaf(n, 2.12194440054690583e-4f, r);
-    float g = 1.0f / 40320.0f;
-    g = fmaf(g, r, 1.0f / 5040.0f);
-    g = fmaf(g, r, 1.0f / 720.0f);
-    g = fmaf(g, r, 1.0f / 120.0f);
-    g = fmaf(g, r, 1.0f / 24.0f);
-    g = fmaf(g, r, 1.0f / 6.0f);
-    g = fmaf(g, r, 0.5f);
-    const float q = g * r * r;
-    const float s = __int_as_float(((int)n + 127) << 23);       // 2^n
-    kl = fmaf(s, q, (fmaf(s, r, s - 1.0f)) - d);
-    em1 = fmaf(s, r + q, s - 1.0f);
+// For |d| <= 80, two numbers at a time: 2^n, r and q.
+__device__ __forceinline__ void exp_parts(f32x2 d, f32x2& s, f32x2& r, f32x2& q) {
+    const f32x2 z = fma2(d, two(1.44269504f), two(12582912.0f));           // 1.5 * 2^23: n stands in the lowest bits
+    const f32x2 n = add2(z, two(-12582912.0f));
+    r = fma2(n, two(-0.693359375f), d);            // ln 2 in two parts, the first with few bits: this product is exact
+    r = fma2(n, two(2.12194440054690583e-4f), r);
+    f32x2 g = two(1.0f / 40320.0f);
+    g = fma2(g, r, two(1.0f / 5040.0f));
+    g = fma2(g, r, two(1.0f / 720.0f));
+    g = fma2(g, r, two(1.0f / 120.0f));
+    g = fma2(g, r, two(1.0f / 24.0f));
+    g = fma2(g, r, two(1.0f / 6.0f));
+    g = fma2(g, r, two(0.5f));
+    q = mul2(mul2(g, r), r);
+    const auto power = [](float z) { return __uint_as_float((__float_as_uint(z) << 23) + 0x3F800000u); };
+    s = two(power(low_of(z)), power(high_of(z)));
+}
+__device__ __forceinline__ void exp_less_line_near(f32x2 d, f32x2& em1, f32x2& kl) {
+    f32x2 s, r, q;
+    exp_parts(d, s, r, q);
+    const f32x2 less = add2(s, two(-1.0f));
+    kl = fma2(s, q, fma2(d, two(-1.0f), fma2(s, r, less)));
+    em1 = fma2(s, add2(r, q), less);
 }
 __device__ __forceinline__ void exp_less_line(float d, float& em1, float& kl) {
     if (fabsf(d) > 80.0f) {                        // 2^n r may overflow before the sum does
         em1 = far_expm1(d);
         kl = em1 - d;
     } else {
-        exp_less_line_near(d, em1, kl);
+        f32x2 em1_2, kl_2;
+        exp_less_line_near(two(d, 0.0f), em1_2, kl_2);
+        em1 = low_of(em1_2);
+        kl = low_of(kl_2);
     }
 }
 
@@ -166,7 +185,9 @@ __device__ __forceinline__ void exp_less_line(float d, float& em1, float& kl) {
 // where it has just been computed.
 //
 // Whether rho is past a border of the clip range would be lost in 32 bits (and a token on the wrong side has a wholly wrong
-// gradient): rho in fp32 is off by up to 2^-22 of itself, so within 2^-20 of a border the comparison is made again in fp64.
+// gradient): rho in fp32 is off by up to 2^-22 and |log rho| 2^-23 of itself, so within four and two times that of a border the
+// comparison is made again in fp64.
+__device__ __forceinline__ float ratio_margin(float delta) { return fmaf(fabsf(delta), 2.384185791015625e-7f, 9.5367431640625e-7f); }
 static __device__ __noinline__ double exact_ratio(double lp, double old_logp) { return exp(lp - old_logp); }      // rare as well
 template <typename F>
 __device__ __forceinline__ float policy_token(const PolicyBatch& b, const PolicyToken& k, F lp, PolicyTerms<float>& out) {
@@ -175,10 +196,10 @@ __device__ __forceinline__ float policy_token(const PolicyBatch& b, const Policy
     const float border = A > 0.0f ? b.high : b.low;
     bool clipped = false;
     if (b.old_logp) {
-        const F delta = lp - (F)k.old_logp;
-        rho = expf((float)delta);
+        const float delta = (float)(lp - (F)k.old_logp);
+        rho = expf(delta);
         clipped = A > 0.0f ? rho > border : A < 0.0f && rho < border;
-        if (fabsf(rho - border) <= 9.5367431640625e-7f * border) {
+        if (fabsf(rho - border) <= ratio_margin(delta) * border) {
             const double exact = exact_ratio((double)lp, (double)k.old_logp);
             clipped = A > 0.0f ? exact > 1.0 + b.clip_high : A < 0.0f && exact < 1.0 - b.clip_low;
         }

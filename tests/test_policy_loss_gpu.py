@@ -163,6 +163,18 @@ def test_borders_of_the_clip_range():
     assert loss == 0.0 and not d.any()
 
 
+@pytest.mark.parametrize("hi", [3.0, 2e5, 1e20])
+def test_borders_of_wide_clip_ranges(hi):
+    """Steps of log rho are steps of rho many times larger there, and so are errors."""
+    x = np.float32(np.log1p(hi))
+    lp = np.array([x + np.float32(k) * np.spacing(x) for k in range(-64, 65)], dtype=np.float32)
+    n = lp.size
+    b = dict(lp=lp, old=np.zeros(n, np.float32), ref=None, adv=np.full(1, 1.5, np.float32), weight=np.ones(1, np.float32), row_start=np.array([0, n], np.int64))
+    check_policy(b, None, 0.2, hi, 0.0)
+    far = dict(b, lp=lp - np.float32(20.0), old=np.full(n, -20.0, np.float32))          # the same ratios, rounded elsewhere
+    check_policy(far, None, 0.2, hi, 0.0)
+
+
 def test_kl_of_policies_that_nearly_agree_and_far_apart():
     d = np.concatenate([np.logspace(-7, 1.5, 400), -np.logspace(-7, 1.5, 400), [0.0, 0.5, -0.5, 0.49999997]]).astype(np.float32)
     lp = np.full(d.size, -1.0, np.float32)

@@ -9,7 +9,9 @@
  *
  * Conventions are those of sr_gate.h: DEVICE pointers, every buffer the caller's, work enqueued
  * on `stream`, checks made before anything is enqueued.  Buffers of a call do not overlap
- * unless it says so.  All of them belong to the current device.
+ * unless it says so.  All of them belong to the current device.  A workspace serves one call at a
+ * time: calls that follow one another on a stream may share it, calls and captured graphs that may
+ * overlap need one each.
  *
  * Logits are [n_tokens][vocab] of type `dtype` (SR_DTYPE_*), row t starting at element
  * t * pitch, pitch >= vocab; rows need no alignment beyond that of an element (16 bytes are

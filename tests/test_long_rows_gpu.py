@@ -60,6 +60,15 @@ def test_hardly_anything_counts(T, V, counting, dtype):
         assert float(got[0]) == 0.0 and not bool(got[3].any())
 
 
+@pytest.mark.parametrize("T,V", [(4, 300), (50, 21000), (400, 21000), (400, 50021)])
+def test_no_rollouts(T, V):
+    """Tokens, but no rollout that they could belong to."""
+    x, y = logits(T, V, "bf16", T)
+    b = dict(old=None, ref=None, adv=np.zeros(0, np.float32), weight=np.zeros(0, np.float32), row_start=np.zeros(1, np.int64))
+    loss, lp, dx, stats, status = step(x, y, b, None, 1.0, 0.0)
+    assert float(loss) == 0.0 and not bool(lp.any()) and not bool(dx.any()) and not bool(stats.any()) and status == 0
+
+
 @pytest.mark.parametrize("T", [1025, 2049, 2500, 4100, 7000])
 def test_batches_of_the_helper_kernels_sizes(T):
     """Lists and sums of clusters of two to eight CTAs, and a list of several sweeps."""

@@ -12,8 +12,8 @@
 // How a row is taken, by its length and by how many there are (held_row, ctas_of_row, ring_ctas):
 //   - up to 40 KB a CTA it is held in registers: all loads on their way together, nothing rescaled, and the loss writes the gradient
 //     from them (1200 rows of 4096 fp32: 11 us of a step's 18.7, 39 MB);
-//   - longer, it streams through the registers, a batch ahead (3072 rows of 151936 bf16: 152 to 163 us, 5.7 to 6.1 TB/s);
-//   - the loss, which needs it twice, holds it in the shared memory of a cluster (the ring below: 3072 such rows and 1024 of zeros
+//   - longer, it streams through the registers, a batch ahead (4096 rows of 151936 bf16, a quarter masked: 152 to 163 us, 5.7 to 6.1 TB/s);
+//   - the loss, which needs it twice, holds it in the shared memory of a cluster (the ring below: the same rows and zeros for those masked
 //     405 us, 2.2 GB; from memory twice 536).
 // Where rows alone do not fill the GPU (fewer than two CTAs an SM), a cluster takes one and its sums meet in shared memory: 8 rows
 // of 151936 take 4.4 us.  Where they do, more CTAs a row cost more than the shorter last wave gives (4096 rows, two a row: 189 us).
@@ -26,7 +26,7 @@
 namespace sr {
 namespace {
 
-constexpr int kRowThreads = 256;          // sums: rows of CTAs that end at other times fill each other's gaps (512 threads, 3072 rows of 151936 bf16: 188 us, 256: 173)
+constexpr int kRowThreads = 256;          // sums: rows of CTAs that end at other times fill each other's gaps (512 threads, 4096 rows of 151936 bf16, a quarter masked: 188 us, 256: 173)
 constexpr int kWriteThreads = 512;        // gradients alone: nobody waits for anybody (256 threads, 2048 such rows: 181 us, 512: 175)
 constexpr int kUnroll = 4;
 constexpr int kHeldThreads = 256, kMostVecs = 10;
@@ -1018,7 +1018,7 @@ token_list_kernel(const __grid_constant__ PolicyBatch b, const int32_t* targets,
 }
 
 // How a row is held: CTAs to a row and vectors a thread, or no way to.  One CTA, or, where the rows alone do not fill the GPU, a
-// cluster as long as each thread still has a vector.
+// cluster as long as each thread still has a vector.  More vectors than ten a thread leave too few CTAs an SM.
 struct Held {
     int ctas, vecs;
 };
@@ -1082,13 +1082,15 @@ bool alike(const LogitsArgs& a, const void* d_logits, int64_t d_pitch) {
     return (apart & 15) == 0 && (a.n_tokens == 1 || ((a.pitch - d_pitch) * dtype_bytes(a.dtype)) % 16 == 0);
 }
 
-// CTAs to a row of the ring kernel, or 0: rows too long for it, too short to be worth it, or too few to keep its CTAs busy.
+// CTAs to a row of the ring kernel, or 0: rows too long for it, short enough to be held in registers, or too few for its CTAs, which
+// stay.  Held, 1200 rows of 20000 bf16 take 31 us, through the ring 36.  160 rows of 50021 in clusters of two are a row and a bit for
+// each: 23 us, and 20 from memory twice; 300 of them 27, and 31.
 int ring_ctas(int n_tokens, int vocab, int elem) {
     const long long vecs = ((long long)vocab * elem + 15) / 16;
     if (n_tokens > kListTokens || vecs <= kHeldThreads * kMostVecs) return 0;
     int ctas = 1;
     while (ctas < kMaxCtas && vecs > (long long)ctas * kChunkVecs * kRingRow) ctas *= 2;
-    return vecs > (long long)ctas * kChunkVecs * kRingRow || (long long)n_tokens * ctas < 2 * 148 ? 0 : ctas;
+    return vecs > (long long)ctas * kChunkVecs * kRingRow || (long long)n_tokens * ctas < 3 * 148 ? 0 : ctas;
 }
 template <typename T>
 int launch_ring(const LogitsArgs& a, const PolicyBatch& b, const StepScratch& ws, int ctas, float* logp, void* d_logits, int64_t d_pitch, int32_t* status, cudaStream_t s) {

@@ -42,7 +42,7 @@ def check(x, y, b, mask, got, beta, rows):
 
 
 @pytest.mark.parametrize("dtype", list(DTYPES))
-@pytest.mark.parametrize("T,V", [(400, 21000), (300, 50021), (200, 151936)])
+@pytest.mark.parametrize("T,V", [(400, 21000), (600, 21000), (300, 50021), (200, 151936)])
 @pytest.mark.parametrize("counting", [0, 1, 3])
 def test_hardly_anything_counts(T, V, counting, dtype):
     x, y = logits(T, V, dtype, T)
@@ -60,7 +60,7 @@ def test_hardly_anything_counts(T, V, counting, dtype):
         assert float(got[0]) == 0.0 and not bool(got[3].any())
 
 
-@pytest.mark.parametrize("T,V", [(4, 300), (50, 21000), (400, 21000), (400, 50021)])
+@pytest.mark.parametrize("T,V", [(4, 300), (50, 21000), (400, 21000), (600, 21000), (400, 50021)])
 def test_no_rollouts(T, V):
     """Tokens, but no rollout that they could belong to."""
     x, y = logits(T, V, "bf16", T)

@@ -573,8 +573,10 @@ policy_loss_logits_kernel(PolicyBatch b, const T* logits, int vocab, long long p
     write_gradient<T, false, false>(row, out, vocab, at, threads, g);
 }
 
+// Bound by how many rows are under way: one takes 4 to 5 us from its CTA's start to its end.  Seven CTAs an SM for one or two vectors a
+// thread (16384 rows of 4096 bf16: 96 us, with five 114); for four vectors six gain 3 % where rows are thousands and lose as much at 1200.
 template <typename T, int kVecs, bool kAlone>
-__global__ void __launch_bounds__(kHeldThreads, kVecs > 7 ? 3 : kVecs > 4 ? 4 : 5)
+__global__ void __launch_bounds__(kHeldThreads, kVecs > 7 ? 3 : kVecs > 4 ? 4 : kVecs > 2 ? 5 : 7)
 held_policy_loss_kernel(PolicyBatch b, const T* logits, int vocab, long long pitch, const int32_t* targets, const int32_t* row_of,
                         double inv_temperature, float c, int some_ctas, float* logp, PolicyTerms<float>* terms, T* d_logits, long long d_pitch) {
     grid_begin();

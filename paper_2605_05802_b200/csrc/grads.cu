@@ -3,8 +3,9 @@
 // The list travels as a kernel argument: no copy to the device, nothing to keep between calls, and a captured call holds its
 // own.  Tensors are cut into pieces of 16 KB and the pieces dealt out evenly, as runs, to a grid that fills the GPU; a CTA
 // searches the tensor of its first piece and walks on from there.  Both kernels are bound by HBM: the norm reads every
-// gradient once, clipping reads and writes it (the factor is known only when all squares are added up).  1.9 GB of bf16: 890 us for
-// both, 6.35 TB/s (pieces of 32 KB: 905); 392 small fp32 tensors, 65 MB: 41 us, 16 + 5 + 23 by kernel.
+// gradient once, clipping reads and writes it (the factor is known only when all squares are added up).  1.9 GB of bf16: 885 us for
+// both, 6.4 TB/s (pieces of 32 KB: 900); 392 small fp32 tensors, 65 MB: 38 us.  Loads of the norm leave in L2 what fits: clipping
+// finds it there (with loads that do not, 41 us).
 //
 // Squares of 32 bytes a thread are added in fp32, and such sums in fp64.  Where a sum of squares leaves the range
 // in which fp32 squares keep their digits (gradients around 2^60 and above, or 2^-50 and below), its elements are squared
@@ -81,7 +82,7 @@ __device__ __forceinline__ double piece_square_sum(const T* p, int n) {
 #pragma unroll
     for (int k = 0; k < kVecsInFlight; ++k) {
         const int i = threadIdx.x + k * kGradThreads;
-        q[k] = i < vecs ? load_once(body + i) : make_uint4(0u, 0u, 0u, 0u);
+        q[k] = i < vecs ? body[i] : make_uint4(0u, 0u, 0u, 0u);
     }
 #pragma unroll
     for (int k = 0; k < kVecsInFlight; k += 2) {

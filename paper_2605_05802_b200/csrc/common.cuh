@@ -110,6 +110,12 @@ __device__ __forceinline__ void grid_begin() {
     asm volatile("griddepcontrol.wait;" ::: "memory");
 }
 
+// A CTA may touch another's shared memory only once that one has started: all threads of a cluster's CTAs arrive at the beginning of
+// the kernel, and wait before the first access.  What lies in between hides the barrier.  Either all of a cluster's threads do both
+// or none does.  (Not the .aligned forms: a warp's lanes may come here apart, from a branch of one thread.)
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.relaxed;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire;" ::: "memory"); }
+
 struct GateArgs {
     const int32_t* seqs;
     const int32_t* lens;

@@ -141,7 +141,8 @@ __device__ __forceinline__ RowSums warp_sum(RowSums r, float c) {
     }
     return r;
 }
-// Sums of all threads' parts (up to eight warps), in every thread; over the cluster where it has several CTAs.
+// Sums of all threads' parts (up to eight warps), in every thread; over the cluster where it has several CTAs, whose threads have
+// arrived at its barrier.
 template <bool kEntropy>
 __device__ __forceinline__ RowSums combine(RowSums r, float c, int ctas) {
     static_assert(kMaxCtas == 8 && kRowThreads <= 256 && kHeldThreads <= 256, "eight parts of the later sums");
@@ -155,6 +156,7 @@ __device__ __forceinline__ RowSums combine(RowSums r, float c, int ctas) {
     if (ctas > 1) {
         // every CTA writes its sums to all the others: after the barrier each reads its own memory, and may leave
         const auto cluster = cooperative_groups::this_cluster();
+        cluster_wait();
         if ((int)threadIdx.x < ctas) *cluster.map_shared_rank(&s_cta[cluster.block_rank()], threadIdx.x) = r;
         cluster.sync();
         r = warp_sum<kEntropy, 8>(lane < ctas ? s_cta[lane] : none, c);
@@ -419,6 +421,7 @@ token_logprob_kernel(const T* logits, int vocab, long long pitch, const int32_t*
         }
         return;
     }
+    if (!kAlone) cluster_arrive();
     const T* row = logits + (size_t)t * pitch;
     const float x_y = first ? to_float(row[y]) : 0.0f;        // on its way meanwhile
     RowSums r = sum_row<T, kEntropy, false, kAlone ? kRowThreads : 0>(row, vocab, part * kRowThreads + threadIdx.x, ctas * kRowThreads, c);
@@ -451,6 +454,7 @@ held_logprob_kernel(const T* logits, int vocab, long long pitch, const int32_t* 
         }
         return;
     }
+    if (!kAlone) cluster_arrive();
     const T* row = logits + (size_t)t * pitch;
     HeldRow<T, kVecs> held;
     held.template load<kAlone>(row, RowParts<T>(row, vocab), part * kHeldThreads + threadIdx.x, ctas * kHeldThreads);
@@ -563,6 +567,7 @@ policy_loss_logits_kernel(PolicyBatch b, const T* logits, int vocab, long long p
         }
         return;
     }
+    if (ctas > 1) cluster_arrive();
     const T* row = logits + (size_t)t * pitch;
     const int32_t y = targets[t];
     const float x_y = to_float(row[y]);                        // before anyone writes: d_logits may be the logits
@@ -593,6 +598,7 @@ held_policy_loss_kernel(PolicyBatch b, const T* logits, int vocab, long long pit
         }
         return;
     }
+    if (!kAlone) cluster_arrive();
     const T* row = logits + (size_t)t * pitch;
     const RowParts<T> parts(row, vocab);
     HeldRow<T, kVecs> held;
@@ -964,6 +970,7 @@ constexpr int kListThreads = 1024, kListTokens = 65536;
 __global__ void __launch_bounds__(kListThreads)
 token_list_kernel(const __grid_constant__ PolicyBatch b, const int32_t* targets, int vocab, int n, int4* list, int32_t* counters, float* logp, PolicyTerms<float>* terms, int32_t* status) {
     grid_begin();
+    cluster_arrive();
     __shared__ int s_warp[32], s_cta[8];
     const auto cluster = cooperative_groups::this_cluster();
     const int ctas = gridDim.x, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -992,6 +999,7 @@ token_list_kernel(const __grid_constant__ PolicyBatch b, const int32_t* targets,
     }
     if (lane == 0) s_warp[warp] = mine;
     __syncthreads();
+    cluster_wait();
     if (warp == 0) {
         const int total = __reduce_add_sync(0xFFFFFFFFu, s_warp[lane]);
         if (lane < ctas) *cluster.map_shared_rank(&s_cta[blockIdx.x], lane) = total;

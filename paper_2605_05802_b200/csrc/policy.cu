@@ -98,6 +98,7 @@ __global__ void __launch_bounds__(kWeightThreads)
 loss_weights_kernel(const int64_t* row_start, const uint8_t* mask, int n_tokens, const int32_t* tokens,
                     const uint8_t* drop_mask, int N, int rows, int mode, double scale, float* weight, int64_t* counts) {
     grid_begin();
+    cluster_arrive();
     __shared__ long long s_tokens[32], s_total[8];
     __shared__ int s_live[32], s_rows[8];
     __shared__ int32_t s_count[kCount ? kRowsOfCta : 1];
@@ -128,6 +129,7 @@ loss_weights_kernel(const int64_t* row_start, const uint8_t* mask, int n_tokens,
     live = __reduce_add_sync(0xFFFFFFFFu, live);
     if (lane == 0) { s_tokens[warp] = sum; s_live[warp] = live; }
     __syncthreads();
+    cluster_wait();
     if (warp == 0) {
         sum = lane < warps ? s_tokens[lane] : 0;
         live = __reduce_add_sync(0xFFFFFFFFu, lane < warps ? s_live[lane] : 0);
@@ -154,7 +156,7 @@ loss_weights_kernel(const int64_t* row_start, const uint8_t* mask, int n_tokens,
 }
 
 // What thread 0 of every CTA does with its sum.  kCluster: the grid is one cluster, whose sums meet in shared memory and become
-// the loss.
+// the loss; its threads have arrived at the cluster's barrier.
 template <bool kCluster>
 __device__ __forceinline__ void leave_sum(PolicyTerms<double> sum, double beta, double* partial, float* loss, float* stats) {
     if (!kCluster) {
@@ -163,6 +165,7 @@ __device__ __forceinline__ void leave_sum(PolicyTerms<double> sum, double beta, 
     }
     __shared__ PolicyTerms<double> s_sum[8];
     const auto cluster = cooperative_groups::this_cluster();
+    cluster_wait();
     if (threadIdx.x == 0) *cluster.map_shared_rank(&s_sum[blockIdx.x], 0) = sum;
     cluster.sync();                        // the first CTA's memory alone is read after it
     if (blockIdx.x == 0 && threadIdx.x == 0) {
@@ -263,6 +266,7 @@ __global__ void __launch_bounds__(kCluster ? 512 : 256, kCluster ? 1 : 2)
 policy_loss_kernel(const __grid_constant__ PolicyBatch b, const float* logp, float* d_logp, int n, double* partial, float* loss,
                    float* stats) {
     grid_begin();
+    if (kCluster) cluster_arrive();
     const int lane = threadIdx.x & 31, warps = blockDim.x >> 5;
     const int all = gridDim.x * warps, warp = blockIdx.x * warps + (threadIdx.x >> 5);
     const uint32_t tokens = (uint32_t)n;                       // token numbers are unsigned: the last lot may end behind 2^31
@@ -354,6 +358,7 @@ template <typename F, bool kCluster>
 __global__ void __launch_bounds__(1024)
 sum_terms_kernel(const PolicyTerms<F>* terms, int n, double beta, double* partial, float* loss, float* stats) {
     grid_begin();
+    if (kCluster) cluster_arrive();
     PolicyTerms<double> sum = {0.0, 0.0, 0.0, 0.0};
 #pragma unroll 4
     for (long long i = (long long)blockIdx.x * blockDim.x + threadIdx.x; i < n; i += (long long)gridDim.x * blockDim.x) {

@@ -795,57 +795,44 @@ ring_policy_loss_kernel(const __grid_constant__ PolicyBatch b, const T* logits, 
             if (!kAlone && lane == 0) barrier_expect(&s_met[side], (uint32_t)(sizeof(RingPart) * kRingWarps) * (uint32_t)ctas);
             look_ahead(turn + 1);              // on its way while this row is summed up
             barrier_wait(&s_met[side], (turn >> 1) & 1, gave_up);
-            // The cluster waits for k0 and at_target: they come from a short chain in fp32, log p to 2^-18 (lg2.approx is off by up to
-            // 2^-22 of a logarithm below 18); what is written down of the token is worked out afterwards, in fp64.
+            // The cluster waits for k0 and at_target.  They come from the log p in fp64 that is written down of the token: every CTA
+            // works it out alike, and gradient and figures take the same side of the clip range.
             constexpr int kParts = kAlone ? 1 : (kMaxCtas * kRingWarps + 31) / 32;
+            const int parts = kRingWarps << log_ctas;          // fewer than the lanes: several have the same one, and sum them up in fewer steps
             RingPart part[kParts];
-            float factor[kParts], M = minus_inf(), S32 = 0.0f;
+            float M = minus_inf();
+            double S = 0.0;
 #pragma unroll
             for (int k = 0; k < kParts; ++k) {
-                part[k] = lane + 32 * k < ctas * kRingWarps ? s_part[side][lane + 32 * k] : RingPart{0.0, minus_inf(), 0.0f};
+                part[k] = 32 * k < parts ? s_part[side][(lane & (parts - 1)) + 32 * k] : RingPart{0.0, minus_inf(), 0.0f};
                 M = fmaxf(M, part[k].m);
             }
             M = warp_max(M);
 #pragma unroll
-            for (int k = 0; k < kParts; ++k) {
-                factor[k] = part[k].m == M ? 1.0f : exp2_approx((part[k].m - M) * c);
-                S32 = fmaf((float)part[k].s, factor[k], S32);
-            }
+            for (int k = 0; k < kParts; ++k) S += part[k].s * (double)(part[k].m == M ? 1.0f : exp2_approx((part[k].m - M) * c));
 #pragma unroll
-            for (int off = 16; off > 0; off >>= 1) S32 += __shfl_xor_sync(0xFFFFFFFFu, S32, off);
-            if (M == minus_inf()) S32 = CUDART_NAN_F;  // no token can occur: there is no distribution
-            float log2_S;
-            asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(log2_S) : "f"(S32));
+            for (int off = 16; off > 0; off >>= 1)
+                if (off < parts) S += __shfl_xor_sync(0xFFFFFFFFu, S, off);
+            if (M == minus_inf()) S = CUDART_NAN;      // no token can occur: there is no distribution
+            const double lp = ((double)x_y - (double)M) * inv_temperature - log_sum(S);
             PolicyTerms<float> term;
-            const float d = policy_token(b, token, fmaf(x_y - M, (float)inv_temperature, -(float)kLn2 * log2_S), term) * (float)inv_temperature;
+            const float d = policy_token(b, token, lp, term) * (float)inv_temperature;
             if (lane == 0) {
                 RowGradient& g = s_gradient[side];
                 g.M = M;
-                g.k0 = -d / S32;
+                g.k0 = -d / (float)S;
                 g.at_target = d;
                 barrier_arrive(&s_ready[side]);
             }
             const int t = row.x;
-            const float x_t = x_y;
-            const PolicyToken token_t = token;
             __syncwarp();
             announce(side ^ 1);
-            if (rank == 0) {
-                double S = 0.0;
-#pragma unroll
-                for (int k = 0; k < kParts; ++k) S += part[k].s * (double)factor[k];
-#pragma unroll
-                for (int off = 16; off > 0; off >>= 1) S += __shfl_xor_sync(0xFFFFFFFFu, S, off);
-                if (M == minus_inf()) S = CUDART_NAN;
-                if (lane == 0) {
-                    const double lp = ((double)x_t - (double)M) * inv_temperature - log_sum(S);
-                    policy_token(b, token_t, lp, term);
-                    if (*gave_up) term.gain = CUDART_NAN_F;
-                    logp[t] = (float)lp;
-                    terms[t] = term;
-                }
-                __syncwarp();
+            if (rank == 0 && lane == 0) {
+                if (*gave_up) term.gain = CUDART_NAN_F;
+                logp[t] = (float)lp;
+                terms[t] = term;
             }
+            __syncwarp();
         }
     } else {
         RingPlace place;                       // of the row's first chunk

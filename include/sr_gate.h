@@ -68,7 +68,7 @@ extern "C" {
 #define SR_STATUS_BAD_STATE 4      /* incremental state header does not match the call; step skipped */
 #define SR_STATUS_BAD_TARGET 8     /* a target token >= vocab was treated as one that does not count */
 #define SR_STATUS_NONFINITE 16     /* the gradient norm is not finite; gradients were not scaled */
-#define SR_STATUS_TIMEOUT 32       /* a kernel gave up a wait for its own copies: its outputs are undefined */
+#define SR_STATUS_TIMEOUT 32       /* a kernel gave up a wait: loss and stats are NaN, other outputs undefined */
 
 int sr_version(void);
 const char* sr_strerror(int code);      /* static string */

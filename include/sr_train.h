@@ -149,7 +149,8 @@ size_t sr_policy_loss_workspace_bytes(int32_t n_tokens);      /* host-only, pure
  *   d_logits   out as for sr_token_logprob_backward (may be the logits themselves)
  *   status     in/out 1 int32 of SR_STATUS_* bits; may be NULL.  SR_STATUS_TIMEOUT: CTAs that share a
  *              row have waited for one another for a second (microseconds are usual) and have given
- *              up; what the call wrote is not to be used
+ *              up; loss and stats are NaN then, status or not, and nothing else that the call wrote
+ *              is to be used
  *   workspace      device scratch of sr_policy_loss_logits_workspace_bytes(n_tokens) bytes, 16-byte aligned
  */
 int sr_policy_loss_logits(const void* logits, int32_t dtype, int32_t n_tokens, int32_t vocab, int64_t pitch,

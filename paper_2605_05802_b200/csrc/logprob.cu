@@ -648,8 +648,8 @@ struct RingRow {
     float x_y;
 };
 constexpr int kRingQueue = 8;        // rows that a CTA may know of
-// Counters: tokens that count; the next row of them to be taken; the next slice of the others.
-enum { kLive, kNextLive, kNextOther };
+// Counters: tokens that count; the next row of them to be taken; the next slice of the others; whether a CTA has given up a wait.
+enum { kLive, kNextLive, kNextOther, kGaveUp };
 
 // kAlone: one CTA to a row.  It is no cluster, and nothing is sent: what would be is written here, and its writers arrive.
 template <typename T, bool kAlone>
@@ -828,7 +828,6 @@ ring_policy_loss_kernel(const __grid_constant__ PolicyBatch b, const T* logits, 
             __syncwarp();
             announce(side ^ 1);
             if (rank == 0 && lane == 0) {
-                if (*gave_up) term.gain = CUDART_NAN_F;
                 logp[t] = (float)lp;
                 terms[t] = term;
             }
@@ -945,10 +944,16 @@ ring_policy_loss_kernel(const __grid_constant__ PolicyBatch b, const T* logits, 
                 out[single] = from_float<T>(v);
             }
         }
-        if (threadIdx.x == 0 && *gave_up && status) atomicOr(status, SR_STATUS_TIMEOUT);
     }
     __syncwarp();
-    if (!kAlone) cooperative_groups::this_cluster().sync();       // nobody leaves while its memory may be written to
+    // Nobody leaves while its memory may be written to; and whoever gave up has said so.  A row that was dropped for it, on whichever
+    // CTA, is missing from the loss, which the sum over the tokens then makes NaN.
+    if (kAlone) __syncthreads();
+    else cooperative_groups::this_cluster().sync();
+    if (threadIdx.x == 0 && *gave_up) {
+        atomicExch(&counters[kGaveUp], 1);
+        if (status) atomicOr(status, SR_STATUS_TIMEOUT);
+    }
 }
 
 // What token_rows_kernel says of every token, as a list: token, target and rollout of those that count, in order, and then the
@@ -999,7 +1004,7 @@ token_list_kernel(const __grid_constant__ PolicyBatch b, const int32_t* targets,
     }
     if (blockIdx.x == 0 && threadIdx.x == 0) {
         counters[kLive] = all;
-        counters[kNextLive] = counters[kNextOther] = 0;
+        counters[kNextLive] = counters[kNextOther] = counters[kGaveUp] = 0;
     }
     for (int base = first; base < last; base += kListThreads) {
         const int t0 = base + 32 * warp, t = t0 + lane;
@@ -1126,9 +1131,11 @@ int launch_step(const LogitsArgs& a, const PolicyBatch& b, const int32_t* row_of
                      1.0 / a.temperature, c, ctas, logp, terms, static_cast<T*>(d_logits), (long long)d_pitch);
 }
 
+// gave_up: where the kernels say so if they give up, or NULL where none can.
 template <typename T>
-int launch_rows(const LogitsArgs& a, const PolicyBatch& b, const StepScratch& ws, float* logp, void* d_logits, int64_t d_pitch, int32_t* status, cudaStream_t s) {
+int launch_rows(const LogitsArgs& a, const PolicyBatch& b, const StepScratch& ws, float* logp, void* d_logits, int64_t d_pitch, int32_t* status, const int32_t** gave_up, cudaStream_t s) {
     const int ring = alike(a, d_logits, d_pitch) ? ring_ctas(a.n_tokens, a.vocab, (int)sizeof(T)) : 0;
+    *gave_up = ring ? ws.counters + kGaveUp : nullptr;
     if (ring) return launch_ring<T>(a, b, ws, ring, logp, d_logits, d_pitch, status, s);
     SR_LAUNCH("token_rows_kernel", token_rows_kernel, (int)(((long long)a.n_tokens + 255) / 256), 256, 0, s, b, a.targets, a.vocab, a.n_tokens, ws.row_of, status);
     return launch_step<T>(a, b, ws.row_of, logp, ws.terms, d_logits, d_pitch, s);
@@ -1157,16 +1164,17 @@ int launch_token_logprob_backward(const LogitsArgs& a, const float* row_stats, c
 
 int launch_policy_loss_logits(const LogitsArgs& a, const PolicyBatch& b, float* loss, float* logp, void* d_logits, int64_t d_pitch, float* stats, int32_t* status,
                               const StepScratch& ws, cudaStream_t s) {
+    const int32_t* gave_up = nullptr;
     if (a.n_tokens > 0) {
         int rc;
         switch (a.dtype) {
-            case SR_DTYPE_F32: rc = launch_rows<float>(a, b, ws, logp, d_logits, d_pitch, status, s); break;
-            case SR_DTYPE_BF16: rc = launch_rows<__nv_bfloat16>(a, b, ws, logp, d_logits, d_pitch, status, s); break;
-            default: rc = launch_rows<__half>(a, b, ws, logp, d_logits, d_pitch, status, s); break;
+            case SR_DTYPE_F32: rc = launch_rows<float>(a, b, ws, logp, d_logits, d_pitch, status, &gave_up, s); break;
+            case SR_DTYPE_BF16: rc = launch_rows<__nv_bfloat16>(a, b, ws, logp, d_logits, d_pitch, status, &gave_up, s); break;
+            default: rc = launch_rows<__half>(a, b, ws, logp, d_logits, d_pitch, status, &gave_up, s); break;
         }
         if (rc != SR_OK) return rc;
     }
-    return launch_sum_terms(ws.terms, a.n_tokens, b.beta, loss, stats, ws.partial, s);
+    return launch_sum_terms(ws.terms, a.n_tokens, b.beta, gave_up, loss, stats, ws.partial, s);
 }
 
 }  // namespace sr

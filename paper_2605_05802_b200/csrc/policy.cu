@@ -9,6 +9,7 @@
 // bound by 94 instructions a token and their latency, with one or two lots of 128 ahead; three CTAs an SM take as long as two, four longer.
 // With a search and branches for every token it took 60.
 #include <cooperative_groups.h>
+#include <math_constants.h>
 
 #include "policy.cuh"
 
@@ -156,9 +157,9 @@ loss_weights_kernel(const int64_t* row_start, const uint8_t* mask, int n_tokens,
 }
 
 // What thread 0 of every CTA does with its sum.  kCluster: the grid is one cluster, whose sums meet in shared memory and become
-// the loss; its threads have arrived at the cluster's barrier.
+// the loss; its threads have arrived at the cluster's barrier.  failed: terms are missing, loss and figures become NaN.
 template <bool kCluster>
-__device__ __forceinline__ void leave_sum(PolicyTerms<double> sum, double beta, double* partial, float* loss, float* stats) {
+__device__ __forceinline__ void leave_sum(PolicyTerms<double> sum, double beta, bool failed, double* partial, float* loss, float* stats) {
     if (!kCluster) {
         if (threadIdx.x == 0) reinterpret_cast<PolicyTerms<double>*>(partial)[blockIdx.x] = sum;
         return;
@@ -170,6 +171,7 @@ __device__ __forceinline__ void leave_sum(PolicyTerms<double> sum, double beta, 
     cluster.sync();                        // the first CTA's memory alone is read after it
     if (blockIdx.x == 0 && threadIdx.x == 0) {
         for (unsigned c = 1; c < gridDim.x; ++c) add_terms(sum, s_sum[c]);
+        if (failed) sum.gain = sum.kl = sum.clipped = sum.rho = CUDART_NAN;
         write_policy_loss(sum, beta, loss, stats);
     }
 }
@@ -350,22 +352,23 @@ policy_loss_kernel(const __grid_constant__ PolicyBatch b, const float* logp, flo
             }
         }
     }
-    leave_sum<kCluster>(block_sum(sum), b.beta, partial, loss, stats);
+    leave_sum<kCluster>(block_sum(sum), b.beta, false, partial, loss, stats);
 }
 
 // Sums of terms: of the CTAs before (double), or of the tokens themselves (float).
 template <typename F, bool kCluster>
 __global__ void __launch_bounds__(1024)
-sum_terms_kernel(const PolicyTerms<F>* terms, int n, double beta, double* partial, float* loss, float* stats) {
+sum_terms_kernel(const PolicyTerms<F>* terms, int n, double beta, const int32_t* gave_up, double* partial, float* loss, float* stats) {
     grid_begin();
     if (kCluster) cluster_arrive();
+    const bool failed = kCluster && gave_up != nullptr && *gave_up != 0;
     PolicyTerms<double> sum = {0.0, 0.0, 0.0, 0.0};
 #pragma unroll 4
     for (long long i = (long long)blockIdx.x * blockDim.x + threadIdx.x; i < n; i += (long long)gridDim.x * blockDim.x) {
         const PolicyTerms<F> t = terms[i];
         add_terms(sum, PolicyTerms<double>{(double)t.gain, (double)t.kl, (double)t.clipped, (double)t.rho});
     }
-    leave_sum<kCluster>(block_sum(sum), beta, partial, loss, stats);
+    leave_sum<kCluster>(block_sum(sum), beta, failed, partial, loss, stats);
 }
 
 }  // namespace
@@ -393,14 +396,14 @@ int launch_loss_weights(const int64_t* row_start, const uint8_t* mask, int32_t n
 }
 
 // Up to 32768 tokens, four a thread, and sums of up to 131072 are one cluster's work: one launch.
-int launch_sum_terms(const PolicyTerms<float>* terms, int n, double beta, float* loss, float* stats, double* partial, cudaStream_t s) {
+int launch_sum_terms(const PolicyTerms<float>* terms, int n, double beta, const int32_t* gave_up, float* loss, float* stats, double* partial, cudaStream_t s) {
     if (n <= 1 << 17) {
         const int ctas = max(1, min(8, (n + 1023) / 1024)), threads = max(32, min(1024, (n + 31) & ~31));
-        return launch_as(true, ctas, "sum_terms_kernel", sum_terms_kernel<float, true>, ctas, threads, 0, s, terms, n, beta, partial, loss, stats);
+        return launch_as(true, ctas, "sum_terms_kernel", sum_terms_kernel<float, true>, ctas, threads, 0, s, terms, n, beta, gave_up, partial, loss, stats);
     }
     const int blocks = (int)min((long long)kMaxPartials, ((long long)n + 4095) / 4096);
-    SR_LAUNCH("sum_terms_kernel", sum_terms_kernel<float, false>, blocks, 1024, 0, s, terms, n, beta, partial, loss, stats);
-    SR_LAUNCH("sum_terms_kernel", sum_terms_kernel<double, true>, 1, 1024, 0, s, reinterpret_cast<const PolicyTerms<double>*>(partial), blocks, beta, partial, loss, stats);
+    SR_LAUNCH("sum_terms_kernel", sum_terms_kernel<float, false>, blocks, 1024, 0, s, terms, n, beta, gave_up, partial, loss, stats);
+    SR_LAUNCH("sum_terms_kernel", sum_terms_kernel<double, true>, 1, 1024, 0, s, reinterpret_cast<const PolicyTerms<double>*>(partial), blocks, beta, gave_up, partial, loss, stats);
     return SR_OK;
 }
 
@@ -413,7 +416,7 @@ int launch_policy_loss(const PolicyBatch& b, const float* logp, int32_t n, float
     }
     const int blocks = (int)min((long long)(148 * 2), ((long long)n + 1023) / 1024);
     SR_LAUNCH("policy_loss_kernel", vec ? policy_loss_kernel<true, false> : policy_loss_kernel<false, false>, blocks, 256, 0, s, b, logp, d_logp, n, partial, loss, stats);
-    SR_LAUNCH("sum_terms_kernel", sum_terms_kernel<double, true>, 1, 1024, 0, s, reinterpret_cast<const PolicyTerms<double>*>(partial), blocks, b.beta, partial, loss, stats);
+    SR_LAUNCH("sum_terms_kernel", sum_terms_kernel<double, true>, 1, 1024, 0, s, reinterpret_cast<const PolicyTerms<double>*>(partial), blocks, b.beta, static_cast<const int32_t*>(nullptr), partial, loss, stats);
     return SR_OK;
 }
 

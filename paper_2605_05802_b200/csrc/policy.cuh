@@ -262,8 +262,8 @@ constexpr int kMaxPartials = 1184;   // CTAs that leave a sum each: eight on eac
 int launch_loss_weights(const int64_t* row_start, const uint8_t* mask, int32_t n_tokens, const uint8_t* drop_mask, int32_t n_groups, int32_t N, int32_t mode,
                         double scale, float* weight, int64_t* counts, void* ws, cudaStream_t s);
 int launch_policy_loss(const PolicyBatch& b, const float* logp, int32_t n, float* loss, float* d_logp, float* stats, double* partial, cudaStream_t s);
-// Sums the terms of n tokens into loss and stats.
-int launch_sum_terms(const PolicyTerms<float>* terms, int n, double beta, float* loss, float* stats, double* partial, cudaStream_t s);
+// Sums the terms of n tokens into loss and stats; NaN where *gave_up is set (NULL: it cannot be).
+int launch_sum_terms(const PolicyTerms<float>* terms, int n, double beta, const int32_t* gave_up, float* loss, float* stats, double* partial, cudaStream_t s);
 
 // logprob.cu
 struct StepScratch {

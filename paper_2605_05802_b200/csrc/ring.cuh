@@ -44,22 +44,22 @@ __device__ __forceinline__ unsigned long long nanoseconds() {
 }
 constexpr unsigned long long kWaitLimit = 1000000000ull;     // a second; a wait takes microseconds
 
-// Waits for the phase with that parity.  After the limit, or where another thread of the CTA has given up, *gave_up is set and the
+// Waits for the phase with that parity.  After `limit` ns (looked at every millisecond or so), or where another thread of the CTA has given up, *gave_up is set and the
 // wait ends all the same: whoever reads it says so in the results.
-__device__ __noinline__ void barrier_wait_long(uint64_t* bar, uint32_t parity, volatile int* gave_up) {
+__device__ __noinline__ void barrier_wait_long(uint64_t* bar, uint32_t parity, volatile int* gave_up, unsigned long long limit) {
     const unsigned long long began = nanoseconds();
     for (;;) {
         for (int k = 0; k < 64; ++k)
             if (barrier_test(bar, parity)) return;
         if (*gave_up) return;
-        if (nanoseconds() - began > kWaitLimit) {
+        if (nanoseconds() - began > limit) {
             *gave_up = 1;
             return;
         }
     }
 }
-__device__ __forceinline__ void barrier_wait(uint64_t* bar, uint32_t parity, volatile int* gave_up) {
-    if (!barrier_test(bar, parity)) barrier_wait_long(bar, parity, gave_up);
+__device__ __forceinline__ void barrier_wait(uint64_t* bar, uint32_t parity, volatile int* gave_up, unsigned long long limit = kWaitLimit) {
+    if (!barrier_test(bar, parity)) barrier_wait_long(bar, parity, gave_up, limit);
 }
 
 // Copies `bytes` (a multiple of 16, both addresses on 16 bytes) from global into this CTA's shared memory and counts them at `bar`.

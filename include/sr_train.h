@@ -110,6 +110,8 @@ size_t sr_loss_weights_workspace_bytes(int32_t n_rollouts);   /* host-only, pure
  *   kl_t   = exp(d) - 1 - d
  *   loss   = sum_r weight[r] sum_{t in r that counts} (beta kl_t - gain_t)
  *   d loss / d logp_t = weight[r] (-A rho [not clipped] + beta (1 - exp(d)))
+ * A factor of 0 leaves its term out whatever stands beside it, a NaN for one: A = 0 the gain, beta = 0
+ * the KL term (of loss and gradient; the figures of rho and kl are sums without these factors).
  * A token counts when it lies in a rollout whose weight is not 0 and its mask byte is non-zero;
  * what stands in the arrays for the others is not used.
  *

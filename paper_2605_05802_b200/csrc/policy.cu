@@ -181,8 +181,8 @@ __device__ __noinline__ float one_token(const PolicyBatch& b, float old_logp, fl
     return policy_token(b, PolicyToken{old_logp, ref_logp, adv, weight}, lp, out);
 }
 // policy_token of four tokens side by side, two to an instruction and without branches: one that does not count (bit 8 j of
-// `counts`) has policies that agree.  Lanes that need another look (a ratio at a border of the clip range, numbers near overflow) take
-// their tokens one by one.  kOne: they lie in one rollout, w[0] and a[0] are its.
+// `counts`) has policies that agree.  Lanes that need another look (a ratio at a border of the clip range, numbers near overflow, a NaN, which
+// a factor of 0 would not take away here) take their tokens one by one.  kOne: they lie in one rollout, w[0] and a[0] are its.
 template <bool kOne>
 __device__ __forceinline__ void four_tokens(const PolicyBatch& b, const float (&lp)[4], const float (&old_logp)[4], const float (&ref_logp)[4], const float (&w)[4],
                                             const float (&a)[4], uint32_t counts, float (&grad)[4], PolicyTerms<float>& sum) {
@@ -209,13 +209,13 @@ __device__ __forceinline__ void four_tokens(const PolicyBatch& b, const float (&
         past[j] = over * side > 0.0f;
         gain[j] = A[j] * (past[j] ? border : rho[j]);
         grad[j] = past[j] ? 0.0f : -gain[j];
-        again |= is[j] && fabsf(over) <= ratio_margin(delta[j]) * border;
+        again |= is[j] && !(fabsf(over) > ratio_margin(delta[j]) * border);
     }
     if (b.ref_logp) {
 #pragma unroll
         for (int j = 0; j < 4; j += 2) {
             const float d0 = is[j] ? ref_logp[j] - lp[j] : 0.0f, d1 = is[j + 1] ? ref_logp[j + 1] - lp[j + 1] : 0.0f;
-            again |= fabsf(d0) > 80.0f || fabsf(d1) > 80.0f;
+            again |= !(fabsf(d0) <= 80.0f && fabsf(d1) <= 80.0f);
             f32x2 em1, both;
             exp_less_line_near(two(d0, d1), em1, both);
             kl[j] = low_of(both);

@@ -45,7 +45,7 @@ extern "C" {
 #define SR_ERR_BAD_MODE (-8)       /* unknown norm_mode or loss mode */
 #define SR_ERR_SCRATCH_LIMIT (-9)  /* sr_gate_noalloc: problem needs more than the built-in scratch */
 #define SR_ERR_BAD_OFFSETS (-10)   /* sr_gate_host_packed: row_start malformed */
-#define SR_ERR_BAD_SIZE (-11)      /* sr_train.h: negative count, empty vocabulary, pitch < vocab */
+#define SR_ERR_BAD_SIZE (-11)      /* sr_train.h: negative count, empty vocabulary, pitch < vocab, 32 TB of gradients */
 #define SR_ERR_BAD_DTYPE (-12)     /* sr_train.h: unknown element type */
 #define SR_ERR_BAD_VALUE (-13)     /* sr_train.h: temperature, clip range, beta, scale or max_norm out of range */
 #define SR_ERR_OVERLAP (-14)       /* sr_train.h: buffers that must not overlap do */

@@ -166,7 +166,8 @@ size_t sr_policy_loss_logits_workspace_bytes(int32_t n_tokens);   /* host-only, 
 
 /*
  * sr_grad_norm -- the L2 norm of all gradients together (Section 4.5), squares summed in fp64 in
- * an order that depends on the sizes alone.
+ * an order that depends on the sizes alone.  Gradients of a call are at most 2^31 - 1 pieces of 16 KB (each
+ * begins a piece of its own): SR_ERR_BAD_SIZE above.
  *
  *   grads, counts, dtypes   HOST arrays of n_tensors: device pointer, number of elements (0 is
  *                           fine, the pointer may then be NULL) and SR_DTYPE_* of each tensor;

@@ -64,7 +64,7 @@ const char* sr_strerror(int code) {
         case SR_ERR_BAD_MODE: return "unknown norm_mode or loss mode";
         case SR_ERR_SCRATCH_LIMIT: return "problem needs more scratch than sr_gate_noalloc's built-in array";
         case SR_ERR_BAD_OFFSETS: return "row_start does not begin at 0, decreases, or exceeds rows x stride symbols";
-        case SR_ERR_BAD_SIZE: return "negative count, empty vocabulary, or a pitch below the vocabulary";
+        case SR_ERR_BAD_SIZE: return "negative count, empty vocabulary, a pitch below the vocabulary, or 32 TB of gradients and more";
         case SR_ERR_BAD_DTYPE: return "unknown element type";
         case SR_ERR_BAD_VALUE: return "temperature, clip range, beta, scale or max_norm out of range";
         case SR_ERR_OVERLAP: return "buffers overlap that must not";

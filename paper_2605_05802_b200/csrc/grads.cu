@@ -17,7 +17,8 @@ namespace {
 
 constexpr int kGradThreads = 256;
 constexpr int kVecsInFlight = 4;
-constexpr int kPieceBytes = kGradThreads * kVecsInFlight * 16;      // 16 KB
+constexpr int kPieceBytes = kGradPiece;
+static_assert(kPieceBytes == kGradThreads * kVecsInFlight * 16, "a piece is what a CTA has in flight");
 constexpr int kGradCtas = 148 * 6;
 
 // kCap tensors; a kernel argument may have 32764 bytes.
@@ -182,7 +183,8 @@ clip_grads_kernel(const __grid_constant__ GradList<kCap> list, const float* norm
     });
 }
 
-// Calls launch_list(list, CTAs) for the tensors, as many at a time as one kernel argument holds.
+// Calls launch_list(list, CTAs) for the tensors, as many at a time as one kernel argument holds.  Their pieces are at most
+// INT32_MAX: the caller has counted them.
 template <int kCap, typename Launch>
 int for_lists(const void* const* grads, const int64_t* counts, const int32_t* dtypes, int32_t n_tensors, void* const* out, Launch launch_list) {
     GradList<kCap> list;
@@ -191,14 +193,12 @@ int for_lists(const void* const* grads, const int64_t* counts, const int32_t* dt
         int n = 0;
         for (; at < n_tensors && n < kCap; ++at) {
             if (counts[at] == 0) continue;
-            const int64_t per = kPieceBytes / dtype_bytes(dtypes[at]), more = (counts[at] + per - 1) / per;
-            if (pieces + more > INT32_MAX) break;              // 64 TB
             list.src[n] = grads[at];
             list.dst[n] = out ? out[at] : const_cast<void*>(grads[at]);
             list.count[n] = counts[at];
             list.dtype[n] = (uint8_t)dtypes[at];
             list.piece[n++] = (int32_t)pieces;
-            pieces += more;
+            pieces += grad_pieces(counts[at], dtypes[at]);
         }
         if (n == 0) break;
         list.piece[n] = (int32_t)pieces;

@@ -158,6 +158,11 @@ int launch_token_logprob_backward(const LogitsArgs& a, const float* row_stats, c
                                   int64_t d_pitch, cudaStream_t s);
 
 // grads.cu
+constexpr int kGradPiece = 16384;    // bytes of a tensor that a CTA takes at a time; pieces of a call are numbered in 32 bits: 32 TB
+inline int64_t grad_pieces(int64_t count, int32_t dtype) {      // count >= 0
+    const int64_t per = kGradPiece / dtype_bytes(dtype);
+    return count / per + (count % per != 0);
+}
 size_t grad_norm_workspace_bytes(int32_t n_tensors);
 int launch_grad_norm(const void* const* grads, const int64_t* counts, const int32_t* dtypes, int32_t n_tensors, float* norm, void* ws, cudaStream_t s);
 int launch_clip_grads(const void* const* grads, const int64_t* counts, const int32_t* dtypes, int32_t n_tensors, const float* norm, float max_norm,

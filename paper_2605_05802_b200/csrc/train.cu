@@ -59,10 +59,13 @@ int check_policy(const float* adv, const float* weight, const int64_t* row_start
 int check_grads(const void* const* grads, const int64_t* counts, const int32_t* dtypes, int32_t n_tensors) {
     if (n_tensors < 0) return SR_ERR_BAD_N;
     if (n_tensors > 0 && (grads == nullptr || counts == nullptr || dtypes == nullptr)) return SR_ERR_NULL;
+    int64_t pieces = 0;
     for (int i = 0; i < n_tensors; ++i) {
-        if (counts[i] < 0 || counts[i] > (int64_t(1) << 43)) return SR_ERR_BAD_SIZE;
+        if (counts[i] < 0) return SR_ERR_BAD_SIZE;
         const int size = dtype_bytes(dtypes[i]);
         if (size == 0) return SR_ERR_BAD_DTYPE;
+        pieces += grad_pieces(counts[i], dtypes[i]);                // of one tensor below 2^52
+        if (pieces > INT32_MAX) return SR_ERR_BAD_SIZE;
         if (counts[i] > 0 && grads[i] == nullptr) return SR_ERR_NULL;
         if (!aligned(grads[i], size)) return SR_ERR_ALIGN;
     }

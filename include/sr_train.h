@@ -88,8 +88,8 @@ int sr_token_logprob_backward(const void* logits, int32_t dtype, int32_t n_token
  * use the same ones.  A rollout without a token that counts gets +0.
  *
  *   row_start  in  [n_groups * N + 1] int64, non-decreasing
- *   mask       in  [n_tokens] uint8 or NULL (every token counts); positions outside
- *                  0 .. n_tokens do not count
+ *   mask       in  [n_tokens] uint8: positions outside 0 .. n_tokens do not count.  NULL: every token
+ *                  between a rollout's row starts counts, wherever these lie, and n_tokens is not used
  *   drop_mask  in  [n_groups] uint8 or NULL: non-zero = cut (sr_gate's stop, for example)
  *   mode           SR_LOSS_*;  scale: finite in fp32
  *   weight     out [n_groups * N] fp32

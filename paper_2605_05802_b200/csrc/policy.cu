@@ -93,7 +93,7 @@ count_tokens_kernel(const int64_t* row_start, int rows, const uint8_t* mask, int
 constexpr int kWeightThreads = 1024;
 
 // One cluster.  kCount: its CTAs count the tokens of up to kRowsOfCta rollouts each; otherwise `tokens` holds the counts, or is
-// NULL where every token counts.
+// NULL where every token counts (n_tokens is the mask's size, and not looked at then).
 template <bool kCount>
 __global__ void __launch_bounds__(kWeightThreads)
 loss_weights_kernel(const int64_t* row_start, const uint8_t* mask, int n_tokens, const int32_t* tokens,

@@ -518,15 +518,15 @@ token_rows_kernel(PolicyBatch b, const int32_t* targets, int vocab, int n, int32
 // By one thread: the token's terms of the loss and the gradient of its row.  A function of its own, so that the registers of a
 // held row are put aside for it in that thread alone.
 __device__ __noinline__ void token_gradient(const PolicyBatch& b, const PolicyToken& k, int t, float x_y, float m, double S, double inv_temperature, float* logp,
-                                            PolicyTerms<float>* terms, RowGradient* g) {
+                                            PolicyTerms* terms, RowGradient* g) {
     const double lp = ((double)x_y - (double)m) * inv_temperature - log_sum(S);
-    PolicyTerms<float> term;
-    const float d = policy_token(b, k, lp, term) * (float)inv_temperature;
+    PolicyParts parts;
+    const float d = policy_gradient(b, k, lp, parts) * (float)inv_temperature;
     g->k0 = -d / (float)S;
     g->at_target = d;
     if (logp) {
         logp[t] = (float)lp;
-        terms[t] = term;
+        terms[t] = policy_terms(b, k, parts);
     }
 }
 __device__ __forceinline__ PolicyToken load_token(const PolicyBatch& b, int t, int rollout) {
@@ -534,7 +534,7 @@ __device__ __forceinline__ PolicyToken load_token(const PolicyBatch& b, int t, i
 }
 // The gradient of a row, in every thread of the CTA; `first` writes down the token's figures.
 __device__ __forceinline__ RowGradient loss_gradient(const PolicyBatch& b, const PolicyToken& k, int t, float x_y, int y, const RowSums& r, double inv_temperature, float c, bool first,
-                                                     float* logp, PolicyTerms<float>* terms) {
+                                                     float* logp, PolicyTerms* terms) {
     __shared__ RowGradient s_g;
     if (threadIdx.x == 0) token_gradient(b, k, t, x_y, r.m, r.s, inv_temperature, first ? logp : nullptr, terms, &s_g);
     __syncthreads();
@@ -551,7 +551,7 @@ __device__ __forceinline__ RowGradient loss_gradient(const PolicyBatch& b, const
 template <typename T>
 __global__ void __launch_bounds__(kRowThreads, 4)
 policy_loss_logits_kernel(PolicyBatch b, const T* logits, int vocab, long long pitch, const int32_t* targets, const int32_t* row_of,
-                          double inv_temperature, float c, int ctas, float* logp, PolicyTerms<float>* terms, T* d_logits, long long d_pitch) {
+                          double inv_temperature, float c, int ctas, float* logp, PolicyTerms* terms, T* d_logits, long long d_pitch) {
     grid_begin();
     const int t = blockIdx.x / ctas, part = blockIdx.x % ctas;
     const int at = part * kRowThreads + threadIdx.x, threads = ctas * kRowThreads;
@@ -563,7 +563,7 @@ policy_loss_logits_kernel(PolicyBatch b, const T* logits, int vocab, long long p
         write_gradient<T, false, true>(nullptr, out, vocab, at, threads, g);
         if (first) {
             logp[t] = 0.0f;
-            terms[t] = PolicyTerms<float>{0.0f, 0.0f, 0.0f, 0.0f};
+            terms[t] = PolicyTerms{0.0, 0.0f, 0.0f, 0.0f};
         }
         return;
     }
@@ -583,7 +583,7 @@ policy_loss_logits_kernel(PolicyBatch b, const T* logits, int vocab, long long p
 template <typename T, int kVecs, bool kAlone>
 __global__ void __launch_bounds__(kHeldThreads, kVecs > 7 ? 3 : kVecs > 4 ? 4 : kVecs > 2 ? 5 : 7)
 held_policy_loss_kernel(PolicyBatch b, const T* logits, int vocab, long long pitch, const int32_t* targets, const int32_t* row_of,
-                        double inv_temperature, float c, int some_ctas, float* logp, PolicyTerms<float>* terms, T* d_logits, long long d_pitch) {
+                        double inv_temperature, float c, int some_ctas, float* logp, PolicyTerms* terms, T* d_logits, long long d_pitch) {
     grid_begin();
     const int ctas = kAlone ? 1 : some_ctas, t = blockIdx.x / ctas, part = blockIdx.x % ctas;
     const int at = part * kHeldThreads + threadIdx.x, threads = ctas * kHeldThreads;
@@ -594,7 +594,7 @@ held_policy_loss_kernel(PolicyBatch b, const T* logits, int vocab, long long pit
         write_gradient<T, false, true>(nullptr, out, vocab, at, threads, RowGradient());
         if (first) {
             logp[t] = 0.0f;
-            terms[t] = PolicyTerms<float>{0.0f, 0.0f, 0.0f, 0.0f};
+            terms[t] = PolicyTerms{0.0, 0.0f, 0.0f, 0.0f};
         }
         return;
     }
@@ -655,7 +655,7 @@ enum { kLive, kNextLive, kNextOther, kGaveUp };
 template <typename T, bool kAlone>
 __global__ void __launch_bounds__(kRingThreads + 64, 2)
 ring_policy_loss_kernel(const __grid_constant__ PolicyBatch b, const T* logits, int vocab, long long pitch, const int4* list, int32_t* counters, int n_tokens, double inv_temperature,
-                        float c, int ctas, float* logp, PolicyTerms<float>* terms, T* d_logits, long long d_pitch, int32_t* status) {
+                        float c, int ctas, float* logp, PolicyTerms* terms, T* d_logits, long long d_pitch, int32_t* status) {
     constexpr int E = Vec<T>::kElems;
     extern __shared__ __align__(128) unsigned char s_ring[];
     __shared__ uint64_t s_full[kRingSlots], s_empty[kRingSlots];                  // chunks that are there, and that are done with
@@ -815,8 +815,8 @@ ring_policy_loss_kernel(const __grid_constant__ PolicyBatch b, const T* logits, 
                 if (off < parts) S += __shfl_xor_sync(0xFFFFFFFFu, S, off);
             if (M == minus_inf()) S = CUDART_NAN;      // no token can occur: there is no distribution
             const double lp = ((double)x_y - (double)M) * inv_temperature - log_sum(S);
-            PolicyTerms<float> term;
-            const float d = policy_token(b, token, lp, term) * (float)inv_temperature;
+            PolicyParts loss_parts;
+            const float d = policy_gradient(b, token, lp, loss_parts) * (float)inv_temperature;
             if (lane == 0) {
                 RowGradient& g = s_gradient[side];
                 g.M = M;
@@ -825,11 +825,12 @@ ring_policy_loss_kernel(const __grid_constant__ PolicyBatch b, const T* logits, 
                 barrier_arrive(&s_ready[side]);
             }
             const int t = row.x;
+            const PolicyToken token_t = token;
             __syncwarp();
             announce(side ^ 1);
             if (rank == 0 && lane == 0) {
                 logp[t] = (float)lp;
-                terms[t] = term;
+                terms[t] = policy_terms(b, token_t, loss_parts);
             }
             __syncwarp();
         }
@@ -960,7 +961,7 @@ ring_policy_loss_kernel(const __grid_constant__ PolicyBatch b, const T* logits, 
 // others, whose figures are written here; and the ring's counters.  One cluster.
 constexpr int kListThreads = 1024, kListTokens = 65536;
 __global__ void __launch_bounds__(kListThreads)
-token_list_kernel(const __grid_constant__ PolicyBatch b, const int32_t* targets, int vocab, int n, int4* list, int32_t* counters, float* logp, PolicyTerms<float>* terms, int32_t* status) {
+token_list_kernel(const __grid_constant__ PolicyBatch b, const int32_t* targets, int vocab, int n, int4* list, int32_t* counters, float* logp, PolicyTerms* terms, int32_t* status) {
     grid_begin();
     cluster_arrive();
     __shared__ int s_warp[32], s_cta[8];
@@ -1020,7 +1021,7 @@ token_list_kernel(const __grid_constant__ PolicyBatch b, const int32_t* targets,
             list[counts ? at : all + (t - at)] = make_int4(t, own.y, own.x, 0);
             if (!counts) {
                 logp[t] = 0.0f;
-                terms[t] = PolicyTerms<float>{0.0f, 0.0f, 0.0f, 0.0f};
+                terms[t] = PolicyTerms{0.0, 0.0f, 0.0f, 0.0f};
             }
         }
         before += total;
@@ -1117,7 +1118,7 @@ int launch_ring(const LogitsArgs& a, const PolicyBatch& b, const StepScratch& ws
                      ws.list, ws.counters, a.n_tokens, 1.0 / a.temperature, c, ctas, logp, ws.terms, static_cast<T*>(d_logits), (long long)d_pitch, status);
 }
 template <typename T>
-int launch_step(const LogitsArgs& a, const PolicyBatch& b, const int32_t* row_of, float* logp, PolicyTerms<float>* terms, void* d_logits, int64_t d_pitch, cudaStream_t s) {
+int launch_step(const LogitsArgs& a, const PolicyBatch& b, const int32_t* row_of, float* logp, PolicyTerms* terms, void* d_logits, int64_t d_pitch, cudaStream_t s) {
     const float c = (float)(1.0 / (kLn2 * a.temperature));
     const Held held = held_row(a.n_tokens, a.vocab, (int)sizeof(T));
     if (held.vecs && alike(a, d_logits, d_pitch))

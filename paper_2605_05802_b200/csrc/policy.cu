@@ -159,12 +159,12 @@ loss_weights_kernel(const int64_t* row_start, const uint8_t* mask, int n_tokens,
 // What thread 0 of every CTA does with its sum.  kCluster: the grid is one cluster, whose sums meet in shared memory and become
 // the loss; its threads have arrived at the cluster's barrier.  failed: terms are missing, loss and figures become NaN.
 template <bool kCluster>
-__device__ __forceinline__ void leave_sum(PolicyTerms<double> sum, double beta, bool failed, double* partial, float* loss, float* stats) {
+__device__ __forceinline__ void leave_sum(PolicySums<double> sum, double beta, bool failed, double* partial, float* loss, float* stats) {
     if (!kCluster) {
-        if (threadIdx.x == 0) reinterpret_cast<PolicyTerms<double>*>(partial)[blockIdx.x] = sum;
+        if (threadIdx.x == 0) reinterpret_cast<PolicySums<double>*>(partial)[blockIdx.x] = sum;
         return;
     }
-    __shared__ PolicyTerms<double> s_sum[8];
+    __shared__ PolicySums<double> s_sum[8];
     const auto cluster = cooperative_groups::this_cluster();
     cluster_wait();
     if (threadIdx.x == 0) *cluster.map_shared_rank(&s_sum[blockIdx.x], 0) = sum;
@@ -176,46 +176,65 @@ __device__ __forceinline__ void leave_sum(PolicyTerms<double> sum, double beta, 
     }
 }
 
-// policy_token for the rare token that the code below leaves to it.
-__device__ __noinline__ float one_token(const PolicyBatch& b, float old_logp, float ref_logp, float adv, float weight, float lp, PolicyTerms<float>& out) {
-    return policy_token(b, PolicyToken{old_logp, ref_logp, adv, weight}, lp, out);
+// Gradient and terms of the rare token that the code below leaves to this.
+__device__ __noinline__ float one_token(const PolicyBatch& b, float old_logp, float ref_logp, float adv, float weight, float lp, PolicyTerms& out) {
+    const PolicyToken token{old_logp, ref_logp, adv, weight};
+    PolicyParts parts;
+    const float gradient = policy_gradient(b, token, lp, parts);
+    out = policy_terms(b, token, parts);
+    return gradient;
 }
-// policy_token of four tokens side by side, two to an instruction and without branches: one that does not count (bit 8 j of
+// The same of four tokens side by side, two to an instruction and without branches: one that does not count (bit 8 j of
 // `counts`) has policies that agree.  Lanes that need another look (a ratio at a border of the clip range, numbers near overflow, a NaN, which
 // a factor of 0 would not take away here) take their tokens one by one.  kOne: they lie in one rollout, w[0] and a[0] are its.
+//
+// Advantages of a group add up to 0, and the loss is a small difference of large terms.  So what is added up in fp32 is w A (rho - 1), from
+// the series that the KL term has, and w A by itself goes into sum_gain, in fp64.  A token that does not count has rho - 1 = 0 and adds
+// nothing to the sums.
 template <bool kOne>
 __device__ __forceinline__ void four_tokens(const PolicyBatch& b, const float (&lp)[4], const float (&old_logp)[4], const float (&ref_logp)[4], const float (&w)[4],
-                                            const float (&a)[4], uint32_t counts, float (&grad)[4], PolicyTerms<float>& sum) {
+                                            const float (&a)[4], uint32_t counts, float (&grad)[4], PolicySums<float>& sum, double& sum_gain) {
+    const float inf = __int_as_float(0x7F800000);
     bool again = false, is[4], past[4];
-    float A[4], rho[4], gain[4], kl[4] = {0.0f, 0.0f, 0.0f, 0.0f}, delta[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    float A[4], rho[4], less[4], used[4], kl[4] = {0.0f, 0.0f, 0.0f, 0.0f}, delta[4] = {0.0f, 0.0f, 0.0f, 0.0f};      // less: rho - 1, to its own size; used: within the clip range
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
         is[j] = (counts >> (8 * j)) & 1u;
-        A[j] = kOne ? a[0] : a[j];
-        rho[j] = is[j] && !(lp[j] == lp[j]) ? lp[j] : 1.0f;     // a NaN stays one
+        A[j] = kOne ? (counts != 0u ? a[0] : 0.0f) : is[j] ? a[j] : 0.0f;
     }
-    if (b.old_logp) {
+    if (!b.old_logp) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {          // off by 2^-22 and |delta| 2^-23 of itself, and 0 below 2^-126
+        for (int j = 0; j < 4; ++j) {
+            less[j] = is[j] && !(lp[j] == lp[j]) ? lp[j] : 0.0f;    // a NaN stays one
+            rho[j] = 1.0f + less[j];
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < 4; j += 2) {
             if (is[j]) delta[j] = lp[j] - old_logp[j];
-            again |= delta[j] > 80.0f;
-            asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(rho[j]) : "f"(delta[j] * 1.44269504f));
+            if (is[j + 1]) delta[j + 1] = lp[j + 1] - old_logp[j + 1];
+            again |= !(fabsf(delta[j]) <= 80.0f) || !(fabsf(delta[j + 1]) <= 80.0f);
+            f32x2 e, em1;
+            exp_near(two(delta[j], delta[j + 1]), e, em1);
+            rho[j] = low_of(e);
+            rho[j + 1] = high_of(e);
+            less[j] = low_of(em1);
+            less[j + 1] = high_of(em1);
         }
     }
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-        const float border = A[j] > 0.0f ? b.high : b.low, side = A[j] > 0.0f ? 1.0f : A[j] < 0.0f ? -1.0f : 0.0f;
-        const float over = rho[j] - border;
-        past[j] = over * side > 0.0f;
-        gain[j] = A[j] * (past[j] ? border : rho[j]);
-        grad[j] = past[j] ? 0.0f : -gain[j];
-        again |= is[j] && !(fabsf(over) > ratio_margin(delta[j]) * border);
+        const float border = A[j] > 0.0f ? b.high : b.low, less_border = A[j] > 0.0f ? b.less_high : b.less_low;
+        used[j] = fminf(fmaxf(less[j], A[j] < 0.0f ? b.less_low : -inf), A[j] > 0.0f ? b.less_high : inf);
+        past[j] = used[j] != less[j];
+        grad[j] = -A[j] * (past[j] ? 0.0f : rho[j]);
+        again |= !(fabsf(less[j] - less_border) > fmaf(fabsf(delta[j]), kMarginSlope * border, kMargin * border));      // also: NaN
     }
     if (b.ref_logp) {
 #pragma unroll
         for (int j = 0; j < 4; j += 2) {
             const float d0 = is[j] ? ref_logp[j] - lp[j] : 0.0f, d1 = is[j + 1] ? ref_logp[j + 1] - lp[j + 1] : 0.0f;
-            again |= !(fabsf(d0) <= 80.0f && fabsf(d1) <= 80.0f);
+            again |= !(fabsf(d0) <= 80.0f) || !(fabsf(d1) <= 80.0f);
             f32x2 em1, both;
             exp_less_line_near(two(d0, d1), em1, both);
             kl[j] = low_of(both);
@@ -227,9 +246,9 @@ __device__ __forceinline__ void four_tokens(const PolicyBatch& b, const float (&
     if (again) {
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            PolicyTerms<float> term = {0.0f, 0.0f, 0.0f, 0.0f};
+            PolicyTerms term = {0.0, 0.0f, 0.0f, 0.0f};
             grad[j] = is[j] ? one_token(b, old_logp[j], ref_logp[j], A[j], kOne ? w[0] : w[j], lp[j], term) : 0.0f;
-            sum.gain += term.gain;
+            sum_gain += term.gain;
             sum.kl += term.kl;
             sum.clipped += term.clipped;
             sum.rho += term.rho;
@@ -238,14 +257,13 @@ __device__ __forceinline__ void four_tokens(const PolicyBatch& b, const float (&
     }
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-        const float weight = kOne ? w[0] : w[j];
-        gain[j] = is[j] ? gain[j] : 0.0f;
         rho[j] = is[j] ? rho[j] : 0.0f;
-        grad[j] = is[j] ? weight * grad[j] : 0.0f;
+        grad[j] = is[j] ? (kOne ? w[0] : w[j]) * grad[j] : 0.0f;
     }
-    const auto of = [&](int j) { return is[j] && past[j] ? 1.0f : 0.0f; };
+    const auto of = [&](int j) { return past[j] ? 1.0f : 0.0f; };
     if (kOne) {
-        sum.gain = fmaf(w[0], (gain[0] + gain[1]) + (gain[2] + gain[3]), sum.gain);
+        sum_gain += (double)__popc(counts) * ((double)w[0] * (double)A[0]);
+        sum.gain = fmaf(w[0] * A[0], (used[0] + used[1]) + (used[2] + used[3]), sum.gain);
         sum.kl = fmaf(w[0], (kl[0] + kl[1]) + (kl[2] + kl[3]), sum.kl);
         sum.clipped = fmaf(w[0], (of(0) + of(1)) + (of(2) + of(3)), sum.clipped);
         sum.rho = fmaf(w[0], (rho[0] + rho[1]) + (rho[2] + rho[3]), sum.rho);
@@ -253,7 +271,8 @@ __device__ __forceinline__ void four_tokens(const PolicyBatch& b, const float (&
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             const float weight = is[j] ? w[j] : 0.0f;
-            sum.gain = fmaf(weight, gain[j], sum.gain);
+            sum_gain += (double)weight * (double)A[j];
+            sum.gain = fmaf(weight * A[j], used[j], sum.gain);
             sum.kl = fmaf(weight, kl[j], sum.kl);
             sum.clipped = fmaf(weight, of(j), sum.clipped);
             sum.rho = fmaf(weight, rho[j], sum.rho);
@@ -275,8 +294,8 @@ policy_loss_kernel(const __grid_constant__ PolicyBatch b, const float* logp, flo
     const long long lots = ((long long)n + 127) >> 7;
     uint32_t lot = (uint32_t)(lots * warp / all);
     const uint32_t end = (uint32_t)(lots * (warp + 1) / all);
-    PolicyTerms<double> sum = {0.0, 0.0, 0.0, 0.0};
-    PolicyTerms<float> mine = {0.0f, 0.0f, 0.0f, 0.0f};
+    PolicySums<double> sum = {0.0, 0.0, 0.0, 0.0};
+    PolicySums<float> mine = {0.0f, 0.0f, 0.0f, 0.0f};
     struct Four {
         float lp[4], old_logp[4], ref_logp[4];
         uint32_t mask;
@@ -326,13 +345,13 @@ policy_loss_kernel(const __grid_constant__ PolicyBatch b, const float* logp, flo
             counts = __vminu4(counts, 0x01010101u);
             float w[4], a[4];
             if (walk.one_rollout(w0, w[0], a[0])) {
-                if (w[0] != 0.0f) four_tokens<true>(b, four.lp, four.old_logp, four.ref_logp, w, a, counts, grad, mine);
+                if (w[0] != 0.0f) four_tokens<true>(b, four.lp, four.old_logp, four.ref_logp, w, a, counts, grad, mine, sum.gain);
             } else {
                 walk.several_rollouts(w0, t0, w, a);
 #pragma unroll
                 for (int j = 0; j < 4; ++j)
                     if (w[j] == 0.0f) counts &= ~(1u << (8 * j));
-                four_tokens<false>(b, four.lp, four.old_logp, four.ref_logp, w, a, counts, grad, mine);
+                four_tokens<false>(b, four.lp, four.old_logp, four.ref_logp, w, a, counts, grad, mine, sum.gain);
             }
         }
         if ((lot & 3u) == 3u || lot + 1 == end) {        // fp32 over up to 16 tokens, fp64 from there on
@@ -340,7 +359,7 @@ policy_loss_kernel(const __grid_constant__ PolicyBatch b, const float* logp, flo
             sum.kl += (double)mine.kl;
             sum.clipped += (double)mine.clipped;
             sum.rho += (double)mine.rho;
-            mine = PolicyTerms<float>{0.0f, 0.0f, 0.0f, 0.0f};
+            mine = PolicySums<float>{0.0f, 0.0f, 0.0f, 0.0f};
         }
         if (d_logp) {
             if (kVec && t0 + 4 <= tokens) {
@@ -355,18 +374,18 @@ policy_loss_kernel(const __grid_constant__ PolicyBatch b, const float* logp, flo
     leave_sum<kCluster>(block_sum(sum), b.beta, false, partial, loss, stats);
 }
 
-// Sums of terms: of the CTAs before (double), or of the tokens themselves (float).
-template <typename F, bool kCluster>
+// Sums of terms: of the tokens (PolicyTerms), or of the CTAs before (PolicySums<double>).
+template <typename Terms, bool kCluster>
 __global__ void __launch_bounds__(1024)
-sum_terms_kernel(const PolicyTerms<F>* terms, int n, double beta, const int32_t* gave_up, double* partial, float* loss, float* stats) {
+sum_terms_kernel(const Terms* terms, int n, double beta, const int32_t* gave_up, double* partial, float* loss, float* stats) {
     grid_begin();
     if (kCluster) cluster_arrive();
     const bool failed = kCluster && gave_up != nullptr && *gave_up != 0;
-    PolicyTerms<double> sum = {0.0, 0.0, 0.0, 0.0};
+    PolicySums<double> sum = {0.0, 0.0, 0.0, 0.0};
 #pragma unroll 4
     for (long long i = (long long)blockIdx.x * blockDim.x + threadIdx.x; i < n; i += (long long)gridDim.x * blockDim.x) {
-        const PolicyTerms<F> t = terms[i];
-        add_terms(sum, PolicyTerms<double>{(double)t.gain, (double)t.kl, (double)t.clipped, (double)t.rho});
+        const Terms t = terms[i];
+        add_terms(sum, PolicySums<double>{(double)t.gain, (double)t.kl, (double)t.clipped, (double)t.rho});
     }
     leave_sum<kCluster>(block_sum(sum), beta, failed, partial, loss, stats);
 }
@@ -396,14 +415,14 @@ int launch_loss_weights(const int64_t* row_start, const uint8_t* mask, int32_t n
 }
 
 // Up to 32768 tokens, four a thread, and sums of up to 131072 are one cluster's work: one launch.
-int launch_sum_terms(const PolicyTerms<float>* terms, int n, double beta, const int32_t* gave_up, float* loss, float* stats, double* partial, cudaStream_t s) {
+int launch_sum_terms(const PolicyTerms* terms, int n, double beta, const int32_t* gave_up, float* loss, float* stats, double* partial, cudaStream_t s) {
     if (n <= 1 << 17) {
         const int ctas = max(1, min(8, (n + 1023) / 1024)), threads = max(32, min(1024, (n + 31) & ~31));
-        return launch_as(true, ctas, "sum_terms_kernel", sum_terms_kernel<float, true>, ctas, threads, 0, s, terms, n, beta, gave_up, partial, loss, stats);
+        return launch_as(true, ctas, "sum_terms_kernel", sum_terms_kernel<PolicyTerms, true>, ctas, threads, 0, s, terms, n, beta, gave_up, partial, loss, stats);
     }
     const int blocks = (int)min((long long)kMaxPartials, ((long long)n + 4095) / 4096);
-    SR_LAUNCH("sum_terms_kernel", sum_terms_kernel<float, false>, blocks, 1024, 0, s, terms, n, beta, gave_up, partial, loss, stats);
-    SR_LAUNCH("sum_terms_kernel", sum_terms_kernel<double, true>, 1, 1024, 0, s, reinterpret_cast<const PolicyTerms<double>*>(partial), blocks, beta, gave_up, partial, loss, stats);
+    SR_LAUNCH("sum_terms_kernel", sum_terms_kernel<PolicyTerms, false>, blocks, 1024, 0, s, terms, n, beta, gave_up, partial, loss, stats);
+    SR_LAUNCH("sum_terms_kernel", sum_terms_kernel<PolicySums<double>, true>, 1, 1024, 0, s, reinterpret_cast<const PolicySums<double>*>(partial), blocks, beta, gave_up, partial, loss, stats);
     return SR_OK;
 }
 
@@ -416,7 +435,7 @@ int launch_policy_loss(const PolicyBatch& b, const float* logp, int32_t n, float
     }
     const int blocks = (int)min((long long)(148 * 2), ((long long)n + 1023) / 1024);
     SR_LAUNCH("policy_loss_kernel", vec ? policy_loss_kernel<true, false> : policy_loss_kernel<false, false>, blocks, 256, 0, s, b, logp, d_logp, n, partial, loss, stats);
-    SR_LAUNCH("sum_terms_kernel", sum_terms_kernel<double, true>, 1, 1024, 0, s, reinterpret_cast<const PolicyTerms<double>*>(partial), blocks, b.beta, static_cast<const int32_t*>(nullptr), partial, loss, stats);
+    SR_LAUNCH("sum_terms_kernel", sum_terms_kernel<PolicySums<double>, true>, 1, 1024, 0, s, reinterpret_cast<const PolicySums<double>*>(partial), blocks, b.beta, static_cast<const int32_t*>(nullptr), partial, loss, stats);
     return SR_OK;
 }
 

@@ -16,15 +16,22 @@ struct PolicyBatch {
     int rows;
     double clip_low, clip_high, beta;
     float low, high, beta32;         // 1 - clip_low, 1 + clip_high, beta
+    float less_low, less_high;       // -clip_low, clip_high: the borders less 1
 };
 // What the loss reads of one token beside its log-probability.
 struct PolicyToken {
     float old_logp, ref_logp, adv, weight;
 };
 
-// Weighted terms of one token, or their sums.
-template <typename F>
+// Weighted terms of one token.  Advantages of a group add up to 0, so that the loss is a small difference of large gains: these
+// are not rounded to fp32.
 struct PolicyTerms {
+    double gain;
+    float kl, clipped, rho;
+};
+// Sums of them.
+template <typename F>
+struct PolicySums {
     F gain, kl, clipped, rho;
 };
 
@@ -146,13 +153,15 @@ static __device__ __noinline__ float far_expm1(float d) { return expm1f(d); }   
 //     e^d - 1 - d = 2^n q + (2^n r + (2^n - 1) - d),
 // whose second part is exactly 0 for n = 0: policies that nearly agree lose nothing.
 // For |d| <= 80, two numbers at a time: 2^n, r and q.
+// kLast: with the last term, which e^d - 1 by itself does not need (2^-26 of r).
+template <bool kLast>
 __device__ __forceinline__ void exp_parts(f32x2 d, f32x2& s, f32x2& r, f32x2& q) {
     const f32x2 z = fma2(d, two(1.44269504f), two(12582912.0f));           // 1.5 * 2^23: n stands in the lowest bits
     const f32x2 n = add2(z, two(-12582912.0f));
     r = fma2(n, two(-0.693359375f), d);            // ln 2 in two parts, the first with few bits: this product is exact
     r = fma2(n, two(2.12194440054690583e-4f), r);
-    f32x2 g = two(1.0f / 40320.0f);
-    g = fma2(g, r, two(1.0f / 5040.0f));
+    f32x2 g = two(1.0f / 5040.0f);
+    if (kLast) g = fma2(two(1.0f / 40320.0f), r, g);
     g = fma2(g, r, two(1.0f / 720.0f));
     g = fma2(g, r, two(1.0f / 120.0f));
     g = fma2(g, r, two(1.0f / 24.0f));
@@ -162,12 +171,26 @@ __device__ __forceinline__ void exp_parts(f32x2 d, f32x2& s, f32x2& r, f32x2& q)
     const auto power = [](float z) { return __uint_as_float((__float_as_uint(z) << 23) + 0x3F800000u); };
     s = two(power(low_of(z)), power(high_of(z)));
 }
+// e^d and e^d - 1, each to its own size.
+__device__ __forceinline__ void exp_near(f32x2 d, f32x2& e, f32x2& em1) {
+    f32x2 s, r, q;
+    exp_parts<false>(d, s, r, q);
+    const f32x2 rest = add2(r, q);
+    e = fma2(s, rest, s);
+    em1 = fma2(s, rest, add2(s, two(-1.0f)));
+}
 __device__ __forceinline__ void exp_less_line_near(f32x2 d, f32x2& em1, f32x2& kl) {
     f32x2 s, r, q;
-    exp_parts(d, s, r, q);
+    exp_parts<true>(d, s, r, q);
     const f32x2 less = add2(s, two(-1.0f));
     kl = fma2(s, q, fma2(d, two(-1.0f), fma2(s, r, less)));
     em1 = fma2(s, add2(r, q), less);
+}
+__device__ __forceinline__ float exp_less_one(float d) {
+    if (fabsf(d) > 80.0f) return far_expm1(d);
+    f32x2 e, em1;
+    exp_near(two(d, 0.0f), e, em1);
+    return low_of(em1);
 }
 __device__ __forceinline__ void exp_less_line(float d, float& em1, float& kl) {
     if (fabsf(d) > 80.0f) {                        // 2^n r may overflow before the sum does
@@ -181,22 +204,27 @@ __device__ __forceinline__ void exp_less_line(float d, float& em1, float& kl) {
     }
 }
 
-// Terms of a token that counts, and the gradient of its log-probability.  `lp` is fp32 where it came from memory, fp64
-// where it has just been computed.
+// The gradient of the log-probability of a token that counts, and what its terms are made of.  `lp` is fp32 where it came from memory,
+// fp64 where it has just been computed.
 //
 // Whether rho is past a border of the clip range would be lost in 32 bits (and a token on the wrong side has a wholly wrong
 // gradient): rho in fp32 is off by up to 2^-22 and |log rho| 2^-23 of itself, so within four and two times that of a border the
 // comparison is made again in fp64.
-__device__ __forceinline__ float ratio_margin(float delta) { return fmaf(fabsf(delta), 2.384185791015625e-7f, 9.5367431640625e-7f); }
+constexpr float kMargin = 9.5367431640625e-7f, kMarginSlope = 2.384185791015625e-7f;
+__device__ __forceinline__ float ratio_margin(float delta) { return fmaf(fabsf(delta), kMarginSlope, kMargin); }
 static __device__ __noinline__ double exact_ratio(double lp, double old_logp) { return exp(lp - old_logp); }      // rare as well
+struct PolicyParts {
+    float rho, delta, kl;            // delta = log rho
+    bool clipped;
+};
 template <typename F>
-__device__ __forceinline__ float policy_token(const PolicyBatch& b, const PolicyToken& k, F lp, PolicyTerms<float>& out) {
-    const float A = k.adv, w = k.weight;
-    float rho = lp == lp ? 1.0f : (float)lp;        // a NaN stays one
-    const float border = A > 0.0f ? b.high : b.low;
+__device__ __forceinline__ float policy_gradient(const PolicyBatch& b, const PolicyToken& k, F lp, PolicyParts& out) {
+    const float A = k.adv;
+    float rho = lp == lp ? 1.0f : (float)lp, delta = rho - 1.0f;         // a NaN stays one
     bool clipped = false;
     if (b.old_logp) {
-        const float delta = (float)(lp - (F)k.old_logp);
+        const float border = A > 0.0f ? b.high : b.low;
+        delta = (float)(lp - (F)k.old_logp);
         rho = expf(delta);
         clipped = A > 0.0f ? rho > border : A < 0.0f && rho < border;
         if (fabsf(rho - border) <= ratio_margin(delta) * border) {
@@ -204,23 +232,25 @@ __device__ __forceinline__ float policy_token(const PolicyBatch& b, const Policy
             clipped = A > 0.0f ? exact > 1.0 + b.clip_high : A < 0.0f && exact < 1.0 - b.clip_low;
         }
     }
-    const float gain = A == 0.0f ? 0.0f : A * (clipped ? border : rho);
-    float d_lp = clipped || A == 0.0f ? 0.0f : -gain;
+    float d_lp = clipped || A == 0.0f ? 0.0f : -A * rho;
     float kl = 0.0f;
     if (b.ref_logp) {
         float em1;
         exp_less_line((float)((F)k.ref_logp - lp), em1, kl);
         if (b.beta != 0.0) d_lp = fmaf(-b.beta32, em1, d_lp);
     }
-    out.gain = w * gain;
-    out.kl = w * kl;
-    out.clipped = clipped ? w : 0.0f;
-    out.rho = w * rho;
-    return w * d_lp;
+    out = PolicyParts{rho, delta, kl, clipped};
+    return k.weight * d_lp;
+}
+// Its terms.  rho - 1 is taken to its own size: see PolicyTerms.
+__device__ __forceinline__ PolicyTerms policy_terms(const PolicyBatch& b, const PolicyToken& k, const PolicyParts& p) {
+    const float A = k.adv, w = k.weight;
+    const double used = !p.clipped ? 1.0 + (double)exp_less_one(p.delta) : A > 0.0f ? 1.0 + b.clip_high : 1.0 - b.clip_low;
+    return PolicyTerms{A == 0.0f ? 0.0 : (double)w * (double)A * used, w * p.kl, p.clipped ? w : 0.0f, w * p.rho};
 }
 
 // The loss from the sums over all tokens.
-__device__ __forceinline__ void write_policy_loss(const PolicyTerms<double>& sum, double beta, float* loss, float* stats) {
+__device__ __forceinline__ void write_policy_loss(const PolicySums<double>& sum, double beta, float* loss, float* stats) {
     *loss = (float)(beta != 0.0 ? beta * sum.kl - sum.gain : -sum.gain);
     if (stats) {
         stats[0] = (float)sum.gain;
@@ -230,7 +260,7 @@ __device__ __forceinline__ void write_policy_loss(const PolicyTerms<double>& sum
     }
 }
 
-__device__ __forceinline__ void add_terms(PolicyTerms<double>& a, const PolicyTerms<double>& b) {
+__device__ __forceinline__ void add_terms(PolicySums<double>& a, const PolicySums<double>& b) {
     a.gain += b.gain;
     a.kl += b.kl;
     a.clipped += b.clipped;
@@ -238,11 +268,11 @@ __device__ __forceinline__ void add_terms(PolicyTerms<double>& a, const PolicyTe
 }
 
 // Sum over the threads of a CTA, in thread 0; every thread takes part.  The order depends on the thread count alone.
-__device__ __forceinline__ PolicyTerms<double> block_sum(PolicyTerms<double> v) {
-    __shared__ PolicyTerms<double> s_warp[32];
+__device__ __forceinline__ PolicySums<double> block_sum(PolicySums<double> v) {
+    __shared__ PolicySums<double> s_warp[32];
 #pragma unroll
     for (int off = 16; off > 0; off >>= 1) {
-        PolicyTerms<double> o;
+        PolicySums<double> o;
         o.gain = __shfl_xor_sync(0xFFFFFFFFu, v.gain, off);
         o.kl = __shfl_xor_sync(0xFFFFFFFFu, v.kl, off);
         o.clipped = __shfl_xor_sync(0xFFFFFFFFu, v.clipped, off);
@@ -263,12 +293,12 @@ int launch_loss_weights(const int64_t* row_start, const uint8_t* mask, int32_t n
                         double scale, float* weight, int64_t* counts, void* ws, cudaStream_t s);
 int launch_policy_loss(const PolicyBatch& b, const float* logp, int32_t n, float* loss, float* d_logp, float* stats, double* partial, cudaStream_t s);
 // Sums the terms of n tokens into loss and stats; NaN where *gave_up is set (NULL: it cannot be).
-int launch_sum_terms(const PolicyTerms<float>* terms, int n, double beta, const int32_t* gave_up, float* loss, float* stats, double* partial, cudaStream_t s);
+int launch_sum_terms(const PolicyTerms* terms, int n, double beta, const int32_t* gave_up, float* loss, float* stats, double* partial, cudaStream_t s);
 
 // logprob.cu
 struct StepScratch {
     double* partial;                 // [kMaxPartials][4]
-    PolicyTerms<float>* terms;       // [n_tokens]
+    PolicyTerms* terms;              // [n_tokens]
     int32_t* row_of;                 // [n_tokens], or the same memory as
     int4* list;                      // [n_tokens]
     int32_t* counters;               // [4]

@@ -144,12 +144,12 @@ int sr_policy_loss(const float* logp, const float* logp_old, const float* logp_r
     if (n_tokens > 0 && logp == nullptr) return SR_ERR_NULL;
     if (!aligned_4(logp, logp_old, logp_ref, d_logp, stats)) return SR_ERR_ALIGN;
     if (short_of(workspace, workspace_bytes, kPartialBytes)) return SR_ERR_WORKSPACE;
-    const PolicyBatch b{logp_old, logp_ref, adv, weight, row_start, mask, n_rollouts, clip_low, clip_high, beta, (float)(1.0 - clip_low), (float)(1.0 + clip_high), (float)beta};
+    const PolicyBatch b{logp_old, logp_ref, adv, weight, row_start, mask, n_rollouts, clip_low, clip_high, beta, (float)(1.0 - clip_low), (float)(1.0 + clip_high), (float)beta, (float)-clip_low, (float)clip_high};
     return launch_policy_loss(b, logp, n_tokens, loss, d_logp, stats, static_cast<double*>(workspace), static_cast<cudaStream_t>(stream));
 }
 
 size_t sr_policy_loss_logits_workspace_bytes(int32_t n_tokens) {
-    return n_tokens < 0 ? 0 : kPartialBytes + align_up((size_t)n_tokens * (sizeof(PolicyTerms<float>) + sizeof(int4)) + 4 * sizeof(int32_t), 256);
+    return n_tokens < 0 ? 0 : kPartialBytes + align_up((size_t)n_tokens * (sizeof(PolicyTerms) + sizeof(int4)) + 4 * sizeof(int32_t), 256);
 }
 
 int sr_policy_loss_logits(const void* logits, int32_t dtype, int32_t n_tokens, int32_t vocab, int64_t pitch, const int32_t* targets, const float* logp_old,
@@ -165,13 +165,13 @@ int sr_policy_loss_logits(const void* logits, int32_t dtype, int32_t n_tokens, i
     rc = check_gradient(logits, dtype, n_tokens, vocab, pitch, d_logits, d_pitch);
     if (rc != SR_OK) return rc;
     if (short_of(workspace, workspace_bytes, sr_policy_loss_logits_workspace_bytes(n_tokens))) return SR_ERR_WORKSPACE;
-    const PolicyBatch b{logp_old, logp_ref, adv, weight, row_start, mask, n_rollouts, clip_low, clip_high, beta, (float)(1.0 - clip_low), (float)(1.0 + clip_high), (float)beta};
+    const PolicyBatch b{logp_old, logp_ref, adv, weight, row_start, mask, n_rollouts, clip_low, clip_high, beta, (float)(1.0 - clip_low), (float)(1.0 + clip_high), (float)beta, (float)-clip_low, (float)clip_high};
     StepScratch ws;
     ws.partial = static_cast<double*>(workspace);
-    ws.terms = reinterpret_cast<PolicyTerms<float>*>(static_cast<char*>(workspace) + kPartialBytes);
-    ws.list = reinterpret_cast<int4*>(ws.terms + n_tokens);
+    ws.list = reinterpret_cast<int4*>(static_cast<char*>(workspace) + kPartialBytes);
     ws.row_of = reinterpret_cast<int32_t*>(ws.list);
-    ws.counters = reinterpret_cast<int32_t*>(ws.list + n_tokens);
+    ws.terms = reinterpret_cast<PolicyTerms*>(ws.list + n_tokens);
+    ws.counters = reinterpret_cast<int32_t*>(ws.terms + n_tokens);
     return launch_policy_loss_logits(LogitsArgs{logits, dtype, n_tokens, vocab, pitch, targets, temperature}, b, loss, logp, d_logits, d_pitch, stats, status, ws,
                                      static_cast<cudaStream_t>(stream));
 }

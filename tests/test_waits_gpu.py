@@ -34,13 +34,22 @@ __global__ void wait_kernel(unsigned long long limit, int arrives, int* out) {
     __syncthreads();
     if (threadIdx.x == 0) out[0] = gave_up;
 }
+__global__ void ones_kernel(PolicyTerms* terms, int n) {
+    const int i = blockIdx.x * 256 + threadIdx.x;
+    if (i < n) terms[i] = PolicyTerms{1, 1, 1, 1};
+}
+}
+extern "C" int terms_bytes(int n) { return n * (int)sizeof(sr::PolicyTerms); }
+extern "C" int make_ones(void* terms, int n, void* s) {
+    sr::ones_kernel<<<n / 256 + 1, 256, 0, (cudaStream_t)s>>>((sr::PolicyTerms*)terms, n);
+    return (int)cudaGetLastError();
 }
 extern "C" int run_wait(long long limit, int arrives, int* out, void* s) {
     sr::wait_kernel<<<1, 64, 0, (cudaStream_t)s>>>((unsigned long long)limit, arrives, out);
     return (int)cudaGetLastError();
 }
 extern "C" int run_sum(const void* terms, int n, double beta, const int* gave_up, float* loss, float* stats, double* partial, void* s) {
-    return sr::launch_sum_terms((const sr::PolicyTerms<float>*)terms, n, beta, gave_up, loss, stats, partial, (cudaStream_t)s);
+    return sr::launch_sum_terms((const sr::PolicyTerms*)terms, n, beta, gave_up, loss, stats, partial, (cudaStream_t)s);
 }
 """
 
@@ -78,7 +87,8 @@ def test_a_wait_ends_and_says_so(lib):
 @pytest.mark.gpu
 @pytest.mark.parametrize("n", [0, 1, 1000, 65536, 200_000])
 def test_a_loss_with_rows_missing_is_nan(lib, n):
-    terms = torch.ones(max(n, 1), 4, device=DEV)
+    terms = torch.empty(lib.terms_bytes(n + 1), dtype=torch.uint8, device=DEV)
+    assert lib.make_ones(address(terms), n, stream()) == 0
     partial = torch.empty(1184 * 4, dtype=torch.float64, device=DEV)
     loss, stats = torch.full((1,), 7.0, device=DEV), torch.full((4,), 7.0, device=DEV)
     for flag, nan in ((None, False), (0, False), (1, True)):

@@ -11,10 +11,10 @@
 //
 // How a row is taken, by its length and by how many there are (held_row, ctas_of_row, ring_ctas):
 //   - up to 40 KB a CTA it is held in registers: all loads on their way together, nothing rescaled, and the loss writes the gradient
-//     from them (1200 rows of 4096 fp32: 11 us of a step's 18.7, 39 MB);
+//     from them (1200 rows of 4096 fp32: 11 us of a step's 18.9, 39 MB);
 //   - longer, it streams through the registers, a batch ahead (4096 rows of 151936 bf16, a quarter masked: 152 to 163 us, 5.7 to 6.1 TB/s);
 //   - the loss, which needs it twice, holds it in the shared memory of a cluster (the ring below: the same rows and zeros for those masked
-//     405 us, 2.2 GB; from memory twice 536).
+//     409 to 416 us, 2.2 GB; from memory twice 536).
 // Where rows alone do not fill the GPU (fewer than two CTAs an SM), a cluster takes one and its sums meet in shared memory: 8 rows
 // of 151936 take 4.4 us.  Where they do, more CTAs a row cost more than the shorter last wave gives (4096 rows, two a row: 189 us).
 #include <cooperative_groups.h>
@@ -619,8 +619,8 @@ held_policy_loss_kernel(PolicyBatch b, const T* logits, int vocab, long long pit
 // the cluster; one warp turns these into the row's gradient and finds out about the row to come; and the eight write the
 // gradient from the same chunks, each of which is then free for the next row.  CTAs stay and take row after row: the copies never
 // wait for the sums of a row, and two CTAs an SM take turns at computing and at waiting.
-// Read once, written once, but not at the rate of a copy (2048 rows of 32000 bf16 61 us, 4.3 TB/s; fp32 93, 5.6): 15 instructions an
-// element (55 % of the issue slots), two of them ex2 (65 % of its rate), and two microseconds a row in which its sums meet.
+// Read once, written once, but not at the rate of a copy (2048 rows of 32000 bf16 62 us, 4.2 TB/s; fp32 93, 5.6): 15 instructions an
+// element (54 % of the issue slots), two of them ex2 (64 % of its rate), and two microseconds a row in which its sums meet.
 constexpr int kRingThreads = 256, kRingWarps = kRingThreads / 32;
 constexpr int kChunkVecs = 2 * kRingThreads;       // two vectors a thread: with one, more instructions went into finding them than into the terms
 constexpr int kChunk = kChunkVecs * 16;            // bytes
@@ -1096,7 +1096,11 @@ bool alike(const LogitsArgs& a, const void* d_logits, int64_t d_pitch) {
 
 // CTAs to a row of the ring kernel, or 0: rows too long for it, short enough to be held in registers, or too few for its CTAs, which
 // stay.  Held, 1200 rows of 20000 bf16 take 31 us, through the ring 36.  160 rows of 50021 in clusters of two are a row and a bit for
-// each: 23 us, and 20 from memory twice; 300 of them 27, and 31.
+// each: 23 us, and 20 from memory twice; 300 of them 27, and 31.  Where rows ask for clusters of eight (above 163840 numbers of 16 bits)
+// slices are short and the sums meet as often, which still pays: 1024 rows of 200000 216 us, from memory twice 233; 256000 234, and
+// 285 (of 163840 in clusters of four 139, and 187).  Rows of more than eight slices have no ring: 600 of 327680 169 us, of 327696 258.
+// Its list is one cluster's work, kept to 65536 tokens: so many rows of 20600 take 1141 us, from memory twice 1189; twice as many take
+// 2403, and with a longer list would take 2265.
 int ring_ctas(int n_tokens, int vocab, int elem) {
     const long long vecs = ((long long)vocab * elem + 15) / 16;
     if (n_tokens > kListTokens || vecs <= kHeldThreads * kMostVecs) return 0;

@@ -5,8 +5,9 @@
 // of dependent loads (8192 rollouts, 5.2M tokens: 8 us; 80 rollouts in one launch: 3).
 //
 // Loss.  Four tokens a thread, 17 bytes a token.  A warp searches row_start once, for the first of its tokens, and moves on from
-// there: 128 tokens mostly lie in one rollout or a few, whose starts the lanes look at together.  5.2M tokens take 31 us, 2.9 TB/s:
-// bound by 94 instructions a token and their latency, with one or two lots of 128 ahead; three CTAs an SM take as long as two, four longer.
+// there: 128 tokens mostly lie in one rollout or a few, whose starts the lanes look at together.  5.2M tokens take 28 us, 3.1 TB/s:
+// bound by 97 instructions a token and their latency, with one or two lots of 128 ahead; with fewer registers three CTAs an SM took as
+// long as two, four longer.
 // With a search and branches for every token it took 60.
 #include <cooperative_groups.h>
 #include <math_constants.h>

@@ -149,7 +149,7 @@ struct RowWalk {
 static __device__ __noinline__ float far_expm1(float d) { return expm1f(d); }       // rare: kept out of the loops
 
 // e^d - 1 and e^d - 1 - d.  With d = n ln 2 + r and |r| <= ln(2) / 2, e^r - 1 = r + q with q = r^2 times the Taylor series of
-// (e^r - 1 - r) / r^2, cut where the next term is below 2^-27 of the sum; then
+// (e^r - 1 - r) / r^2, cut where the next term is below 2^-27 of the sum (ln 2 in two parts is Cody and Waite's); then
 //     e^d - 1 - d = 2^n q + (2^n r + (2^n - 1) - d),
 // whose second part is exactly 0 for n = 0: policies that nearly agree lose nothing.
 // For |d| <= 80, two numbers at a time: 2^n, r and q.

@@ -45,10 +45,10 @@ extern "C" {
 #define SR_ERR_BAD_MODE (-8)       /* unknown norm_mode or loss mode */
 #define SR_ERR_SCRATCH_LIMIT (-9)  /* sr_gate_noalloc: problem needs more than the built-in scratch */
 #define SR_ERR_BAD_OFFSETS (-10)   /* sr_gate_host_packed: row_start malformed */
-#define SR_ERR_BAD_SIZE (-11)      /* sr_train.h: negative count, empty vocabulary, pitch < vocab, 32 TB of gradients */
-#define SR_ERR_BAD_DTYPE (-12)     /* sr_train.h: unknown element type */
-#define SR_ERR_BAD_VALUE (-13)     /* sr_train.h: temperature, clip range, beta, scale or max_norm out of range */
-#define SR_ERR_OVERLAP (-14)       /* sr_train.h: buffers that must not overlap do */
+#define SR_ERR_BAD_SIZE (-11)      /* sr_train.h, sr_tokens.h: negative count, empty vocabulary, pitch < vocab, 32 TB of gradients */
+#define SR_ERR_BAD_DTYPE (-12)     /* sr_train.h, sr_tokens.h: unknown element type, or two that do not go together */
+#define SR_ERR_BAD_VALUE (-13)     /* sr_train.h, sr_tokens.h: temperature, clip range, beta, scale or max_norm out of range */
+#define SR_ERR_OVERLAP (-14)       /* sr_train.h, sr_tokens.h: buffers that must not overlap do */
 
 /* limits */
 #define SR_MAX_N 32                /* rollouts per group */
@@ -66,9 +66,10 @@ extern "C" {
 #define SR_STATUS_NEG_LEN 1        /* a negative length was treated as 0 */
 #define SR_STATUS_STEP_OVERFLOW 2  /* an action arrived for a rollout already at max_steps; ignored */
 #define SR_STATUS_BAD_STATE 4      /* incremental state header does not match the call; step skipped */
-#define SR_STATUS_BAD_TARGET 8     /* a target token >= vocab was treated as one that does not count */
+#define SR_STATUS_BAD_TARGET 8     /* a token >= vocab was treated as one that does not count */
 #define SR_STATUS_NONFINITE 16     /* the gradient norm is not finite; gradients were not scaled */
 #define SR_STATUS_TIMEOUT 32       /* a kernel gave up a wait: loss and stats are NaN, other outputs undefined */
+#define SR_STATUS_BAD_INDEX 64     /* a mask_row >= n_masks was treated as none */
 
 int sr_version(void);
 const char* sr_strerror(int code);      /* static string */

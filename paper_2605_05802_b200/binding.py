@@ -1,4 +1,5 @@
-"""Thin binding of the sr_gate C ABI (include/sr_gate.h, include/sr_train.h, include/sr_probe.h).
+"""Thin binding of the sr_gate C ABI (include/sr_gate.h, include/sr_train.h, include/sr_tokens.h,
+include/sr_probe.h).
 
 Argument marshalling only: every step of the path runs in the CUDA library.  The calls
 a program makes per batch or per step go through a compiled extension
@@ -29,6 +30,7 @@ SR_NORM_MAXLEN, SR_NORM_NONE = 0, 1
 SR_NO_ACTION = -(2 ** 31)
 SR_STATUS_NEG_LEN, SR_STATUS_STEP_OVERFLOW, SR_STATUS_BAD_STATE = 1, 2, 4
 SR_STATUS_BAD_TARGET, SR_STATUS_NONFINITE, SR_STATUS_TIMEOUT = 8, 16, 32
+SR_STATUS_BAD_INDEX = 64
 SR_DTYPE_F32, SR_DTYPE_BF16, SR_DTYPE_F16 = 0, 1, 2
 SR_LOSS_SUM, SR_LOSS_TOKEN_MEAN, SR_LOSS_ROLLOUT_MEAN = 0, 1, 2
 SR_MAX_N, SR_MAX_K, SR_MAX_INCR_STEPS = 32, 1024, 32
@@ -80,6 +82,14 @@ _SIGNATURES = {
     "sr_grad_norm": (ctypes.c_int, [_vp, _vp, _vp, _i32, _vp, _vp, _sz, _vp]),
     "sr_grad_norm_workspace_bytes": (_sz, [_i32]),
     "sr_clip_grads": (ctypes.c_int, [_vp, _vp, _vp, _i32, _vp, _f64, _vp, _vp, _vp]),
+    "sr_adjust_logits": (ctypes.c_int, [_vp, _i32, _i32, _i32, _i64, _vp, _i64, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _i64,
+                                        _vp, _vp, _vp, _i32, _i64, _vp, _vp, _i64, _vp, _vp]),
+    "sr_adjust_logits_backward": (ctypes.c_int, [_vp, _i32, _i32, _i32, _i64, _vp, _i64, _vp, _i64, _vp, _vp, _vp, _vp, _i32,
+                                                 _i64, _vp, _vp, _i64, _vp, _vp]),
+    "sr_embed_tokens": (ctypes.c_int, [_vp, _i32, _i32, _i32, _i64, _vp, _i32, _f64, _vp, _i32, _i64, _vp, _vp]),
+    "sr_embed_tokens_backward": (ctypes.c_int, [_vp, _i32, _i32, _i32, _i64, _vp, _i32, _f64, _vp, _i32, _i64, _i32, _vp, _vp,
+                                                _sz, _vp]),
+    "sr_embed_tokens_backward_workspace_bytes": (_sz, [_i32, _i32, _i32]),
     "sr_gate_stages": (ctypes.c_int, [_vp, _vp, _i32, _i32, _i32, _i32, _f64, _i32, _vp, _vp, _vp, _vp,
                                       _vp, _vp, _sz, _vp, _vp]),
     "sr_probe_int32": (ctypes.c_int, [_i32, _i32, _i32, _i32, _vp, _vp]),
@@ -384,6 +394,53 @@ def sr_clip_grads(grads, norm: torch.Tensor, max_norm: float, *, out=None, statu
                   stream=None) -> None:
     """grads times min(1, max_norm / (norm + 1e-6)), in place or into ``out`` (a list alike)."""
     _check(_native().sr_clip_grads(grads, norm, max_norm, out, status, stream))
+
+
+def sr_adjust_logits(logits: torch.Tensor, *, history: Optional[torch.Tensor] = None,
+                     history_start: Optional[torch.Tensor] = None, history_len: Optional[torch.Tensor] = None,
+                     prompt_len: Optional[torch.Tensor] = None, repetition: Optional[torch.Tensor] = None,
+                     presence: Optional[torch.Tensor] = None, frequency: Optional[torch.Tensor] = None,
+                     bias_token: Optional[torch.Tensor] = None, bias_value: Optional[torch.Tensor] = None,
+                     bias_start: Optional[torch.Tensor] = None, bias_len: Optional[torch.Tensor] = None,
+                     allowed: Optional[torch.Tensor] = None, mask_row: Optional[torch.Tensor] = None,
+                     out: torch.Tensor, status: Optional[torch.Tensor] = None, stream=None) -> None:
+    """logits [T, V] (float32, bfloat16 or float16; rows may lie apart) -> out, which may be the logits.
+
+    Row t's history is history[history_start[t]:][:history_len[t]] (int32 ids; int64 and int32 [T]), its first prompt_len[t]
+    ids the prompt; repetition, presence and frequency are float32 [T].  Its biases are entries bias_start[t] .. + bias_len[t]
+    of bias_token (int32) and bias_value (float32).  allowed int32 [masks, words]: bit v % 32 of word v // 32 of row
+    mask_row[t] (int32; negative: no mask; None: row t) says whether token v may be taken; the others become -inf."""
+    _check(_native().sr_adjust_logits(logits, history, history_start, history_len, prompt_len, repetition, presence, frequency,
+                                      bias_token, bias_value, bias_start, bias_len, allowed, mask_row, out, status, stream))
+
+
+def sr_adjust_logits_backward(d_out: torch.Tensor, logits: Optional[torch.Tensor], *, history: Optional[torch.Tensor] = None,
+                              history_start: Optional[torch.Tensor] = None, history_len: Optional[torch.Tensor] = None,
+                              repetition: Optional[torch.Tensor] = None, allowed: Optional[torch.Tensor] = None,
+                              mask_row: Optional[torch.Tensor] = None, d_logits: torch.Tensor,
+                              status: Optional[torch.Tensor] = None, stream=None) -> None:
+    """Gradient of sr_adjust_logits: d_out [T, V] -> d_logits, which may be d_out or the logits.  The logits are those that
+    sr_adjust_logits was given (not what it wrote), and may be None without a repetition penalty."""
+    _check(_native().sr_adjust_logits_backward(d_out, logits, history, history_start, history_len, repetition, allowed, mask_row,
+                                               d_logits, status, stream))
+
+
+def sr_embed_tokens(table: torch.Tensor, tokens: torch.Tensor, scale: float = 1.0, *, out: torch.Tensor,
+                    status: Optional[torch.Tensor] = None, stream=None) -> None:
+    """table [V, D], tokens int32 -> out [T, D] = scale * table[tokens], zeros for negative tokens.  Types are the same, or
+    the table's is float32."""
+    _check(_native().sr_embed_tokens(table, tokens, scale, out, status, stream))
+
+
+def sr_embed_tokens_backward_workspace_bytes(n_tokens: int, vocab: int, width: int) -> int:
+    return int(load().sr_embed_tokens_backward_workspace_bytes(n_tokens, vocab, width))
+
+
+def sr_embed_tokens_backward(d_out: torch.Tensor, tokens: torch.Tensor, scale: float = 1.0, *, d_table: torch.Tensor,
+                             accumulate: bool = False, workspace: torch.Tensor = None,
+                             status: Optional[torch.Tensor] = None, stream=None) -> None:
+    """d_out [T, D] -> d_table [V, D]: every row of it, or, with ``accumulate``, added to those of the tokens that were taken."""
+    _check(_native().sr_embed_tokens_backward(d_out, tokens, scale, d_table, int(accumulate), status, workspace, stream))
 
 
 def sr_probe_int32(variant: int, iters: int, blocks: int, threads: int, sink: torch.Tensor,

@@ -17,7 +17,7 @@ NATIVE = os.path.join(HERE, "_native.so")
 BINDING = os.path.join(CSRC, "torch_binding.cpp")
 SOURCES = ["api.cu", "gate_single.cu", "gate_multi.cu", "incremental.cu", "advantage.cu", "probe.cu",
            "gate_noalloc.cu", "signals.cu", "gate_packed.cu", "compact.cu", "train.cu", "logprob.cu",
-           "policy.cu", "grads.cu"]
+           "policy.cu", "grads.cu", "tokens.cu", "adjust.cu", "embed.cu"]
 
 
 def _stale(target: str, sources) -> bool:

@@ -18,6 +18,7 @@
 
 #include "sr_gate.h"
 #include "sr_probe.h"
+#include "sr_tokens.h"
 #include "sr_train.h"
 
 namespace {
@@ -605,6 +606,139 @@ PyObject* py_clip_grads(PyObject*, PyObject* const* argv, Py_ssize_t argc) {
     });
 }
 
+// ------------------------------------------------------------------ operators on token ids (sr_tokens.h)
+// Histories and masks, as both directions take them.
+struct Rules {
+    const int32_t *history, *history_len;
+    const int64_t* history_start;
+    int64_t n_history = 0, mask_pitch = 0;
+    const uint32_t* allowed;
+    const int32_t* mask_row;
+    int32_t n_masks = 0;
+    void histories(OneDevice& dev, Args& a, int32_t n) {
+        const at::Tensor* t = a.tensor("history");
+        history = on<int32_t>(dev, t, kI32, kAnySize, "history");
+        n_history = t ? t->numel() : 0;
+        if (n_history == 0) history = nullptr;
+        history_start = on<int64_t>(dev, a.tensor("history_start"), kI64, n, "history_start");
+        history_len = on<int32_t>(dev, a.tensor("history_len"), kI32, n, "history_len");
+    }
+    void masks(OneDevice& dev, Args& a, int32_t n, int32_t vocab) {
+        const at::Tensor* t = dev.add(a.tensor("allowed"), "allowed");
+        allowed = nullptr;
+        if (t) {
+            if (t->dim() != 2) raise(PyExc_ValueError, "allowed must be [masks, words]");
+            if (t->scalar_type() != kI32) raise(PyExc_TypeError, std::string("allowed: expected torch.int32, got ") + dtype_name(t->scalar_type()));
+            if (t->size(1) < ((int64_t)vocab + 31) / 32) raise(PyExc_ValueError, "allowed needs a bit for every token of the vocabulary");
+            if (t->size(1) > 1 && t->stride(1) != 1) raise(PyExc_ValueError, "allowed: the words of a mask must be consecutive");
+            n_masks = count32(t->size(0), "allowed");
+            mask_pitch = n_masks > 1 ? t->stride(0) : t->size(1);
+            allowed = static_cast<const uint32_t*>(t->data_ptr());
+        }
+        mask_row = on<int32_t>(dev, a.tensor("mask_row"), kI32, n, "mask_row");
+        if (t && !mask_row && n_masks < n) raise(PyExc_ValueError, "allowed needs a row for every row of logits, or mask_row");
+        if (n_masks == 0 && t && n > 0) raise(PyExc_ValueError, "allowed has no rows");
+    }
+};
+// [rows, width], rows apart by any pitch that does not make them overlap
+struct Rows {
+    void* data;
+    int32_t dtype, n, width;
+    int64_t pitch;
+    Rows(OneDevice& dev, const at::Tensor* t, const char* name, const char* shape) {
+        if (t == nullptr || t->dim() != 2) raise(PyExc_ValueError, std::string(name) + " must be " + shape);
+        dtype = dtype_code(*dev.add(t, name), name);
+        n = count32(t->size(0), name);
+        width = count32(t->size(1), name);
+        if (width > 1 && t->stride(1) != 1) raise(PyExc_ValueError, std::string(name) + ": the elements of a row must be consecutive");
+        pitch = n > 1 ? t->stride(0) : width;
+        data = t->data_ptr();
+    }
+};
+
+PyObject* py_adjust_logits(PyObject*, PyObject* const* argv, Py_ssize_t argc) {
+    return guarded(argv, argc, 17, [](Args& a) {
+        OneDevice dev;
+        const Logits x(dev, a.tensor("logits"), "logits");
+        Rules r;
+        r.histories(dev, a, x.n);
+        const int32_t* prompt = on<int32_t>(dev, a.tensor("prompt_len"), kI32, x.n, "prompt_len");
+        const float* repetition = on<float>(dev, a.tensor("repetition"), kF32, x.n, "repetition");
+        const float* presence = on<float>(dev, a.tensor("presence"), kF32, x.n, "presence");
+        const float* frequency = on<float>(dev, a.tensor("frequency"), kF32, x.n, "frequency");
+        const at::Tensor *bt = a.tensor("bias_token"), *bv = a.tensor("bias_value");
+        const int64_t n_bias = bv ? bv->numel() : 0;
+        const int32_t* bias_token = on<int32_t>(dev, bt, kI32, n_bias, "bias_token");
+        const float* bias_value = on<float>(dev, bv, kF32, kAnySize, "bias_value");
+        const int64_t* bias_start = on<int64_t>(dev, a.tensor("bias_start"), kI64, x.n, "bias_start");
+        const int32_t* bias_len = on<int32_t>(dev, a.tensor("bias_len"), kI32, x.n, "bias_len");
+        if (n_bias == 0) bias_value = nullptr;
+        r.masks(dev, a, x.n, x.vocab);
+        const Logits y = same_logits(dev, a.tensor("out"), x, "out");
+        int32_t* status = on<int32_t>(dev, a.tensor("status"), kI32, 1, "status");
+        void* s = a.stream();
+        return unlocked([&] { return sr_adjust_logits(x.data, x.dtype, x.n, x.vocab, x.pitch, r.history, r.n_history, r.history_start, r.history_len, prompt, repetition, presence, frequency, bias_token, bias_value, n_bias, bias_start, bias_len, r.allowed, r.n_masks, r.mask_pitch, r.mask_row, y.data, y.pitch, status, s); });
+    });
+}
+
+PyObject* py_adjust_logits_backward(PyObject*, PyObject* const* argv, Py_ssize_t argc) {
+    return guarded(argv, argc, 11, [](Args& a) {
+        OneDevice dev;
+        const Logits d(dev, a.tensor("d_out"), "d_out");
+        const at::Tensor* xt = a.tensor("logits");
+        void* x = nullptr;
+        int64_t pitch = d.vocab;
+        if (xt) {
+            const Logits l = same_logits(dev, xt, d, "logits");
+            x = l.data;
+            pitch = l.pitch;
+        }
+        Rules r;
+        r.histories(dev, a, d.n);
+        const float* repetition = on<float>(dev, a.tensor("repetition"), kF32, d.n, "repetition");
+        r.masks(dev, a, d.n, d.vocab);
+        const Logits dx = same_logits(dev, a.tensor("d_logits"), d, "d_logits");
+        int32_t* status = on<int32_t>(dev, a.tensor("status"), kI32, 1, "status");
+        void* s = a.stream();
+        return unlocked([&] { return sr_adjust_logits_backward(d.data, d.dtype, d.n, d.vocab, d.pitch, x, pitch, r.history, r.n_history, r.history_start, r.history_len, repetition, r.allowed, r.n_masks, r.mask_pitch, r.mask_row, dx.data, dx.pitch, status, s); });
+    });
+}
+
+PyObject* py_embed_tokens(PyObject*, PyObject* const* argv, Py_ssize_t argc) {
+    return guarded(argv, argc, 6, [](Args& a) {
+        OneDevice dev;
+        const Rows table(dev, a.tensor("table"), "table", "[vocabulary, width]");
+        const at::Tensor* tt = a.tensor("tokens");
+        const double scale = a.real();
+        const Rows out(dev, a.tensor("out"), "out", "[tokens, width]");
+        if (out.width != table.width) raise(PyExc_ValueError, "out must have the table's width");
+        const int32_t* tokens = on<int32_t>(dev, tt, kI32, out.n, "tokens");
+        if (tt && tt->numel() != out.n) raise(PyExc_ValueError, "out must have a row for every token");
+        int32_t* status = on<int32_t>(dev, a.tensor("status"), kI32, 1, "status");
+        void* s = a.stream();
+        return unlocked([&] { return sr_embed_tokens(table.data, table.dtype, table.n, table.width, table.pitch, tokens, out.n, scale, out.data, out.dtype, out.pitch, status, s); });
+    });
+}
+
+PyObject* py_embed_tokens_backward(PyObject*, PyObject* const* argv, Py_ssize_t argc) {
+    return guarded(argv, argc, 8, [](Args& a) {
+        OneDevice dev;
+        const Rows d(dev, a.tensor("d_out"), "d_out", "[tokens, width]");
+        const at::Tensor* tt = a.tensor("tokens");
+        const int32_t* tokens = on<int32_t>(dev, tt, kI32, d.n, "tokens");
+        if (tt && tt->numel() != d.n) raise(PyExc_ValueError, "d_out must have a row for every token");
+        const double scale = a.real();
+        const Rows table(dev, a.tensor("d_table"), "d_table", "[vocabulary, width]");
+        if (d.width != table.width) raise(PyExc_ValueError, "d_table must have d_out's width");
+        const int32_t accumulate = a.integer();
+        int32_t* status = on<int32_t>(dev, a.tensor("status"), kI32, 1, "status");
+        size_t bytes;
+        void* ws = scratch_on(dev, a, bytes);
+        void* s = a.stream();
+        return unlocked([&] { return sr_embed_tokens_backward(d.data, d.dtype, d.n, d.width, d.pitch, tokens, table.n, scale, table.data, table.dtype, table.pitch, accumulate, status, ws, bytes, s); });
+    });
+}
+
 #define SR_METHOD(name) {"sr_" #name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(py_##name)), METH_FASTCALL, nullptr}
 PyMethodDef g_methods[] = {
     SR_METHOD(gate), SR_METHOD(gate_noalloc), SR_METHOD(gate_decide), SR_METHOD(gate_host),
@@ -612,7 +746,8 @@ PyMethodDef g_methods[] = {
     SR_METHOD(gate_or_rule), SR_METHOD(group_signals), SR_METHOD(batch_stats),
     SR_METHOD(kept_groups), SR_METHOD(grpo_advantage), SR_METHOD(token_logprob), SR_METHOD(token_logprob_backward),
     SR_METHOD(loss_weights), SR_METHOD(policy_loss), SR_METHOD(policy_loss_logits), SR_METHOD(grad_norm),
-    SR_METHOD(clip_grads), {nullptr, nullptr, 0, nullptr}};
+    SR_METHOD(clip_grads), SR_METHOD(adjust_logits), SR_METHOD(adjust_logits_backward), SR_METHOD(embed_tokens),
+    SR_METHOD(embed_tokens_backward), {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_native", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -4,22 +4,12 @@
 #include <algorithm>
 #include <new>
 
+#include "checks.cuh"
 #include "policy.cuh"
 
 using namespace sr;
 
 namespace {
-
-bool aligned(const void* p, size_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
-
-// Whether all of these (NULL or not) lie on the boundary of a 32-bit number.
-template <typename... P>
-bool aligned_4(const P*... p) { return (aligned(p, 4) && ...); }
-
-bool short_of(const void* ws, size_t have, size_t need) { return ws == nullptr || have < need || !aligned(ws, 16); }
-
-constexpr double kLargest = 3.4028234663852886e38;   // what fp32 holds
-constexpr int64_t kMaxPitch = int64_t(1) << 31;      // n_tokens * pitch * 4 bytes stay below 2^64
 
 // What every call on logits has in common.
 int check_logits(const void* logits, int32_t dtype, int32_t n_tokens, int32_t vocab, int64_t pitch, const int32_t* targets, double temperature) {
@@ -30,22 +20,6 @@ int check_logits(const void* logits, int32_t dtype, int32_t n_tokens, int32_t vo
     if (n_tokens > 0 && (logits == nullptr || targets == nullptr)) return SR_ERR_NULL;
     if (!aligned(logits, dtype_bytes(dtype)) || !aligned(targets, 4)) return SR_ERR_ALIGN;
     return SR_OK;
-}
-
-// d_logits is the logits themselves, or none of its rows meets one of theirs.
-int check_gradient(const void* logits, int32_t dtype, int32_t n_tokens, int32_t vocab, int64_t pitch, const void* d_logits, int64_t d_pitch) {
-    if (d_pitch < vocab || d_pitch > kMaxPitch) return SR_ERR_BAD_SIZE;
-    if (n_tokens == 0) return SR_OK;
-    if (d_logits == nullptr) return SR_ERR_NULL;
-    const int64_t size = dtype_bytes(dtype);
-    if (!aligned(d_logits, (size_t)size)) return SR_ERR_ALIGN;
-    const uint64_t a = reinterpret_cast<uintptr_t>(logits), b = reinterpret_cast<uintptr_t>(d_logits);
-    const auto bytes = [&](int64_t row) { return ((uint64_t)(n_tokens - 1) * (uint64_t)row + (uint64_t)vocab) * (uint64_t)size; };       // below 2^64
-    const uint64_t a_end = a + bytes(pitch), b_end = b + bytes(d_pitch);
-    if (a_end <= b || b_end <= a) return SR_OK;
-    if (pitch != d_pitch) return n_tokens == 1 && a == b ? SR_OK : SR_ERR_OVERLAP;
-    const int64_t off = ((((int64_t)(b - a)) / size) % pitch + pitch) % pitch;              // column of the one in a row of the other
-    return a == b || (off >= vocab && off + vocab <= pitch) ? SR_OK : SR_ERR_OVERLAP;
 }
 
 int check_policy(const float* adv, const float* weight, const int64_t* row_start, int32_t n_rollouts, double clip_low, double clip_high, double beta, const float* loss) {
@@ -111,7 +85,7 @@ int sr_token_logprob_backward(const void* logits, int32_t dtype, int32_t n_token
     if (rc != SR_OK) return rc;
     if (n_tokens > 0 && (row_stats == nullptr || d_logp == nullptr || (d_entropy != nullptr && entropy == nullptr))) return SR_ERR_NULL;
     if (!aligned_4(row_stats, entropy, d_logp, d_entropy)) return SR_ERR_ALIGN;
-    rc = check_gradient(logits, dtype, n_tokens, vocab, pitch, d_logits, d_pitch);
+    rc = check_rows(logits, pitch, d_logits, d_pitch, dtype, n_tokens, vocab);
     if (rc != SR_OK) return rc;
     return launch_token_logprob_backward(LogitsArgs{logits, dtype, n_tokens, vocab, pitch, targets, temperature}, row_stats, entropy, d_logp, d_entropy, d_logits, d_pitch,
                                          static_cast<cudaStream_t>(stream));
@@ -162,7 +136,7 @@ int sr_policy_loss_logits(const void* logits, int32_t dtype, int32_t n_tokens, i
     if (rc != SR_OK) return rc;
     if (n_tokens > 0 && logp == nullptr) return SR_ERR_NULL;
     if (!aligned_4(logp, logp_old, logp_ref, stats, status)) return SR_ERR_ALIGN;
-    rc = check_gradient(logits, dtype, n_tokens, vocab, pitch, d_logits, d_pitch);
+    rc = check_rows(logits, pitch, d_logits, d_pitch, dtype, n_tokens, vocab);
     if (rc != SR_OK) return rc;
     if (short_of(workspace, workspace_bytes, sr_policy_loss_logits_workspace_bytes(n_tokens))) return SR_ERR_WORKSPACE;
     const PolicyBatch b{logp_old, logp_ref, adv, weight, row_start, mask, n_rollouts, clip_low, clip_high, beta, (float)(1.0 - clip_low), (float)(1.0 + clip_high), (float)beta, (float)-clip_low, (float)clip_high};

@@ -63,39 +63,40 @@ Spread spread(int width, int cols, int most) {
 }
 
 // ------------------------------------------------------------------------------------------------- forward
-template <typename Table, typename Out, int kCols>
+// A group of `across` threads takes kRows tokens at a time: their ids first, then their rows, so that as many loads are in flight.
+template <typename Table, typename Out, int kCols, int kRows>
 __global__ void __launch_bounds__(kThreads)
-embed_kernel(const __grid_constant__ EmbedArgs a, int across) {
+embed_kernel(const __grid_constant__ EmbedArgs a, int across, int tiles) {
     grid_begin();
-    const int groups = kThreads / across, lane = threadIdx.x & (across - 1);
-    const int64_t t = (int64_t)blockIdx.x * groups + threadIdx.x / across;
-    if (t >= a.n_tokens) return;
-    const int id = a.tokens[t];
-    const bool taken = id >= 0 && id < a.vocab;
-    if (id >= a.vocab && lane == 0 && a.status) atomicOr(a.status, SR_STATUS_BAD_TARGET);
-    const Table* row = static_cast<const Table*>(a.table) + (taken ? (int64_t)id * a.table_pitch : 0);
-    Out* out = static_cast<Out*>(a.out) + t * a.pitch;
-    constexpr int kAhead = 4;
-    for (int c0 = lane * kCols; c0 < a.width; c0 += kAhead * across * kCols) {
-        Cols<Table, kCols> v[kAhead];
+    const int groups = kThreads / across, tile = blockIdx.x % tiles;
+    const int c = (tile * across + (threadIdx.x & (across - 1))) * kCols;
+    const int64_t t0 = ((int64_t)(blockIdx.x / tiles) * groups + threadIdx.x / across) * kRows;
+    if (c >= a.width) return;
+    int id[kRows];
+    bool bad = false;
 #pragma unroll
-        for (int k = 0; k < kAhead; ++k) {
-            const int c = c0 + k * across * kCols;
-            if (taken && c < a.width) v[k].load(row + c);
-            else v[k].zero();
-        }
-#pragma unroll
-        for (int k = 0; k < kAhead; ++k) {
-            const int c = c0 + k * across * kCols;
-            if (c >= a.width) break;
-            float x[kCols];
-#pragma unroll
-            for (int e = 0; e < kCols; ++e) x[e] = taken ? a.scale * v[k].at(e) : 0.0f;
-            Cols<Out, kCols> o;
-            o.set(x);
-            o.store(out + c);
-        }
+    for (int k = 0; k < kRows; ++k) {
+        id[k] = t0 + k < a.n_tokens ? a.tokens[t0 + k] : -1;
+        bad |= id[k] >= a.vocab;
+        if (id[k] >= a.vocab) id[k] = -1;
     }
+    Cols<Table, kCols> v[kRows];
+#pragma unroll
+    for (int k = 0; k < kRows; ++k) {
+        if (id[k] >= 0) v[k].load(static_cast<const Table*>(a.table) + (int64_t)id[k] * a.table_pitch + c);
+        else v[k].zero();
+    }
+#pragma unroll
+    for (int k = 0; k < kRows; ++k) {
+        if (t0 + k >= a.n_tokens) break;
+        float x[kCols];
+#pragma unroll
+        for (int e = 0; e < kCols; ++e) x[e] = id[k] >= 0 ? a.scale * v[k].at(e) : 0.0f;
+        Cols<Out, kCols> o;
+        o.set(x);
+        o.store(static_cast<Out*>(a.out) + (t0 + k) * a.pitch + c);
+    }
+    if (bad && c == 0 && a.status) atomicOr(a.status, SR_STATUS_BAD_TARGET);
 }
 
 // ------------------------------------------------------------------------------------------------- sorting
@@ -333,8 +334,16 @@ int cols_of(int most, const void* p, int64_t pitch, int size_p, const void* q, i
 template <typename Table, typename Out, int kCols>
 int embed_with(const EmbedArgs& a, cudaStream_t s) {
     const Spread sp = spread(a.width, kCols, kThreads);
-    const int groups = kThreads / sp.across;
-    SR_LAUNCH("embed_kernel", (embed_kernel<Table, Out, kCols>), (a.n_tokens - 1) / groups + 1, kThreads, 0, s, a, sp.across);
+    const auto ctas = [&](int rows) { return (((int64_t)a.n_tokens - 1) / (kThreads / sp.across * rows) + 1) * sp.tiles; };
+    // as many rows to a thread as leave the GPU a wave of CTAs
+    if (ctas(8) >= 148 * 6) {
+        if (ctas(8) > INT32_MAX) return SR_ERR_BAD_SIZE;
+        SR_LAUNCH("embed_kernel", (embed_kernel<Table, Out, kCols, 8>), (int)ctas(8), kThreads, 0, s, a, sp.across, sp.tiles);
+    } else if (ctas(2) >= 148 * 6) {
+        SR_LAUNCH("embed_kernel", (embed_kernel<Table, Out, kCols, 2>), (int)ctas(2), kThreads, 0, s, a, sp.across, sp.tiles);
+    } else {
+        SR_LAUNCH("embed_kernel", (embed_kernel<Table, Out, kCols, 1>), (int)ctas(1), kThreads, 0, s, a, sp.across, sp.tiles);
+    }
     return SR_OK;
 }
 template <typename Table, typename Out>

@@ -1,8 +1,9 @@
 """The operators on token ids in 64 bits, from their formulas, and how far a kernel may be from them.
 
 A rounding to nearest is off by half a step: 2^-24 of the value in fp32, eps(type) / 2 at the end, where the smallest number of the type is the
-least step.  Adjusted logits are at most four fp32 operations, each of them on numbers no larger than S = |x'| + |f c| + |p| + |b|: 4 x 2^-24 S,
-the largest of x / r and x r for x'.  A sum of n fp32 terms in any order is within (n - 1) 2^-24 (1 + n 2^-24) of the sum of their sizes; scaling
+least step.  Adjusted logits are at most four fp32 operations, each of them on numbers no larger than S = |x'| + |f c| + |p| + |b|, x' being
+x / r or x r: 4 x 2^-24 S.  For 16-bit logits x / r may be x times the rounded 1 / r, a fifth rounding of x': 5 x 2^-24 S; and for
+gradients two instead of one.  A sum of n fp32 terms in any order is within (n - 1) 2^-24 (1 + n 2^-24) of the sum of their sizes; scaling
 it, and adding what stood there, is a rounding each."""
 import numpy as np
 import torch
@@ -47,7 +48,7 @@ def adjust(x, hist=None, start=None, length=None, prompt=None, rep=None, pres=No
                 size[t, v] += abs(b)
                 touched[t, v] = True
     eps = torch.finfo(out_dtype).eps
-    bound = np.where(touched, 2.0 ** -22 * size * (1 + eps) + eps / 2 * np.abs(np.nan_to_num(y, nan=0.0, posinf=0.0, neginf=0.0)) + SMALLEST.get(out_dtype, 0.0), 0.0)
+    bound = np.where(touched, (4 if out_dtype == torch.float32 else 5) * 2.0 ** -24 * size * (1 + eps) + eps / 2 * np.abs(np.nan_to_num(y, nan=0.0, posinf=0.0, neginf=0.0)) + SMALLEST.get(out_dtype, 0.0), 0.0)
     if allowed is not None:
         for t in range(T):
             m = t if mask_row is None else int(mask_row[t])
@@ -74,7 +75,7 @@ def adjust_gradient(d, x, hist=None, start=None, length=None, rep=None, allowed=
             if 0 <= m < len(allowed):
                 dx[t, ~allowed[m]] = 0.0
     eps = torch.finfo(d.dtype).eps
-    bound = np.where(touched, (2.0 ** -24 * (1 + eps) + eps / 2) * np.abs(dx) + SMALLEST[d.dtype], 0.0)
+    bound = np.where(touched, ((1 if d.dtype == torch.float32 else 2) * 2.0 ** -24 * (1 + eps) + eps / 2) * np.abs(dx) + SMALLEST[d.dtype], 0.0)
     return torch.from_numpy(dx), torch.from_numpy(bound)
 
 

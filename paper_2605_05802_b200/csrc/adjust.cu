@@ -7,8 +7,6 @@
 // owner of the new token notes it, and the CTA's threads go from row to row without a barrier.  Vectors pass through registers once, the
 // next row's on their way meanwhile; those of which no token is allowed are not read.  Counts are whole numbers and a token's bias is the
 // largest index in the list, so no order of atomics enters a result.
-#include <stdlib.h>
-
 #include <algorithm>
 
 #include "tokens.cuh"
@@ -18,11 +16,14 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kVecs = 4;                         // a thread's, of a row of the slice
-constexpr int kIdsAhead = 1536;                  // of the next row's history, and of its biases each: copied while this row is written
+constexpr int kIdsAhead = 1536;                  // of the next row's history, and of its biases: copied while this row is written
 constexpr int kBiasesAhead = 512;
-constexpr uint32_t kInPrompt = 0x80000000u;      // of a count: seen in the prompt,
-constexpr uint32_t kBiased = 0x40000000u;        // in the bias list; the rest: how often behind the prompt
 constexpr int kMostLength = 0x3FFFFFFF;          // of a history
+constexpr int kMostBiases = 0xFFFF;              // of a list
+// A token's count, 16 bits: seen in the prompt, in the bias list, and how often behind the prompt.  From kMany on, give or take what
+// the CTA's threads add at once, occurrences are counted in a table of few such tokens.
+constexpr uint32_t kInPrompt = 0x8000u, kBiased = 0x4000u, kTimes = 0x3FFFu, kMany = 0x2000u;
+constexpr int kFrequent = 128;
 template <typename T>
 constexpr int kSliceOf = kThreads * kVecs * Vec<T>::kElems;
 
@@ -32,6 +33,15 @@ template <typename T>
 __device__ __forceinline__ uint32_t banned_word(bool backward) {
     if (backward) return 0u;
     return sizeof(T) == 4 ? 0xFF800000u : std::is_same<T, __half>::value ? 0xFC00FC00u : 0xFF80FF80u;
+}
+
+// Word i of a vector without the tokens whose bits are 0.
+template <typename T, bool kBackward>
+__device__ __forceinline__ uint32_t cut(uint32_t w, uint32_t bits, int i) {
+    uint32_t keep;
+    if (sizeof(T) == 4) keep = 0u - ((bits >> i) & 1u);
+    else asm("prmt.b32 %0, %1, %2, 0xDD88;" : "=r"(keep) : "r"(bits << (7 - 2 * i)), "r"(bits << (14 - 2 * i)));      // signs of bytes, twice each
+    return (w & keep) | (banned_word<T>(kBackward) & ~keep);
 }
 
 // Bits l .. l + 31 of a row of words, the first `need` of them; the word behind is read only where one of those is in it.
@@ -52,8 +62,8 @@ __device__ __forceinline__ uint32_t shared_at(const void* p) { return (uint32_t)
 __device__ __forceinline__ void copy_word(void* to, const void* from) { asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(shared_at(to)), "l"(from) : "memory"); }
 __device__ __forceinline__ void copy_vector(void* to, const void* from) { asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(shared_at(to)), "l"(from) : "memory"); }
 __device__ __forceinline__ void copies_end() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-__device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_all;" ::: "memory"); }
-__device__ __forceinline__ void copies_wait_but_one() { asm volatile("cp.async.wait_group 1;" ::: "memory"); }
+template <int kLater>                     // groups that may still be on their way
+__device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(kLater) : "memory"); }
 
 // What a row brings along; written to shared memory a batch of rows at a time, by one warp.
 struct Record {
@@ -61,31 +71,66 @@ struct Record {
     int32_t len, prompt, bias_len;
     int32_t from;                   // positions from here on are new; -1: nothing is as in the row before
     int32_t id;                     // the one new token, where there is one
-    int32_t mask_behind;            // the mask of the row after the next
+    int32_t mask, mask_ahead;       // this row's, and that of the row whose mask is looked up in this row's turn
     float repetition, shrink, presence, frequency;      // shrink: its reciprocal
 };
 constexpr int kBatch = 16;
 
+// Tokens that are seen thousands of times, out of line: a call that hardly any row makes.
+__device__ __noinline__ void count_frequent(uint32_t* table, int l) {
+    for (int i = 0; i < kFrequent; ++i) {
+        const int slot = (l + i) % kFrequent;
+        const uint32_t had = atomicCAS(&table[slot], 0u, (uint32_t)l + 1u);
+        if (had != 0u && had != (uint32_t)l + 1u) continue;
+        atomicAdd(&table[kFrequent + slot], 1u);
+        return;
+    }
+}
+__device__ __noinline__ uint32_t times_frequent(const uint32_t* table, uint32_t times, int l, int id, const int32_t* history, int64_t n_history, const Record& r) {
+    for (int i = 0; i < kFrequent; ++i)
+        if (table[(l + i) % kFrequent] == (uint32_t)l + 1u) return times + table[kFrequent + (l + i) % kFrequent];
+    int64_t from;                   // more of them than the table holds
+    const int skip = min(r.prompt, r.len), n = inside(r.start + skip, r.len - skip, n_history, from);
+    times = 0;
+    for (int k = 0; k < n; ++k) times += history[from + k] == id;
+    return times;
+}
+
 // kSparse: out is in, and only vectors that change are read and written.
-// kShift: rows lie in different ways against 16 bytes, or in and out do.  The touched tokens are then bits of shared memory, which all
-// threads read, and a barrier stands before and behind each change of them.
+// kShift: not all rows of in and out begin on 16 bytes.  The touched tokens are then bits of shared memory, which all threads read, and a
+// barrier stands before and behind each change of them.
+constexpr int kStages = 3;           // rows of the ring: one is changed and written while two are on their way
+
+// Where things lie in dynamic shared memory (bytes).
+template <typename T, bool kBackward, bool kSparse>
+struct Layout {
+    static constexpr int kSlice = kSliceOf<T>, kRow = kVecs * kThreads * 16;
+    static constexpr int kRaw = (kSparse ? 1 : kStages) * kRow, kCount = kRaw + (kBackward ? kRow : 0), kEntry = kCount + (kBackward ? 0 : kSlice * 2),
+                         kBiasIds = kEntry + kSlice * 2, kBiasValues = kBiasIds + kBiasesAhead * 4, kAll = kBiasValues + 2 * kBiasesAhead * 4;
+    static constexpr int bytes(bool counts, bool biases) { return kBackward ? kCount : biases ? kAll : counts ? kEntry : kCount; }
+};
+
 template <typename T, bool kBackward, bool kSparse, bool kShift>
 __global__ void __launch_bounds__(kThreads, 3)
 adjust_kernel(const __grid_constant__ AdjustArgs a, int runs, int rows_per_cta) {
-    constexpr int E = Vec<T>::kElems, kSlice = kSliceOf<T>, kWords = kThreads + 1;        // kSlice / 32 + 1 of them in kShift
-    constexpr uint32_t kAll = (1u << E) - 1u;
-    extern __shared__ __align__(16) uint32_t s_tables[];
+    using Lay = Layout<T, kBackward, kSparse>;
+    constexpr int E = Vec<T>::kElems, kSlice = Lay::kSlice, kBits = E * kVecs;
+    static_assert(kBits <= 32, "a bit for each token of a thread's vectors");
+    constexpr int kWords = kThreads + 1;                 // at least kSlice / 32 + 1
+    constexpr uint32_t kEvery = (uint32_t)((1ull << kBits) - 1u), kAll = (1u << E) - 1u;
+    extern __shared__ __align__(16) unsigned char s_bytes[];
     __shared__ uint32_t s_touched[2][kWords];
     __shared__ Record s_record[kBatch];
-    __shared__ uint4 s_vector[kThreads];                 // each thread's own, and so are the ids
-    __shared__ int32_t s_ids[kIdsAhead], s_bias_ids[kBackward ? 1 : kBiasesAhead];
-    __shared__ float s_bias_values[2][kBackward ? 1 : kBiasesAhead];
-    __shared__ uint4 s_raw[kBackward ? kVecs * kThreads : 1];            // the logits of touched vectors, a row ahead
+    __shared__ int32_t s_ids[kIdsAhead];                 // a thread's own
+    __shared__ uint32_t s_frequent[kBackward ? 1 : 2 * kFrequent];                        // 1 + token, and its further occurrences
     grid_begin();
     const int tid = threadIdx.x;
-    const bool histories = a.history_start != nullptr, biases = !kBackward && a.bias_value != nullptr;
-    uint32_t* const count = s_tables;                                                     // [kSlice], forward
-    uint32_t* const entry = s_tables + kSlice;                                            // [kSlice], with biases: 1 + index in the row's list, of what lies inside its array
+    const bool histories = a.history_start != nullptr, biases = !kBackward && a.bias_value != nullptr, counts = !kBackward && (histories || biases);
+    uint4* const s_raw = reinterpret_cast<uint4*>(s_bytes + Lay::kRaw);                   // backward: the logits of touched vectors, a row ahead; a thread's own
+    uint16_t* const count = reinterpret_cast<uint16_t*>(s_bytes + Lay::kCount);           // [kSlice]
+    uint16_t* const entry = reinterpret_cast<uint16_t*>(s_bytes + Lay::kEntry);           // [kSlice]: 1 + index in the row's list, of what lies inside its array
+    int32_t* const s_bias_ids = reinterpret_cast<int32_t*>(s_bytes + Lay::kBiasIds);      // a thread's own
+    float* const s_bias_values = reinterpret_cast<float*>(s_bytes + Lay::kBiasValues);    // [2][kBiasesAhead]
     const int first = (int)(blockIdx.x / runs) * kSlice, n = min(kSlice, a.vocab - first);
     const int64_t row0 = (int64_t)(blockIdx.x % runs) * rows_per_cta;
     const int row_end = (int)min((int64_t)a.n_rows, row0 + rows_per_cta);
@@ -95,52 +140,48 @@ adjust_kernel(const __grid_constant__ AdjustArgs a, int runs, int rows_per_cta) 
     int flags = 0;
 
     // elements before the first boundary of 16 bytes of both, and the vectors behind them
-    int head = 0, vecs = 0;
+    int head = 0, vecs = n / E;
     const auto split = [&](const T* x, const T* y, int& h, int& v) {
         const uintptr_t p = reinterpret_cast<uintptr_t>(x), q = reinterpret_cast<uintptr_t>(y);
         const int off = (int)(p & 15) / (int)sizeof(T);
-        h = kShift && ((p ^ q) & 15) != 0 ? n : min(n, off ? E - off : 0);
+        h = ((p ^ q) & 15) != 0 ? n : min(n, off ? E - off : 0);
         v = (n - h) / E;
     };
-    if (!kShift) split(in, out, head, vecs);
-    uint32_t word = 0u;                                  // touched tokens of the thread's vectors, E bits of each
-    // Place of a token that lies in no vector: 0 .. 7 before them, 8 .. 15 behind; the threads of that number have them.
-    const auto outside = [&](int l) { return l < head ? l : 8 + l - head - vecs * E; };
-    bool odd = false;                                    // whether the thread's is touched
+    uint32_t word = 0u;                                  // touched tokens of the thread's vectors
+    bool odd = false;                                    // whether the token is that thread `tid` has behind the vectors
+    const auto bits_of_vector = [&](uint32_t w, int k) { return (w >> (k * E)) & kAll; };
+    const auto stage_of = [&](int row) { return reinterpret_cast<uint4*>(s_bytes) + (kSparse ? 0 : (row - (int)row0) % kStages * (kVecs * kThreads)); };
 
-    if (!kBackward && (histories || biases)) {
-        for (int i = tid; i < kSlice / 4; i += kThreads) {
+    if (counts) {
+        for (int i = tid; i < kSlice / 8; i += kThreads) {
             reinterpret_cast<uint4*>(count)[i] = make_uint4(0u, 0u, 0u, 0u);
             if (biases) reinterpret_cast<uint4*>(entry)[i] = make_uint4(0u, 0u, 0u, 0u);
         }
+        for (int i = tid; i < 2 * kFrequent; i += kThreads) s_frequent[i] = 0u;
     }
+    bool frequent = false;                               // whether the thread has counted there
     for (int i = tid; i < 2 * kWords; i += kThreads) s_touched[0][i] = 0u;
 
-    // A turn begins with the next row's masks and vectors and ends with this row's: the first one has none.
-    constexpr uint32_t kEvery = E * kVecs == 32 ? 0xFFFFFFFFu : (1u << (E * kVecs & 31)) - 1u;
-    uint4 q[kVecs];
+    // Masks: that of a row, -1 for none; the words with the bits of the thread's vectors; those bits.
     const auto mask_at = [&](int m) { return a.allowed + (int64_t)m * a.mask_pitch + (first >> 5); };
-    const auto mask_of = [&](int64_t row) {              // -1: none
+    const auto mask_of = [&](int64_t row) {
         if (!a.allowed || row >= row_end) return -1;
         const int m = a.mask_row ? a.mask_row[row] : (int)row;
         if (m >= a.n_masks) flags |= SR_STATUS_BAD_INDEX;
         return m < a.n_masks ? m : -1;
     };
-    // Words with the bits of the thread's vectors, and those bits.
     struct MaskWords {
-        uint32_t lo[kVecs], hi[kVecs];
+        uint32_t lo[kVecs], hi[kShift ? kVecs : 1];
     };
     const auto words_of = [&](int m, int h, int v) {
         MaskWords w = {};
         if (m >= 0) {
-            const uint32_t* const words = mask_at(m);
 #pragma unroll
             for (int k = 0; k < kVecs; ++k) {
-                const int l = h + (tid + k * kThreads) * E;
-                if (tid + k * kThreads < v) {
-                    w.lo[k] = words[l >> 5];
-                    if ((l & 31) + E > 32) w.hi[k] = words[(l >> 5) + 1];
-                }
+                const int j = tid + k * kThreads, l = (kShift ? h : 0) + j * E;
+                if (j >= v) continue;
+                w.lo[k] = mask_at(m)[l >> 5];
+                if (kShift && (l & 31) + E > 32) w.hi[k] = mask_at(m)[(l >> 5) + 1];
             }
         }
         return w;
@@ -148,38 +189,55 @@ adjust_kernel(const __grid_constant__ AdjustArgs a, int runs, int rows_per_cta) 
     const auto bits_of = [&](const MaskWords& w, int m, int h) {
         uint32_t bits = 0u;
 #pragma unroll
-        for (int k = 0; k < kVecs; ++k) bits |= (__funnelshift_r(w.lo[k], w.hi[k], h + (tid + k * kThreads) * E) & kAll) << (k * E);
+        for (int k = 0; k < kVecs; ++k) {
+            const int sh = ((kShift ? h : 0) + (tid + k * kThreads) * E) & 31;
+            bits |= ((kShift ? __funnelshift_r(w.lo[k], w.hi[k], sh) : w.lo[k] >> sh) & kAll) << (k * E);
+        }
         return m < 0 ? kEvery : bits;
     };
-    int mask = -1, next_mask = mask_of(row0);            // of the row and the one behind it
-    uint32_t allowed = kEvery, next_allowed = kShift ? kEvery : bits_of(words_of(next_mask, head, vecs), next_mask, head);      // of the thread's vectors
+
+    // The turn of a row looks up the mask of the row kDepth behind it, has the vectors of the row before that one copied into the ring,
+    // and changes and writes its own.  The first turns are those of no row.
+    constexpr int kDepth = kSparse ? 1 : kStages;
+    uint32_t allowed[kDepth];                            // of the thread's vectors, from this row on
+    int head_ahead = 0, vecs_ahead = vecs;               // of the row that is looked up; the same for all but in kShift
+    if (kShift) split(in, out, head_ahead, vecs_ahead);
+#pragma unroll
+    for (int d = 0; d < kDepth; ++d) allowed[d] = kEvery;
+    {
+        const int m = mask_of(row0);
+        if (a.allowed) allowed[kDepth - 1] = bits_of(words_of(m, head_ahead, vecs_ahead), m, head_ahead);
+    }
     int at = kBatch;                                     // of the records
-    bool ids_ahead = false;                              // this row's are on their way to shared memory
     int half = 0;                                        // of s_touched and s_bias_values, for the row at hand
-    uint32_t raw_ahead = 0u;                             // touched tokens whose logits are on their way
+    // the ids of a row that begins anew, on their way to shared memory while the one before it is written
+    const auto copy_ids = [&](int64_t start, int len, int64_t bias_start, int bias_len) {
+        int64_t from;
+        if (histories) {
+            const int ids_n = min(inside(start, len, a.n_history, from), kIdsAhead);
 #pragma unroll 1
-    for (int row = (int)row0 - 1; row < row_end; ++row) {
-        const T* const next_in = row < row0 ? in : in + a.pitch;
-        int next_head = head, next_vecs = vecs;          // the same for all rows but in kShift
-        uint4 ahead[kVecs];
-#pragma unroll
-        for (int k = 0; k < kVecs; ++k) ahead[k] = make_uint4(0u, 0u, 0u, 0u);
-        if (row + 1 < row_end) {
-            if (kShift) {
-                split(next_in, row < row0 ? out : out + a.out_pitch, next_head, next_vecs);
-                next_allowed = bits_of(words_of(next_mask, next_head, next_vecs), next_mask, next_head);
-            }
-            if (!kSparse) {
-                const uint4* p = reinterpret_cast<const uint4*>(next_in + next_head) + tid;
-#pragma unroll
-                for (int k = 0; k < kVecs; ++k)
-                    if (tid + k * kThreads < next_vecs && ((next_allowed >> (k * E)) & kAll) != 0u) ahead[k] = load_once(p + k * kThreads);
+            for (int c = tid; c < ids_n; c += kThreads) copy_word(&s_ids[c], a.history + from + c);
+        }
+        if (biases) {
+            const int ids_n = min(inside(bias_start, bias_len, a.n_bias, from), kBiasesAhead);
+#pragma unroll 1
+            for (int c = tid; c < ids_n; c += kThreads) {
+                copy_word(&s_bias_ids[c], a.bias_token + from + c);
+                copy_word(&s_bias_values[(half ^ 1) * kBiasesAhead + c], a.bias_value + from + c);
             }
         }
-        int mask_behind = -1;
-        if (row < row0) mask_behind = mask_of(row0 + 1);
-        MaskWords words_behind = {};
-        if (!kShift && row < row0 && a.allowed) words_behind = words_of(mask_behind, head, vecs);
+    };
+    bool ids_ahead = true;                               // whether this row's are
+    {
+        const int64_t start = histories ? a.history_start[row0] : 0, bias_start = biases ? a.bias_start[row0] : 0;
+        const int len = histories ? a.history_len[row0] : 0, bias_len = biases ? a.bias_len[row0] : 0;
+        copy_ids(start, min(len, kMostLength), bias_start, min(bias_len, kMostBiases));
+        copies_end();
+    }
+    uint32_t raw_ahead = 0u;                             // touched vectors whose logits are on their way
+#pragma unroll 1
+    for (int row = (int)row0 - (kDepth - 1); row < row_end; ++row) {
+        int mask_ahead = -1;
         if (row >= row0) {
             if (at == kBatch) {                          // records of the rows from here on, by the first warp
                 if (row > row0) __syncthreads();
@@ -203,9 +261,12 @@ adjust_kernel(const __grid_constant__ AdjustArgs a, int runs, int rows_per_cta) 
                                 r.bias_len = a.bias_len[mine];
                             }
                         }
-                        r.mask_behind = mask_of(mine + 2);
+                        r.mask = mask_of(mine);
+                        r.mask_ahead = mask_of(mine + kDepth);
                         if (r.len < 0 || r.bias_len < 0) flags |= SR_STATUS_NEG_LEN;
+                        if (r.bias_len > kMostBiases) flags |= SR_STATUS_BAD_INDEX;
                         r.len = min(max(r.len, 0), kMostLength);
+                        r.bias_len = min(r.bias_len, kMostBiases);
                         r.prompt = max(r.prompt, 0);
                         r.shrink = __fdiv_rn(1.0f, r.repetition);
                     }
@@ -233,10 +294,18 @@ adjust_kernel(const __grid_constant__ AdjustArgs a, int runs, int rows_per_cta) 
                 at = 0;
             }
             const Record& r = s_record[at++];
-            mask_behind = r.mask_behind;
-            if (!kShift && a.allowed) words_behind = words_of(mask_behind, head, vecs);
+            mask_ahead = r.mask_ahead;
 
             // the tables of this row
+            const auto flag = [&](int l, uint32_t bit) { atomicOr(reinterpret_cast<uint32_t*>(count) + (l >> 1), bit << ((l & 1) * 16)); };
+            const auto add_one = [&](int l) {
+                if ((count[l] & kTimes) < kMany) {
+                    atomicAdd(reinterpret_cast<uint32_t*>(count) + (l >> 1), 1u << ((l & 1) * 16));
+                    return;
+                }
+                frequent = true;
+                count_frequent(s_frequent, l);
+            };
             if (r.from < 0 || r.len > r.from + 1 || (kShift && r.len > r.from)) {
                 if (kShift && row > row0) __syncthreads();           // the row before is done with them
                 if (r.from < 0) half ^= 1;
@@ -244,31 +313,41 @@ adjust_kernel(const __grid_constant__ AdjustArgs a, int runs, int rows_per_cta) 
                     if (r.from >= 0) {
                         if (!kShift) {                   // more than one new token: the owners' bits meet theirs
                             s_touched[half][tid] = word;
-                            if (odd) atomicOr(&s_touched[half][kThreads], 1u << tid);
+                            if (odd) atomicOr(&s_touched[half][kWords - 1], 1u << tid);
                         }
-                    } else if (kShift) {
-                        for (int i = tid; !kBackward && (histories || biases) && i < n; i += kThreads) {
-                            count[i] = 0u;
-                            if (biases) entry[i] = 0u;
+                    } else {
+                        if (kShift) {
+                            for (int i = tid; counts && i < kSlice / 8; i += kThreads) {
+                                reinterpret_cast<uint4*>(count)[i] = make_uint4(0u, 0u, 0u, 0u);
+                                if (biases) reinterpret_cast<uint4*>(entry)[i] = make_uint4(0u, 0u, 0u, 0u);
+                            }
+                            for (int i = tid; i < kWords; i += kThreads) s_touched[half][i] = 0u;
+                        } else if (!kBackward) {
+#pragma unroll
+                            for (int k = 0; k < kVecs; ++k) {
+                                if (bits_of_vector(word, k) == 0u) continue;
+                                const int l0 = (tid + k * kThreads) * E;
+#pragma unroll
+                                for (int e = 0; e < E; e += 2) {
+                                    *reinterpret_cast<uint32_t*>(count + l0 + e) = 0u;
+                                    if (biases) *reinterpret_cast<uint32_t*>(entry + l0 + e) = 0u;
+                                }
+                            }
+                            if (odd) {
+                                count[vecs * E + tid] = 0u;
+                                if (biases) entry[vecs * E + tid] = 0u;
+                            }
                         }
-                        for (int i = tid; i < kWords; i += kThreads) s_touched[half][i] = 0u;
-                    } else if (!kBackward) {
-                        const auto forget = [&](int l) {
-                            count[l] = 0u;
-                            if (biases) entry[l] = 0u;
-                        };
-#pragma unroll 1
-                        for (uint32_t left = word; left != 0u; left &= left - 1u) {
-                            const int b = __ffs(left) - 1;
-                            forget(head + (tid + b / E * kThreads) * E + b % E);
-                        }
-                        if (odd) forget(tid < 8 ? tid : head + vecs * E + tid - 8);
                     }
-                    __syncthreads();
+                    if (__syncthreads_or(frequent) && r.from < 0) {
+                        for (int i = tid; !kBackward && i < 2 * kFrequent; i += kThreads) s_frequent[i] = 0u;
+                        frequent = false;
+                        __syncthreads();
+                    }
                 }
                 // ids of the bias list, then of the history, in the slice
                 const bool copied = ids_ahead && r.from < 0;
-                if (copied) copies_wait();
+                if (copied) copies_wait<kBackward ? 2 : 1>();
 #pragma unroll 1
                 for (int pass = biases && r.from < 0 ? 0 : 1; pass < 1 + histories; ++pass) {
                     int64_t from;
@@ -284,19 +363,28 @@ adjust_kernel(const __grid_constant__ AdjustArgs a, int runs, int rows_per_cta) 
                             return;
                         }
                         if (!kBackward) {
-                            if (pass == 0) {
-                                atomicMax(&entry[l], (uint32_t)c + 1u);
-                                atomicOr(&count[l], kBiased);
+                            if (pass == 0) {             // the largest index, in 16 bits of a word
+                                uint32_t* const w = reinterpret_cast<uint32_t*>(entry) + (l >> 1);
+                                const uint32_t sh = (l & 1) * 16, mine = (uint32_t)c + 1u;
+                                for (uint32_t had = *w; ((had >> sh) & 0xFFFFu) < mine;) {
+                                    const uint32_t now = atomicCAS(w, had, (had & ~(0xFFFFu << sh)) | mine << sh);
+                                    if (now == had) break;
+                                    had = now;
+                                }
+                                flag((int)l, kBiased);
                             } else if (c >= behind) {
-                                atomicAdd(&count[l], 1u);
+                                add_one((int)l);
                             } else {
-                                atomicOr(&count[l], kInPrompt);
+                                flag((int)l, kInPrompt);
                             }
                         }
-                        const int v = (int)l - head;
-                        if (kShift) atomicOr(&s_touched[half][l >> 5], 1u << (l & 31));
-                        else if (v < 0 || v >= vecs * E) atomicOr(&s_touched[half][kThreads], 1u << outside((int)l));
-                        else atomicOr(&s_touched[half][(v / E) & (kThreads - 1)], 1u << ((v / E / kThreads) * E + v % E));
+                        if (kShift) {
+                            atomicOr(&s_touched[half][l >> 5], 1u << (l & 31));
+                        } else if ((int)l >= vecs * E) {
+                            atomicOr(&s_touched[half][kWords - 1], 1u << (l - vecs * E));
+                        } else {
+                            atomicOr(&s_touched[half][l / E % kThreads], 1u << (l / E / kThreads * E + l % E));
+                        }
                     };
                     int c = tid;
                     if (copied) {
@@ -305,40 +393,41 @@ adjust_kernel(const __grid_constant__ AdjustArgs a, int runs, int rows_per_cta) 
 #pragma unroll 1
                         for (; c < held_n; c += kThreads) one(c, held[c]);
                     } else if (pass == 0) {
-                        for (int k = tid; k < min(ids_n, kBiasesAhead); k += kThreads) s_bias_values[half][k] = a.bias_value[from + k];
+                        for (int k = tid; k < min(ids_n, kBiasesAhead); k += kThreads) s_bias_values[half * kBiasesAhead + k] = a.bias_value[from + k];
                     }
 #pragma unroll 1
                     for (; c < ids_n; c += 4 * kThreads) {
                         int32_t id[4];
 #pragma unroll
                         for (int k = 0; k < 4; ++k) id[k] = c + k * kThreads < ids_n ? ids[c + k * kThreads] : -1;
-#pragma unroll
-                        for (int k = 0; k < 4; ++k) one(c + k * kThreads, id[k]);
+#pragma unroll 1
+                        for (int k = 0; k < 4; ++k) one(c + k * kThreads, k == 0 ? id[0] : k == 1 ? id[1] : k == 2 ? id[2] : id[3]);
                     }
                 }
                 __syncthreads();
                 if (!kShift) {
                     word = s_touched[half][tid];
-                    odd = tid < 16 && ((s_touched[half][kThreads] >> tid) & 1u);
-                    s_touched[half ^ 1][tid] = 0u;       // for the next time: everybody has read it before the barriers above
-                    if (tid == 0) s_touched[half ^ 1][kThreads] = 0u;
+                    odd = tid < E && ((s_touched[half][kWords - 1] >> tid) & 1u);
+                    s_touched[half ^ 1][tid] = 0u;       // for the next time: all have read it before the barriers above
+                    if (tid == 0) s_touched[half ^ 1][kWords - 1] = 0u;
                 }
             } else if (!kShift && r.id >= first && r.id - first < n) {
-                const int l = r.id - first, v = l - head;            // one new token: its owner notes it
+                const int l = r.id - first;              // one new token: its owner notes it
                 bool mine;
-                if (v < 0 || v >= vecs * E) {
-                    mine = outside(l) == tid;
+                if (l >= vecs * E) {
+                    mine = l - vecs * E == tid;
                     odd |= mine;
                 } else {
-                    mine = ((v / E) & (kThreads - 1)) == tid;
-                    if (mine) word |= 1u << ((v / E / kThreads) * E + v % E);
+                    mine = l / E % kThreads == tid;
+                    if (mine) word |= 1u << (l / E / kThreads * E + l % E);
                 }
-                if (mine && !kBackward) {
-                    if (r.from >= r.prompt) count[l] += 1u;
-                    else count[l] |= kInPrompt;
+                if (mine && !kBackward) {                // others change other halves of a word meanwhile: atomics too
+                    if (r.from >= r.prompt) add_one(l);
+                    else flag(l, kInPrompt);
                 }
             }
             if (kShift) {
+                split(in, out, head, vecs);
                 word = 0u;
 #pragma unroll
                 for (int k = 0; k < kVecs; ++k) {
@@ -347,149 +436,147 @@ adjust_kernel(const __grid_constant__ AdjustArgs a, int runs, int rows_per_cta) 
                 }
             }
 
-            // on their way while this row is written: the ids of the next, where it begins anew
             ids_ahead = at < kBatch && row + 1 < row_end && s_record[at < kBatch ? at : 0].from < 0;
-            if (ids_ahead) {
-                const Record& next = s_record[at];
-                int64_t from;
-                if (histories) {
-                    const int ids_n = min(inside(next.start, next.len, a.n_history, from), kIdsAhead);
-#pragma unroll 1
-                    for (int c = tid; c < ids_n; c += kThreads) copy_word(&s_ids[c], a.history + from + c);
-                }
-                if (biases) {
-                    const int ids_n = min(inside(next.bias_start, next.bias_len, a.n_bias, from), kBiasesAhead);
-#pragma unroll 1
-                    for (int c = tid; c < ids_n; c += kThreads) {
-                        copy_word(&s_bias_ids[c], a.bias_token + from + c);
-                        copy_word(&s_bias_values[half ^ 1][c], a.bias_value + from + c);
-                    }
-                }
-            }
-            copies_end();
+            if (ids_ahead) copy_ids(s_record[at].start, s_record[at].len, s_record[at].bias_start, s_record[at].bias_len);
+        }
+        copies_end();
 
+        // vectors of the last row that was looked up, and the mask of the next one
+        MaskWords words = {};
+        if (!kSparse) {
+            const int ahead = row + kDepth - 1;
+            if (ahead < row_end) {
+                const uint4* const p = reinterpret_cast<const uint4*>(static_cast<const T*>(a.in) + ahead * a.pitch + first + head_ahead) + tid;
+                uint4* const to = stage_of(ahead) + tid;
+#pragma unroll
+                for (int k = 0; k < kVecs; ++k)
+                    if (tid + k * kThreads < vecs_ahead && bits_of_vector(allowed[kDepth - 1], k) != 0u) copy_vector(to + k * kThreads, p + k * kThreads);
+            }
+        }
+        copies_end();
+        if (row < row0) mask_ahead = mask_of((int64_t)row + kDepth);
+        if (kShift && row + kDepth < row_end) {
+            const int64_t ahead = (int64_t)row + kDepth;
+            split(static_cast<const T*>(a.in) + ahead * a.pitch + first, static_cast<T*>(a.out) + ahead * a.out_pitch + first, head_ahead, vecs_ahead);
+        }
+        if (a.allowed) words = words_of(mask_ahead, head_ahead, vecs_ahead);
+
+        if (row >= row0) {
+            const Record& r = s_record[at - 1];
             // This row.  16-bit logits are multiplied by the reciprocal, whose 2^-24 their last rounding (2^-9, 2^-12) hides.
-            const float repetition = r.repetition, shrink = r.shrink;
             const auto changed = [&](int l, float v, bool positive) {
-                const auto repeated = [&] { return kBackward ? positive : v > 0.0f; };
-                if (kBackward) return sizeof(T) == 4 ? (repeated() ? v / repetition : v * repetition) : v * (repeated() ? shrink : repetition);
-                const uint32_t c = count[l], times = c & ~(kInPrompt | kBiased);
-                if (c & ~kBiased) v = sizeof(T) == 4 ? (repeated() ? v / repetition : v * repetition) : v * (repeated() ? shrink : repetition);
+                const float repetition = r.repetition;
+                const auto repeated = [&](bool larger) { return sizeof(T) == 4 ? (larger ? v / repetition : v * repetition) : v * (larger ? r.shrink : repetition); };
+                if (kBackward) return repeated(positive);
+                const uint32_t c = count[l];
+                uint32_t times = c & kTimes;
+                if (c & ~kBiased) v = repeated(v > 0.0f);
+                if (times >= kMany) times = times_frequent(s_frequent, times, l, first + l, a.history, a.n_history, r);
                 const float less = fmaf(-r.frequency, (float)times, v) - r.presence;
                 v = times ? less : v;
                 if (c & kBiased) {
                     const int e = (int)entry[l] - 1;
-                    v += e < kBiasesAhead ? s_bias_values[half][e] : a.bias_value[max(r.bias_start, (int64_t)0) + e];
+                    v += e < kBiasesAhead ? s_bias_values[half * kBiasesAhead + e] : a.bias_value[max(r.bias_start, (int64_t)0) + e];
                 }
                 return v;
             };
             // elements in no vector
 #pragma unroll 1
-            for (int i = tid; kShift ? i < n - vecs * E : i < 16; i += kThreads) {
-                const int l = kShift ? (i < head ? i : i + vecs * E) : i < 8 ? i : head + vecs * E + i - 8;
-                if (!kShift && (i < 8 ? l >= head : l >= n)) continue;
-                if (mask >= 0 && !((mask_at(mask)[l >> 5] >> (l & 31)) & 1u)) out[l] = banned_value<T>(kBackward);
+            for (int i = tid; i < n - vecs * E; i += kThreads) {
+                const int l = i < head ? i : i + vecs * E;
+                if (r.mask >= 0 && !((mask_at(r.mask)[l >> 5] >> (l & 31)) & 1u)) out[l] = banned_value<T>(kBackward);
                 else if (kShift ? (s_touched[half][l >> 5] >> (l & 31)) & 1u : odd) out[l] = from_float<T>(changed(l, to_float(in[l]), kBackward && to_float(raw[l]) > 0.0f));
                 else if (!kSparse) out[l] = in[l];
             }
+            uint4* const mine = stage_of(row) + tid;     // the thread's vectors
             if (kSparse) {
                 const uint4* p = reinterpret_cast<const uint4*>(in + head) + tid;
 #pragma unroll
-                for (int k = 0; k < kVecs; ++k) {        // vectors with a token that stays and one that changes
-                    const uint32_t m = (allowed >> (k * E)) & kAll, t = (word >> (k * E)) & kAll;
-                    if (tid + k * kThreads < vecs && m != 0u && (m != kAll || t != 0u)) q[k] = load_once(p + k * kThreads);
-                }
-            }
-            const uint32_t left = word & allowed;        // tokens that change, one after the other in the thread's part of shared memory
-            if (left != 0u) {
-                T* const mine = reinterpret_cast<T*>(s_vector + tid);
-                if (kBackward) copies_wait_but_one();
-#pragma unroll
-                for (int k = 0; k < kVecs; ++k) {
-                    if (((left >> (k * E)) & kAll) == 0u) continue;
-                    s_vector[tid] = q[k];
-                    const int l0 = head + (tid + k * kThreads) * E;
-                    const T* const raw_held = reinterpret_cast<const T*>(s_raw + (kBackward ? k * kThreads + tid : 0));
-#pragma unroll 1
-                    for (uint32_t b = (left >> (k * E)) & kAll; b != 0u; b &= b - 1u) {
-                        const int e = __ffs(b) - 1;
-                        bool positive = false;           // the logit whose gradient this is
-                        if (kBackward) positive = to_float((raw_ahead >> (k * E)) & 1u ? raw_held[e] : raw[l0 + e]) > 0.0f;
-                        mine[e] = from_float<T>(changed(l0 + e, to_float(mine[e]), positive));
-                    }
-                    q[k] = s_vector[tid];
-                }
-            }
-            if (kBackward) {                             // the next row's logits of what is touched already
-                raw_ahead = 0u;
-                if (word != 0u && !kShift && row + 1 < row_end && (reinterpret_cast<uintptr_t>(raw + a.logits_pitch + head) & 15) == 0) {
-                    const uint4* const p = reinterpret_cast<const uint4*>(raw + a.logits_pitch + head) + tid;
-#pragma unroll
-                    for (int k = 0; k < kVecs; ++k) {
-                        if (((word & next_allowed) >> (k * E) & kAll) == 0u) continue;
-                        copy_vector(&s_raw[k * kThreads + tid], p + k * kThreads);
-                        raw_ahead |= kAll << (k * E);
-                    }
+                for (int k = 0; k < kVecs; ++k) {        // those with a token that stays and one that changes
+                    const uint32_t m = bits_of_vector(allowed[0], k), t = bits_of_vector(word, k);
+                    if (tid + k * kThreads < vecs && m != 0u && (m != kAll || t != 0u)) copy_vector(mine + k * kThreads, p + k * kThreads);
                 }
                 copies_end();
+                copies_wait<0>();
+            } else if (!kBackward) {
+                copies_wait<2 * kStages - 2>();
+            } else {
+                copies_wait<3 * kStages - 3>();
+            }
+            const uint32_t left = word & allowed[0];     // tokens that change, one after the other
+            if (kBackward && !kShift && left != 0u && raw_ahead != 0u) copies_wait<2>();
+#pragma unroll 1
+            for (uint32_t b = left; b != 0u; b &= b - 1u) {
+                const int bit = __ffs(b) - 1, v = bit / E * kThreads, l = head + (tid + v) * E + bit % E;
+                T* const x = reinterpret_cast<T*>(mine + v) + bit % E;
+                bool positive = false;                   // the logit whose gradient this is
+                if (kBackward) positive = to_float((raw_ahead >> bit) & 1u ? reinterpret_cast<const T*>(s_raw + tid + v)[bit % E] : raw[l]) > 0.0f;
+                *x = from_float<T>(changed(l, to_float(*x), positive));
             }
             uint4* const to = reinterpret_cast<uint4*>(out + head) + tid;
 #pragma unroll
             for (int k = 0; k < kVecs; ++k) {
                 if (tid + k * kThreads >= vecs) break;
-                const uint32_t m = (allowed >> (k * E)) & kAll;
-                if (kSparse && m == kAll && ((word >> (k * E)) & kAll) == 0u) continue;
+                const uint32_t m = bits_of_vector(allowed[0], k);
+                if (kSparse && m == kAll && bits_of_vector(word, k) == 0u) continue;
+                uint4 q = mine[k * kThreads];
                 if (m != kAll) {
-                    uint32_t w[4] = {q[k].x, q[k].y, q[k].z, q[k].w};
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        uint32_t keep;
-                        if (E == 4) keep = (m >> i) & 1u ? 0xFFFFFFFFu : 0u;
-                        else keep = ((m >> (2 * i)) & 1u ? 0x0000FFFFu : 0u) | ((m >> (2 * i + 1)) & 1u ? 0xFFFF0000u : 0u);
-                        w[i] = (w[i] & keep) | (banned_word<T>(kBackward) & ~keep);
-                    }
-                    q[k] = make_uint4(w[0], w[1], w[2], w[3]);
+                    q.x = cut<T, kBackward>(q.x, m, 0);
+                    q.y = cut<T, kBackward>(q.y, m, 1);
+                    q.z = cut<T, kBackward>(q.z, m, 2);
+                    q.w = cut<T, kBackward>(q.w, m, 3);
                 }
-                store_once(to + k * kThreads, q[k]);
+                store_once(to + k * kThreads, q);
+            }
+            if (kBackward && !kShift) {                  // the next row's logits of what is touched already
+                raw_ahead = 0u;
+                if (word != 0u && row + 1 < row_end && (reinterpret_cast<uintptr_t>(raw + a.logits_pitch) & 15) == 0) {
+                    const uint4* const p = reinterpret_cast<const uint4*>(raw + a.logits_pitch) + tid;
+#pragma unroll
+                    for (int k = 0; k < kVecs; ++k) {
+                        if (bits_of_vector(word, k) == 0u) continue;
+                        copy_vector(&s_raw[k * kThreads + tid], p + k * kThreads);
+                        raw_ahead |= kAll << (k * E);
+                    }
+                }
             }
             in += a.pitch;
             out += a.out_pitch;
             if (kBackward) raw += a.logits_pitch;
         }
+        if (kBackward) copies_end();
 #pragma unroll
-        for (int k = 0; k < kVecs; ++k) q[k] = ahead[k];
-        mask = next_mask;
-        allowed = next_allowed;
-        next_mask = mask_behind;
-        if (!kShift) next_allowed = bits_of(words_behind, mask_behind, head);
-        head = next_head;
-        vecs = next_vecs;
+        for (int d = 0; d + 1 < kDepth; ++d) allowed[d] = allowed[d + 1];
+        if (a.allowed) allowed[kDepth - 1] = bits_of(words, mask_ahead, head_ahead);
     }
     if (a.status && flags) atomicOr(a.status, flags);
 }
 
-template <typename T, bool kBackward>
-int launch_type(const AdjustArgs& a, cudaStream_t s) {
+template <typename T, bool kBackward, bool kSparse, bool kShift>
+int launch_form(const AdjustArgs& a, cudaStream_t s) {
     constexpr int kSlice = kSliceOf<T>;
     const int slices = (a.vocab - 1) / kSlice + 1;
     // Few rows get a CTA each a slice; many are dealt out in runs, so that a rollout's rows find its history at hand, but
-    // leave every SM a few turns.
+    // leave every SM a few turns.  Slices go from the lowest ids on: with most vocabularies these are the tokens that are seen most often, and
+    // whose CTAs take longest.
     const int64_t units = (int64_t)slices * a.n_rows;
-    static const char* tune = getenv("TUNE_WAVES");
-    static const char* tune2 = getenv("TUNE_SLOTS");
-    const int waves = tune ? atoi(tune) : 3, slots = tune2 ? atoi(tune2) : 296;
-    int64_t rows = std::min<int64_t>((units - 1) / (slots * waves) + 1, 64);
+    int64_t rows = std::min<int64_t>((units - 1) / (148 * 3 * 2) + 1, 64);   // two turns of three CTAs
     rows = std::max(rows, (units - 1) / (INT32_MAX - slices) + 1);           // CTAs are numbered in 31 bits
     const int64_t runs = (a.n_rows - 1) / rows + 1, ctas = slices * runs;
-    const size_t smem = kBackward ? 0 : (size_t)(a.bias_value ? 2 : a.history_start ? 1 : 0) * kSlice * sizeof(uint32_t);
-    const auto apart = [&](int64_t pitch) { return a.n_rows > 1 && pitch * (int64_t)sizeof(T) % 16 != 0; };
-    const bool alike = ((reinterpret_cast<uintptr_t>(a.in) ^ reinterpret_cast<uintptr_t>(a.out)) & 15) == 0;
-    const bool shift = !alike || apart(a.pitch) || apart(a.out_pitch);
-    const auto kernel = a.in == a.out ? (shift ? adjust_kernel<T, kBackward, true, true> : adjust_kernel<T, kBackward, true, false>)
-                                      : (shift ? adjust_kernel<T, kBackward, false, true> : adjust_kernel<T, kBackward, false, false>);
-    if (smem > 24 * 1024) SR_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
-    SR_LAUNCH("adjust_kernel", kernel, (int)ctas, kThreads, smem, s, a, (int)runs, (int)rows);
+    using Lay = Layout<T, kBackward, kSparse>;
+    const int smem = Lay::bytes(a.history_start != nullptr, a.bias_value != nullptr);
+    const auto kernel = adjust_kernel<T, kBackward, kSparse, kShift>;
+    SR_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, Lay::kAll));
+    SR_LAUNCH("adjust_kernel", kernel, (int)ctas, kThreads, (size_t)smem, s, a, (int)runs, (int)rows);
     return SR_OK;
+}
+template <typename T, bool kBackward>
+int launch_type(const AdjustArgs& a, cudaStream_t s) {
+    const auto on_16 = [&](const void* p, int64_t pitch) { return reinterpret_cast<uintptr_t>(p) % 16 == 0 && (a.n_rows == 1 || pitch * (int64_t)sizeof(T) % 16 == 0); };
+    const bool in_place = a.in == a.out;
+    if (!on_16(a.in, a.pitch) || !on_16(a.out, a.out_pitch)) return in_place ? launch_form<T, kBackward, true, true>(a, s) : launch_form<T, kBackward, false, true>(a, s);
+    if (in_place) return launch_form<T, kBackward, true, false>(a, s);
+    return launch_form<T, kBackward, false, false>(a, s);
 }
 
 }  // namespace

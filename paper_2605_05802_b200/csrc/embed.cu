@@ -106,11 +106,10 @@ embed_kernel(const __grid_constant__ EmbedArgs a, int across, int tiles) {
 constexpr int kSortThreads = 1024;
 constexpr int kSortWarps = kSortThreads / 32;
 constexpr int kMostBits = 10;
-constexpr int kSortCtas = 8;
+constexpr int kSortCtas = 16;      // more than every GPU has to run together, but not more than a B200 does
 
 struct SortScratch {
-    int32_t* key[2];
-    int32_t* pos[2];
+    int2* sorted[2];        // (token, position)
     uint32_t* count;        // [kSortCtas][1 << kMostBits]
 };
 
@@ -120,11 +119,17 @@ __device__ __forceinline__ int32_t load_l2(const void* p) {
     asm volatile("ld.global.cg.s32 %0, [%1];" : "=r"(v) : "l"(p) : "memory");
     return v;
 }
+__device__ __forceinline__ int2 load_l2(const int2* p) {
+    int2 v;
+    asm volatile("ld.global.cg.v2.s32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "l"(p) : "memory");
+    return v;
+}
 __device__ __forceinline__ uint32_t below(uint32_t peers) { return __popc(peers & ((1u << (threadIdx.x & 31)) - 1u)); }
 
+constexpr int kHeld = 8;            // tokens a lane loads at a time; as many are held from counting to placing
 __global__ void __launch_bounds__(kSortThreads)
 sort_tokens_kernel(const int32_t* tokens, int n, int vocab, int passes, int bits, SortScratch ws, int32_t* status) {
-    extern __shared__ uint32_t s_hist[];                // [kSortWarps][bins]
+    extern __shared__ __align__(16) uint32_t s_hist[];  // [kSortWarps][bins]
     __shared__ uint32_t s_base[1 << kMostBits], s_warp[kSortWarps];
     grid_begin();
     const int ctas = gridDim.x, cta = blockIdx.x, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -134,28 +139,49 @@ sort_tokens_kernel(const int32_t* tokens, int n, int vocab, int passes, int bits
     uint32_t* const hist = s_hist + warp * bins;
     bool bad = false;
     for (int p = 0; p < passes; ++p) {
-        const int32_t *key = p ? ws.key[(p - 1) & 1] : tokens, *pos = p ? ws.pos[(p - 1) & 1] : nullptr;
+        const int2* const from = ws.sorted[(p - 1) & 1];
+        int2* const to = ws.sorted[p & 1];
         const int shift = p * bits;
-        const auto key_at = [&](int64_t i) {
-            const int32_t k = load_l2(key + i);
-            bad |= k > vocab || (p == 0 && k == vocab);
-            return k < 0 || k > vocab ? vocab : k;                   // what is no token comes last
+        int32_t k[kHeld], at[kHeld];
+        const auto load = [&](int64_t i0) {
+#pragma unroll
+            for (int u = 0; u < kHeld; ++u) {
+                const int64_t i = i0 + u * 32 + lane;
+                k[u] = 0;
+                at[u] = (int32_t)i;
+                if (i < end && p == 0) {
+                    k[u] = load_l2(tokens + i);
+                } else if (i < end) {
+                    const int2 v = load_l2(from + i);
+                    k[u] = v.x;
+                    at[u] = v.y;
+                }
+            }
+#pragma unroll
+            for (int u = 0; u < kHeld; ++u) {
+                bad |= k[u] > vocab || (p == 0 && k[u] == vocab);
+                if (k[u] < 0 || k[u] > vocab) k[u] = vocab;          // what is no token comes last
+            }
         };
-        for (int i = threadIdx.x; i < kSortWarps * bins; i += kSortThreads) s_hist[i] = 0u;
+        const auto digit = [&](int64_t i, int32_t of) { return i < end ? (of >> shift) & (bins - 1) : bins; };
+        for (int i = threadIdx.x; i < kSortWarps * bins / 4; i += kSortThreads) reinterpret_cast<uint4*>(s_hist)[i] = make_uint4(0u, 0u, 0u, 0u);
         __syncthreads();
-        for (int64_t i0 = begin; i0 < end; i0 += 32) {
-            const int64_t i = i0 + lane;
-            const bool real = i < end;
-            const int32_t k = real ? key_at(i) : 0;
-            const int d = real ? (k >> shift) & (bins - 1) : bins;
-            const uint32_t peers = __match_any_sync(0xFFFFFFFFu, d);
-            if (real && below(peers) == 0) hist[d] += __popc(peers);
-            __syncwarp();
+        for (int64_t i0 = begin; i0 < end; i0 += kHeld * 32) {
+            load(i0);
+#pragma unroll
+            for (int u = 0; u < kHeld; ++u) {
+                if (i0 + u * 32 >= end) break;
+                const int d = digit(i0 + u * 32 + lane, k[u]);
+                const uint32_t peers = __match_any_sync(0xFFFFFFFFu, d);
+                if (d < bins && below(peers) == 0) hist[d] += __popc(peers);
+                __syncwarp();
+            }
         }
         __syncthreads();
         const int b = threadIdx.x;
         if (b < bins) {
             uint32_t sum = 0;
+#pragma unroll 8
             for (int w = 0; w < kSortWarps; ++w) {
                 const uint32_t c = s_hist[w * bins + b];
                 s_hist[w * bins + b] = sum;
@@ -165,12 +191,16 @@ sort_tokens_kernel(const int32_t* tokens, int n, int vocab, int passes, int bits
         }
         cg::this_cluster().sync();
         uint32_t total = 0, before = 0;
-        if (b < bins)
-            for (int c = 0; c < ctas; ++c) {
-                const uint32_t v = (uint32_t)load_l2(ws.count + (c << kMostBits) + b);
-                before += c < cta ? v : 0u;
-                total += v;
+        if (b < bins) {
+            uint32_t v[kSortCtas];
+#pragma unroll
+            for (int c = 0; c < kSortCtas; ++c) v[c] = c < ctas ? (uint32_t)load_l2(ws.count + (c << kMostBits) + b) : 0u;
+#pragma unroll
+            for (int c = 0; c < kSortCtas; ++c) {
+                before += c < cta ? v[c] : 0u;
+                total += v[c];
             }
+        }
         uint32_t scan = total;                           // of the bins before this one
         for (int o = 1; o < 32; o <<= 1) {
             const uint32_t v = __shfl_up_sync(0xFFFFFFFFu, scan, o);
@@ -181,26 +211,81 @@ sort_tokens_kernel(const int32_t* tokens, int n, int vocab, int passes, int bits
         for (int w = 0; w < warp; ++w) before += s_warp[w];
         if (b < bins) s_base[b] = before + scan - total;
         __syncthreads();
-        for (int64_t i0 = begin; i0 < end; i0 += 32) {
-            const int64_t i = i0 + lane;
-            const bool real = i < end;
-            const int32_t k = real ? key_at(i) : 0;
-            const int32_t at = real ? (p ? load_l2(pos + i) : (int32_t)i) : 0;
-            const int d = real ? (k >> shift) & (bins - 1) : bins;
-            const uint32_t peers = __match_any_sync(0xFFFFFFFFu, d);
-            uint32_t to = 0;
-            if (real) to = s_base[d] + hist[d] + below(peers);
-            __syncwarp();
-            if (real) {
-                if (below(peers) == 0) hist[d] += __popc(peers);
-                ws.key[p & 1][to] = k;
-                ws.pos[p & 1][to] = at;
+        for (int64_t i0 = begin; i0 < end; i0 += kHeld * 32) {
+            if (a_warp > kHeld * 32) load(i0);
+#pragma unroll
+            for (int u = 0; u < kHeld; ++u) {
+                if (i0 + u * 32 >= end) break;
+                const int d = digit(i0 + u * 32 + lane, k[u]);
+                const uint32_t peers = __match_any_sync(0xFFFFFFFFu, d);
+                uint32_t place = 0;
+                if (d < bins) place = s_base[d] + hist[d] + below(peers);
+                __syncwarp();
+                if (d < bins) {
+                    if (below(peers) == 0) hist[d] += __popc(peers);
+                    to[place] = make_int2(k[u], at[u]);
+                }
+                __syncwarp();
             }
-            __syncwarp();
         }
         cg::this_cluster().sync();
     }
     if (bad && status) atomicOr(status, SR_STATUS_BAD_TARGET);
+}
+
+// Few tokens: the place of each is the number of those that belong before it.  A CTA has 32 tokens and all keys in shared memory; eight threads
+// share the keys of a token.
+constexpr int kFewTokens = 4096, kRanked = 32;
+__global__ void __launch_bounds__(kThreads)
+rank_tokens_kernel(const int32_t* tokens, int n, int vocab, int2* sorted, int32_t* status) {
+    extern __shared__ __align__(16) int32_t s_key[];    // [n up to a multiple of 32]
+    __shared__ int s_rank[kRanked];
+    grid_begin();
+    const int padded = (n + 31) & ~31;
+    bool bad = false;
+    for (int i0 = threadIdx.x; i0 < padded; i0 += 8 * kThreads) {
+        int32_t k[8];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) k[u] = i0 + u * kThreads < n ? tokens[i0 + u * kThreads] : -1;
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+            if (i0 + u * kThreads >= padded) break;
+            bad |= k[u] >= vocab;
+            s_key[i0 + u * kThreads] = k[u] < 0 || k[u] > vocab ? vocab : k[u];
+        }
+    }
+    if (threadIdx.x < kRanked) s_rank[threadIdx.x] = 0;
+    __syncthreads();
+    constexpr int kParts = kThreads / kRanked;
+    const int t = threadIdx.x % kRanked, i = blockIdx.x * kRanked + t, part = threadIdx.x / kRanked;
+    if (i < n) {
+        // keys before the token count when they are not larger, those behind it when they are smaller
+        const int mine = s_key[i], lo = padded / kParts * part, hi = lo + padded / kParts;
+        const int middle = max(lo, min(hi, i & ~3));
+        int rank = 0;
+        const auto count = [&](int from, int to, auto before) {
+#pragma unroll 4
+            for (int j = from; j < to; j += 4) {
+                const int4 k = *reinterpret_cast<const int4*>(s_key + j);
+                rank += before(k.x) + before(k.y) + before(k.z) + before(k.w);
+            }
+        };
+        const auto not_larger = [&](int k) { return (int)(k <= mine); };
+        const auto smaller = [&](int k) { return (int)(k < mine); };
+        count(lo, middle, not_larger);
+        if (middle < hi && middle == (i & ~3)) {
+            for (int j = middle; j < middle + 4; ++j) rank += j < i ? not_larger(s_key[j]) : smaller(s_key[j]);
+            count(middle + 4, hi, smaller);
+        } else {
+            count(middle, hi, smaller);
+        }
+        atomicAdd(&s_rank[t], rank);
+    }
+    __syncthreads();
+    if (i < n && part == 0) {
+        sorted[s_rank[t]] = make_int2(s_key[i], i);
+    }
+    if (bad && status && blockIdx.x == 0) atomicOr(status, SR_STATUS_BAD_TARGET);
 }
 
 // ------------------------------------------------------------------------------------------------- sums
@@ -210,15 +295,16 @@ struct Pieces {
 };
 constexpr int kBatch = 8;
 Pieces pieces_of(int n_tokens, int width) {
-    // a wave of the GPU (148 x 8 groups of 2048 columns), not shorter than 8 tokens and not longer than 512
+    // a wave of the GPU (148 x 8 groups of 2048 columns); not shorter than a batch, or two where there are enough tokens (a frequent one then
+    // crosses half as many pieces), and not longer than 512
     const int64_t even = (int64_t)n_tokens * width / (2048 * 1184);
-    const int length = (int)std::min<int64_t>(std::max<int64_t>((even + kBatch - 1) / kBatch * kBatch, kBatch), 512);
+    const int length = (int)std::min<int64_t>(std::max<int64_t>((even + kBatch - 1) / kBatch * kBatch, n_tokens > 2048 ? 2 * kBatch : kBatch), 512);
     return Pieces{length, n_tokens > 0 ? (n_tokens - 1) / length + 1 : 0};
 }
 
 struct SumArgs {
     EmbedGradArgs g;
-    const int32_t *key, *pos;        // sorted
+    const int2* sorted;              // (token, position)
     float* partial;                  // [pieces][2][width]: of the run that came from the piece before, and of the one that goes on
     Pieces pieces;
 };
@@ -241,41 +327,102 @@ __device__ __forceinline__ void write_row(const EmbedGradArgs& g, int token, int
     o.store(to);
 }
 
+// Writes zeros to the rows [begin, end) that no token took.
+constexpr int kMostZeroRows = 1024;
+template <typename Table, int kCols>
+__device__ __forceinline__ void zero_rows(const SumArgs& a, int begin, int end, int across) {
+    __shared__ uint32_t s_taken[kMostZeroRows / 32];
+    __shared__ int s_from;
+    const EmbedGradArgs& g = a.g;
+    if (threadIdx.x < kMostZeroRows / 32) s_taken[threadIdx.x] = 0u;
+    if (threadIdx.x < 32) {                              // the first sorted token of these rows: 32 probes at a time
+        int lo = 0, hi = g.n_tokens;                     // all before lo are smaller, none from hi on is
+        while (lo < hi) {
+            const int step = (hi - lo - 1) / 32 + 1, at = (int)min((int64_t)hi - 1, (int64_t)lo + (int64_t)step * (threadIdx.x + 1) - 1);
+            const int smaller = __popc(__ballot_sync(0xFFFFFFFFu, a.sorted[at].x < begin));
+            const int64_t from = (int64_t)lo + (int64_t)step * smaller;
+            hi = (int)min((int64_t)hi, from + step - 1);
+            lo = (int)min((int64_t)hi, from);
+            if (smaller == 32) lo = hi;
+        }
+        if (threadIdx.x == 0) s_from = lo;
+    }
+    __syncthreads();
+    for (int64_t i = s_from + (int64_t)threadIdx.x; i < g.n_tokens; i += kThreads) {
+        const int token = a.sorted[i].x;
+        if (token >= end) break;
+        atomicOr(&s_taken[(token - begin) >> 5], 1u << ((token - begin) & 31));
+    }
+    __syncthreads();
+    Cols<Table, kCols> zero;
+    zero.zero();
+    for (int r = threadIdx.x / across; r < end - begin; r += kThreads / across) {
+        if ((s_taken[r >> 5] >> (r & 31)) & 1u) continue;
+        Table* const row = static_cast<Table*>(g.d_table) + (int64_t)(begin + r) * g.table_pitch;
+        for (int c = (threadIdx.x & (across - 1)) * kCols; c < g.width; c += across * kCols) zero.store(row + c);
+    }
+}
+
+// The first `sum_ctas` CTAs sum pieces, the others write zeros, `zero_rows_each` rows each.
 template <typename Grad, typename Table, int kCols>
 __global__ void __launch_bounds__(kThreads)
-embed_sums_kernel(const __grid_constant__ SumArgs a, int across, int tiles) {
+embed_sums_kernel(const __grid_constant__ SumArgs a, int across, int tiles, int sum_ctas, int zero_rows_each) {
     grid_begin();
     const EmbedGradArgs& g = a.g;
+    if ((int)blockIdx.x >= sum_ctas) {
+        const int64_t begin = (int64_t)((int)blockIdx.x - sum_ctas) * zero_rows_each;
+        zero_rows<Table, kCols>(a, (int)begin, (int)min((int64_t)g.vocab, begin + zero_rows_each), across);
+        return;
+    }
     const int tile = blockIdx.x % tiles, piece = (blockIdx.x / tiles) * (kThreads / across) + threadIdx.x / across;
     const int c = (tile * across + (threadIdx.x & (across - 1))) * kCols;
     if (piece >= a.pieces.n || c >= g.width) return;
     const int64_t begin = (int64_t)piece * a.pieces.length, end = min((int64_t)g.n_tokens, begin + a.pieces.length);
     const Grad* const d = static_cast<const Grad*>(g.d_out) + c;
-    bool came = begin > 0 && a.key[begin - 1] == a.key[begin];
+    bool came = begin > 0 && a.sorted[begin - 1].x == a.sorted[begin].x;
     float sum[kCols];
 #pragma unroll
     for (int e = 0; e < kCols; ++e) sum[e] = 0.0f;
-    for (int64_t i0 = begin; i0 < end; i0 += kBatch) {
-        int token[kBatch + 1];
-#pragma unroll
-        for (int k = 0; k <= kBatch; ++k) token[k] = i0 + k < g.n_tokens ? a.key[i0 + k] : g.vocab;
-        Cols<Grad, kCols> v[kBatch];
-#pragma unroll
-        for (int k = 0; k < kBatch; ++k)
-            if (token[k] < g.vocab) v[k].load(d + (int64_t)a.pos[i0 + k] * g.pitch);
+    int token[kBatch + 1], pos[kBatch];                  // of a batch; pieces begin on multiples of it
+    const auto load_ids = [&](int64_t i0) {
 #pragma unroll
         for (int k = 0; k < kBatch; ++k) {
-            if (token[k] >= g.vocab) return;             // nothing but what is no token from here on
+            const int2 one = i0 + k < end ? a.sorted[i0 + k] : make_int2(g.vocab, 0);
+            token[k] = one.x;
+            pos[k] = one.y;
+        }
+        token[kBatch] = i0 + kBatch < g.n_tokens ? a.sorted[i0 + kBatch].x : g.vocab;
+    };
+    load_ids(begin);
+    for (int64_t i0 = begin; i0 < end; i0 += kBatch) {
+        Cols<Grad, kCols> v[kBatch];
+        int here[kBatch + 1];
+#pragma unroll
+        for (int k = 0; k < kBatch; ++k) {
+            if (token[k] < g.vocab) v[k].load(d + (int64_t)pos[k] * g.pitch);
+            here[k] = token[k];
+        }
+        here[kBatch] = token[kBatch];
+        if (end - i0 < kBatch) {                         // the last one: the token behind it
+            const int behind = end < g.n_tokens ? a.sorted[end].x : g.vocab;
+#pragma unroll
+            for (int k = 1; k <= kBatch; ++k)
+                if (i0 + k >= end) here[k] = behind;
+        }
+        if (i0 + kBatch < end) load_ids(i0 + kBatch);
+#pragma unroll
+        for (int k = 0; k < kBatch; ++k) {
+            if (i0 + k >= end || here[k] >= g.vocab) return;         // nothing but what is no token from here on
 #pragma unroll
             for (int e = 0; e < kCols; ++e) sum[e] += v[k].at(e);
-            const bool last = i0 + k + 1 == end, ends = token[k + 1] != token[k];
+            const bool last = i0 + k + 1 == end, ends = here[k + 1] != here[k];
             if (!last && !ends) continue;
             if (ends && !came) {
-                write_row<Table, kCols>(g, token[k], c, sum);
+                write_row<Table, kCols>(g, here[k], c, sum);
             } else {
-                float* const to = a.partial + ((int64_t)piece * 2 + (came ? 0 : 1)) * g.width + c;
-#pragma unroll
-                for (int e = 0; e < kCols; ++e) to[e] = sum[e];
+                Cols<float, kCols> part;
+                part.set(sum);
+                part.store(a.partial + ((int64_t)piece * 2 + (came ? 0 : 1)) * g.width + c);
             }
             came = false;
 #pragma unroll
@@ -294,29 +441,38 @@ embed_join_kernel(const __grid_constant__ SumArgs a, int across, int tiles) {
     const int c = (tile * across + (threadIdx.x & (across - 1))) * kCols;
     if (piece + 1 >= a.pieces.n || c >= g.width) return;
     const int64_t begin = (int64_t)piece * a.pieces.length, end = begin + a.pieces.length;       // not the last piece: it is whole
-    const int token = a.key[end - 1];
-    if (token >= g.vocab || a.key[end] != token) return;
-    if (a.key[begin] == token && begin > 0 && a.key[begin - 1] == token) return;                // began further ahead
+    const int token = a.sorted[end - 1].x;
+    if (token >= g.vocab || a.sorted[end].x != token) return;
+    if (a.sorted[begin].x == token && begin > 0 && a.sorted[begin - 1].x == token) return;                // began further ahead
     float sum[kCols];
-    const float* from = a.partial + ((int64_t)piece * 2 + 1) * g.width + c;
+    Cols<float, kCols> first;
+    first.load(a.partial + ((int64_t)piece * 2 + 1) * g.width + c);
 #pragma unroll
-    for (int e = 0; e < kCols; ++e) sum[e] = from[e];
-    for (int next = piece + 1; next < a.pieces.n && a.key[(int64_t)next * a.pieces.length] == token; ++next) {
-        from = a.partial + (int64_t)next * 2 * g.width + c;
+    for (int e = 0; e < kCols; ++e) sum[e] = first.at(e);
+    // how many of the pieces from `next` on, up to a batch, begin with the run's token
+    const auto count = [&](int next) {
+        int n = 0;
 #pragma unroll
-        for (int e = 0; e < kCols; ++e) sum[e] += from[e];
+        for (int k = 0; k < kBatch; ++k) n += next + k < a.pieces.n && a.sorted[(int64_t)(next + k) * a.pieces.length].x == token;
+        return n;
+    };
+    int next = piece + 1, n = count(next);
+    while (n > 0) {
+        Cols<float, kCols> part[kBatch];
+#pragma unroll
+        for (int k = 0; k < kBatch; ++k) {
+            part[k].zero();
+            if (k < n) part[k].load(a.partial + (int64_t)(next + k) * 2 * g.width + c);
+        }
+        next += kBatch;
+        const int more = n == kBatch ? count(next) : 0;
+#pragma unroll
+        for (int k = 0; k < kBatch; ++k)
+#pragma unroll
+            for (int e = 0; e < kCols; ++e) sum[e] += part[k].at(e);
+        n = more;
     }
     write_row<Table, kCols>(g, token, c, sum);
-}
-
-template <typename Table, int kCols>
-__global__ void __launch_bounds__(kThreads)
-zero_rows_kernel(Table* table, int vocab, int width, int64_t pitch) {
-    grid_begin();
-    Cols<Table, kCols> zero;
-    zero.zero();
-    for (int64_t row = blockIdx.x; row < vocab; row += gridDim.x)
-        for (int c = threadIdx.x * kCols; c < width; c += kThreads * kCols) zero.store(table + row * pitch + c);
 }
 
 // ------------------------------------------------------------------------------------------------- launches
@@ -348,7 +504,7 @@ int embed_with(const EmbedArgs& a, cudaStream_t s) {
 }
 template <typename Table, typename Out>
 int embed_types(const EmbedArgs& a, cudaStream_t s) {
-    constexpr int kMost = 16 / (int)sizeof(Out);
+    constexpr int kMost = 16 / (int)(sizeof(Table) > sizeof(Out) ? sizeof(Table) : sizeof(Out));
     switch (cols_of(kMost, a.table, a.table_pitch, sizeof(Table), a.out, a.pitch, sizeof(Out), a.width)) {
         case 8: if constexpr (kMost == 8) return embed_with<Table, Out, 8>(a, s); else break;
         case 4: return embed_with<Table, Out, 4>(a, s);
@@ -372,10 +528,7 @@ GradScratch grad_scratch(void* ws, int n_tokens, int width) {
         return p;
     };
     GradScratch g;
-    for (int k = 0; k < 2; ++k) {
-        g.sort.key[k] = reinterpret_cast<int32_t*>(take((size_t)n_tokens * 4));
-        g.sort.pos[k] = reinterpret_cast<int32_t*>(take((size_t)n_tokens * 4));
-    }
+    for (int k = 0; k < 2; ++k) g.sort.sorted[k] = reinterpret_cast<int2*>(take((size_t)n_tokens * sizeof(int2)));
     g.sort.count = reinterpret_cast<uint32_t*>(take((size_t)kSortCtas * (sizeof(uint32_t) << kMostBits)));
     g.partial = reinterpret_cast<float*>(take((size_t)pieces_of(n_tokens, width).n * 2 * width * sizeof(float)));
     g.bytes = at;
@@ -385,38 +538,40 @@ GradScratch grad_scratch(void* ws, int n_tokens, int width) {
 template <typename Grad, typename Table, int kCols>
 int embed_grad_with(const SumArgs& a, cudaStream_t s) {
     const Spread sp = spread(a.g.width, kCols, kThreads);
-    const int64_t blocks = ((int64_t)a.pieces.n - 1) / (kThreads / sp.across) + 1;       // times the tiles: below n_tokens * width / 256
-    SR_LAUNCH("embed_sums_kernel", (embed_sums_kernel<Grad, Table, kCols>), (int)(blocks * sp.tiles), kThreads, 0, s, a, sp.across, sp.tiles);
-    SR_LAUNCH("embed_join_kernel", (embed_join_kernel<Table, kCols>), (int)(blocks * sp.tiles), kThreads, 0, s, a, sp.across, sp.tiles);
-    return SR_OK;
-}
-
-template <typename Table, int kCols>
-int zero_rows(const EmbedGradArgs& g, cudaStream_t s) {
-    SR_LAUNCH("zero_rows_kernel", (zero_rows_kernel<Table, kCols>), std::min(g.vocab, 148 * 16), kThreads, 0, s, static_cast<Table*>(g.d_table), g.vocab, g.width, g.table_pitch);
+    const int64_t sum_ctas = a.pieces.n > 0 ? (((int64_t)a.pieces.n - 1) / (kThreads / sp.across) + 1) * sp.tiles : 0;       // below n_tokens * width / 256
+    int zero_each = 0, zero_ctas = 0;
+    if (!a.g.accumulate) {
+        zero_each = std::min(std::max((a.g.vocab - 1) / (148 * 8) + 1, 1), kMostZeroRows);
+        zero_ctas = (a.g.vocab - 1) / zero_each + 1;
+    }
+    if (sum_ctas + zero_ctas == 0) return SR_OK;
+    SR_LAUNCH("embed_sums_kernel", (embed_sums_kernel<Grad, Table, kCols>), (int)(sum_ctas + zero_ctas), kThreads, 0, s, a, sp.across, sp.tiles, (int)sum_ctas, zero_each);
+    if (a.pieces.n > 1) SR_LAUNCH("embed_join_kernel", (embed_join_kernel<Table, kCols>), (int)sum_ctas, kThreads, 0, s, a, sp.across, sp.tiles);
     return SR_OK;
 }
 
 template <typename Grad, typename Table>
 int embed_grad_types(const EmbedGradArgs& g, void* ws, cudaStream_t s) {
-    constexpr int kMost = 16 / (int)sizeof(Grad);
-    const int cols = cols_of(kMost, g.d_out, g.pitch, sizeof(Grad), g.d_table, g.table_pitch, sizeof(Table), g.width);
-    if (!g.accumulate) {
-        const int rc = cols == 8 ? zero_rows<Table, 8>(g, s) : cols == 4 ? zero_rows<Table, 4>(g, s) : cols == 2 ? zero_rows<Table, 2>(g, s) : zero_rows<Table, 1>(g, s);
-        if (rc != SR_OK) return rc;
-    }
-    if (g.n_tokens == 0) return SR_OK;
+    constexpr int kMost = 16 / (int)(sizeof(Table) > sizeof(Grad) ? sizeof(Table) : sizeof(Grad));
     const GradScratch scratch = grad_scratch(ws, g.n_tokens, g.width);
-    int key_bits = 1;
-    while ((g.vocab >> key_bits) != 0) ++key_bits;                       // `vocab` itself stands for what is no token
-    const int passes = (key_bits - 1) / kMostBits + 1, bits = (key_bits - 1) / passes + 1;
-    const int ctas = g.n_tokens > 8192 ? kSortCtas : 1;
-    const size_t smem = (size_t)kSortWarps * sizeof(uint32_t) << bits;
-    SR_CUDA_TRY(cudaFuncSetAttribute(sort_tokens_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)((size_t)kSortWarps * sizeof(uint32_t) << kMostBits)));
-    const int rc = launch_as(true, ctas, "sort_tokens_kernel", sort_tokens_kernel, ctas, kSortThreads, smem, s, g.tokens, g.n_tokens, g.vocab, passes, bits, scratch.sort, g.status);
-    if (rc != SR_OK) return rc;
-    const SumArgs a{g, scratch.sort.key[(passes - 1) & 1], scratch.sort.pos[(passes - 1) & 1], scratch.partial, pieces_of(g.n_tokens, g.width)};
-    switch (cols) {
+    int sorted = 0;                                                      // which of the two buffers
+    if (g.n_tokens > kFewTokens) {
+        int key_bits = 1;
+        while ((g.vocab >> key_bits) != 0) ++key_bits;                   // `vocab` itself stands for what is no token
+        const int passes = (key_bits - 1) / kMostBits + 1, bits = (key_bits - 1) / passes + 1;
+        const size_t smem = (size_t)kSortWarps * sizeof(uint32_t) << bits;
+        SR_CUDA_TRY(cudaFuncSetAttribute(sort_tokens_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)((size_t)kSortWarps * sizeof(uint32_t) << kMostBits)));
+        SR_CUDA_TRY(cudaFuncSetAttribute(sort_tokens_kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
+        const int rc = launch_as(true, kSortCtas, "sort_tokens_kernel", sort_tokens_kernel, kSortCtas, kSortThreads, smem, s, g.tokens, g.n_tokens, g.vocab, passes, bits, scratch.sort,
+                                 g.status);
+        if (rc != SR_OK) return rc;
+        sorted = (passes - 1) & 1;
+    } else if (g.n_tokens > 0) {
+        SR_LAUNCH("rank_tokens_kernel", rank_tokens_kernel, (g.n_tokens - 1) / kRanked + 1, kThreads, (size_t)((g.n_tokens + 31) & ~31) * sizeof(int32_t), s, g.tokens, g.n_tokens, g.vocab,
+                  scratch.sort.sorted[0], g.status);
+    }
+    const SumArgs a{g, scratch.sort.sorted[sorted], scratch.partial, pieces_of(g.n_tokens, g.width)};
+    switch (cols_of(kMost, g.d_out, g.pitch, sizeof(Grad), g.d_table, g.table_pitch, sizeof(Table), g.width)) {
         case 8: if constexpr (kMost == 8) return embed_grad_with<Grad, Table, 8>(a, s); else break;
         case 4: return embed_grad_with<Grad, Table, 4>(a, s);
         case 2: return embed_grad_with<Grad, Table, 2>(a, s);

@@ -16,14 +16,14 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kVecs = 4;                         // a thread's, of a row of the slice
-constexpr int kIdsAhead = 1536;                  // of the next row's history, and of its biases: copied while this row is written
-constexpr int kBiasesAhead = 512;
+constexpr int kIdsAhead = 1024;                  // of the next row's history, and of its biases: copied while this row is written
+constexpr int kBiasesAhead = 256;
 constexpr int kMostLength = 0x3FFFFFFF;          // of a history
 constexpr int kMostBiases = 0xFFFF;              // of a list
 // A token's count, 16 bits: seen in the prompt, in the bias list, and how often behind the prompt.  From kMany on, give or take what
 // the CTA's threads add at once, occurrences are counted in a table of few such tokens.
 constexpr uint32_t kInPrompt = 0x8000u, kBiased = 0x4000u, kTimes = 0x3FFFu, kMany = 0x2000u;
-constexpr int kFrequent = 128;
+constexpr int kFrequent = 64;
 template <typename T>
 constexpr int kSliceOf = kThreads * kVecs * Vec<T>::kElems;
 
@@ -67,14 +67,16 @@ __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_grou
 
 // What a row brings along; written to shared memory a batch of rows at a time, by one warp.
 struct Record {
-    int64_t start, bias_start;
+    int64_t start, bias_start;      // as given,
     int32_t len, prompt, bias_len;
-    int32_t from;                   // positions from here on are new; -1: nothing is as in the row before
+    int64_t from_at, bias_at;       // and of the history (from `from` on) and the list what lies inside their arrays,
+    int32_t n, bias_n, behind;      // with the first of its ids that is behind the prompt
+    int32_t from;                   // positions of the history from here on are new; -1: nothing is as in the row before
     int32_t id;                     // the one new token, where there is one
     int32_t mask, mask_ahead;       // this row's, and that of the row whose mask is looked up in this row's turn
     float repetition, shrink, presence, frequency;      // shrink: its reciprocal
 };
-constexpr int kBatch = 16;
+constexpr int kBatch = 8;
 
 // Tokens that are seen thousands of times, out of line: a call that hardly any row makes.
 __device__ __noinline__ void count_frequent(uint32_t* table, int l) {
@@ -99,21 +101,20 @@ __device__ __noinline__ uint32_t times_frequent(const uint32_t* table, uint32_t 
 // kSparse: out is in, and only vectors that change are read and written.
 // kShift: not all rows of in and out begin on 16 bytes.  The touched tokens are then bits of shared memory, which all threads read, and a
 // barrier stands before and behind each change of them.
-constexpr int kStages = 3;           // rows of the ring: one is changed and written while two are on their way
-
 // Where things lie in dynamic shared memory (bytes).
-template <typename T, bool kBackward, bool kSparse>
+// kStages: rows of the ring, one of which is changed and written while the others are on their way.
+template <typename T, int kStages, bool kBackward>
 struct Layout {
     static constexpr int kSlice = kSliceOf<T>, kRow = kVecs * kThreads * 16;
-    static constexpr int kRaw = (kSparse ? 1 : kStages) * kRow, kCount = kRaw + (kBackward ? kRow : 0), kEntry = kCount + (kBackward ? 0 : kSlice * 2),
+    static constexpr int kRaw = kStages * kRow, kCount = kRaw + (kBackward ? kRow : 0), kEntry = kCount + (kBackward ? 0 : kSlice * 2),
                          kBiasIds = kEntry + kSlice * 2, kBiasValues = kBiasIds + kBiasesAhead * 4, kAll = kBiasValues + 2 * kBiasesAhead * 4;
     static constexpr int bytes(bool counts, bool biases) { return kBackward ? kCount : biases ? kAll : counts ? kEntry : kCount; }
 };
 
-template <typename T, bool kBackward, bool kSparse, bool kShift>
+template <typename T, int kStages, bool kBackward, bool kSparse, bool kShift>
 __global__ void __launch_bounds__(kThreads, 3)
 adjust_kernel(const __grid_constant__ AdjustArgs a, int runs, int rows_per_cta) {
-    using Lay = Layout<T, kBackward, kSparse>;
+    using Lay = Layout<T, kStages, kBackward>;
     constexpr int E = Vec<T>::kElems, kSlice = Lay::kSlice, kBits = E * kVecs;
     static_assert(kBits <= 32, "a bit for each token of a thread's vectors");
     constexpr int kWords = kThreads + 1;                 // at least kSlice / 32 + 1
@@ -150,7 +151,7 @@ adjust_kernel(const __grid_constant__ AdjustArgs a, int runs, int rows_per_cta) 
     uint32_t word = 0u;                                  // touched tokens of the thread's vectors
     bool odd = false;                                    // whether the token is that thread `tid` has behind the vectors
     const auto bits_of_vector = [&](uint32_t w, int k) { return (w >> (k * E)) & kAll; };
-    const auto stage_of = [&](int row) { return reinterpret_cast<uint4*>(s_bytes) + (kSparse ? 0 : (row - (int)row0) % kStages * (kVecs * kThreads)); };
+    const auto stage_of = [&](int row) { return reinterpret_cast<uint4*>(s_bytes) + (row - (int)row0) % kStages * (kVecs * kThreads); };
 
     if (counts) {
         for (int i = tid; i < kSlice / 8; i += kThreads) {
@@ -198,7 +199,7 @@ adjust_kernel(const __grid_constant__ AdjustArgs a, int runs, int rows_per_cta) 
 
     // The turn of a row looks up the mask of the row kDepth behind it, has the vectors of the row before that one copied into the ring,
     // and changes and writes its own.  The first turns are those of no row.
-    constexpr int kDepth = kSparse ? 1 : kStages;
+    constexpr int kDepth = kStages;
     uint32_t allowed[kDepth];                            // of the thread's vectors, from this row on
     int head_ahead = 0, vecs_ahead = vecs;               // of the row that is looked up; the same for all but in kShift
     if (kShift) split(in, out, head_ahead, vecs_ahead);
@@ -211,19 +212,16 @@ adjust_kernel(const __grid_constant__ AdjustArgs a, int runs, int rows_per_cta) 
     int at = kBatch;                                     // of the records
     int half = 0;                                        // of s_touched and s_bias_values, for the row at hand
     // the ids of a row that begins anew, on their way to shared memory while the one before it is written
-    const auto copy_ids = [&](int64_t start, int len, int64_t bias_start, int bias_len) {
-        int64_t from;
+    const auto copy_ids = [&](int64_t from_at, int n, int64_t bias_at, int bias_n) {
         if (histories) {
-            const int ids_n = min(inside(start, len, a.n_history, from), kIdsAhead);
 #pragma unroll 1
-            for (int c = tid; c < ids_n; c += kThreads) copy_word(&s_ids[c], a.history + from + c);
+            for (int c = tid; c < min(n, kIdsAhead); c += kThreads) copy_word(&s_ids[c], a.history + from_at + c);
         }
         if (biases) {
-            const int ids_n = min(inside(bias_start, bias_len, a.n_bias, from), kBiasesAhead);
 #pragma unroll 1
-            for (int c = tid; c < ids_n; c += kThreads) {
-                copy_word(&s_bias_ids[c], a.bias_token + from + c);
-                copy_word(&s_bias_values[(half ^ 1) * kBiasesAhead + c], a.bias_value + from + c);
+            for (int c = tid; c < min(bias_n, kBiasesAhead); c += kThreads) {
+                copy_word(&s_bias_ids[c], a.bias_token + bias_at + c);
+                copy_word(&s_bias_values[(half ^ 1) * kBiasesAhead + c], a.bias_value + bias_at + c);
             }
         }
     };
@@ -231,7 +229,9 @@ adjust_kernel(const __grid_constant__ AdjustArgs a, int runs, int rows_per_cta) 
     {
         const int64_t start = histories ? a.history_start[row0] : 0, bias_start = biases ? a.bias_start[row0] : 0;
         const int len = histories ? a.history_len[row0] : 0, bias_len = biases ? a.bias_len[row0] : 0;
-        copy_ids(start, min(len, kMostLength), bias_start, min(bias_len, kMostBiases));
+        int64_t from_at, bias_at;
+        const int ids_n = inside(start, min(len, kMostLength), a.n_history, from_at), bias_n = inside(bias_start, min(bias_len, kMostBiases), a.n_bias, bias_at);
+        copy_ids(from_at, ids_n, bias_at, bias_n);
         copies_end();
     }
     uint32_t raw_ahead = 0u;                             // touched vectors whose logits are on their way
@@ -282,6 +282,10 @@ adjust_kernel(const __grid_constant__ AdjustArgs a, int runs, int rows_per_cta) 
                     const bool same = mine > row0 && r.start == before.start && r.prompt == before.prompt && r.len >= before.len && r.bias_start == before.bias_start &&
                                       r.bias_len == before.bias_len;
                     r.from = same ? before.len : -1;
+                    const int done = max(r.from, 0);
+                    r.n = inside(r.start + done, r.len - done, a.n_history, r.from_at);
+                    r.behind = (int)(r.prompt - (r.from_at - r.start));
+                    r.bias_n = inside(r.bias_start, r.bias_len, a.n_bias, r.bias_at);
                     r.id = -1;
                     if (real && same && r.len == before.len + 1) {
                         const int64_t pos = r.start + before.len;
@@ -350,12 +354,8 @@ adjust_kernel(const __grid_constant__ AdjustArgs a, int runs, int rows_per_cta) 
                 if (copied) copies_wait<kBackward ? 2 : 1>();
 #pragma unroll 1
                 for (int pass = biases && r.from < 0 ? 0 : 1; pass < 1 + histories; ++pass) {
-                    int64_t from;
-                    const int done = pass == 0 ? 0 : max(r.from, 0);
-                    const int64_t start = (pass == 0 ? r.bias_start : r.start) + done;
-                    const int ids_n = inside(start, (pass == 0 ? r.bias_len : r.len) - done, pass == 0 ? a.n_bias : a.n_history, from);
-                    const int32_t* const ids = (pass == 0 ? a.bias_token : a.history) + from;
-                    const int behind = pass == 0 ? 0 : (int)(r.prompt - done - (from - start));      // the first id behind the prompt
+                    const int ids_n = pass == 0 ? r.bias_n : r.n, behind = r.behind;
+                    const int32_t* const ids = pass == 0 ? a.bias_token + r.bias_at : a.history + r.from_at;
                     const auto one = [&](int c, int32_t id) {
                         const uint32_t l = (uint32_t)id - (uint32_t)first;
                         if (id < 0 || l >= (uint32_t)n) {
@@ -393,7 +393,7 @@ adjust_kernel(const __grid_constant__ AdjustArgs a, int runs, int rows_per_cta) 
 #pragma unroll 1
                         for (; c < held_n; c += kThreads) one(c, held[c]);
                     } else if (pass == 0) {
-                        for (int k = tid; k < min(ids_n, kBiasesAhead); k += kThreads) s_bias_values[half * kBiasesAhead + k] = a.bias_value[from + k];
+                        for (int k = tid; k < min(ids_n, kBiasesAhead); k += kThreads) s_bias_values[half * kBiasesAhead + k] = a.bias_value[r.bias_at + k];
                     }
 #pragma unroll 1
                     for (; c < ids_n; c += 4 * kThreads) {
@@ -437,7 +437,7 @@ adjust_kernel(const __grid_constant__ AdjustArgs a, int runs, int rows_per_cta) 
             }
 
             ids_ahead = at < kBatch && row + 1 < row_end && s_record[at < kBatch ? at : 0].from < 0;
-            if (ids_ahead) copy_ids(s_record[at].start, s_record[at].len, s_record[at].bias_start, s_record[at].bias_len);
+            if (ids_ahead) copy_ids(s_record[at].from_at, s_record[at].n, s_record[at].bias_at, s_record[at].bias_n);
         }
         copies_end();
 
@@ -476,7 +476,7 @@ adjust_kernel(const __grid_constant__ AdjustArgs a, int runs, int rows_per_cta) 
                 v = times ? less : v;
                 if (c & kBiased) {
                     const int e = (int)entry[l] - 1;
-                    v += e < kBiasesAhead ? s_bias_values[half * kBiasesAhead + e] : a.bias_value[max(r.bias_start, (int64_t)0) + e];
+                    v += e < kBiasesAhead ? s_bias_values[half * kBiasesAhead + e] : a.bias_value[r.bias_at + e];
                 }
                 return v;
             };
@@ -552,7 +552,7 @@ adjust_kernel(const __grid_constant__ AdjustArgs a, int runs, int rows_per_cta) 
     if (a.status && flags) atomicOr(a.status, flags);
 }
 
-template <typename T, bool kBackward, bool kSparse, bool kShift>
+template <typename T, int kStages, bool kBackward, bool kSparse, bool kShift>
 int launch_form(const AdjustArgs& a, cudaStream_t s) {
     constexpr int kSlice = kSliceOf<T>;
     const int slices = (a.vocab - 1) / kSlice + 1;
@@ -563,9 +563,9 @@ int launch_form(const AdjustArgs& a, cudaStream_t s) {
     int64_t rows = std::min<int64_t>((units - 1) / (148 * 3 * 2) + 1, 64);   // two turns of three CTAs
     rows = std::max(rows, (units - 1) / (INT32_MAX - slices) + 1);           // CTAs are numbered in 31 bits
     const int64_t runs = (a.n_rows - 1) / rows + 1, ctas = slices * runs;
-    using Lay = Layout<T, kBackward, kSparse>;
+    using Lay = Layout<T, kStages, kBackward>;
     const int smem = Lay::bytes(a.history_start != nullptr, a.bias_value != nullptr);
-    const auto kernel = adjust_kernel<T, kBackward, kSparse, kShift>;
+    const auto kernel = adjust_kernel<T, kStages, kBackward, kSparse, kShift>;
     SR_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, Lay::kAll));
     SR_LAUNCH("adjust_kernel", kernel, (int)ctas, kThreads, (size_t)smem, s, a, (int)runs, (int)rows);
     return SR_OK;
@@ -573,10 +573,11 @@ int launch_form(const AdjustArgs& a, cudaStream_t s) {
 template <typename T, bool kBackward>
 int launch_type(const AdjustArgs& a, cudaStream_t s) {
     const auto on_16 = [&](const void* p, int64_t pitch) { return reinterpret_cast<uintptr_t>(p) % 16 == 0 && (a.n_rows == 1 || pitch * (int64_t)sizeof(T) % 16 == 0); };
-    const bool in_place = a.in == a.out;
-    if (!on_16(a.in, a.pitch) || !on_16(a.out, a.out_pitch)) return in_place ? launch_form<T, kBackward, true, true>(a, s) : launch_form<T, kBackward, false, true>(a, s);
-    if (in_place) return launch_form<T, kBackward, true, false>(a, s);
-    return launch_form<T, kBackward, false, false>(a, s);
+    const bool shift = !on_16(a.in, a.pitch) || !on_16(a.out, a.out_pitch);
+    if (a.in == a.out) return shift ? launch_form<T, 1, kBackward, true, true>(a, s) : launch_form<T, 1, kBackward, true, false>(a, s);
+    // A ring of three rows; with biases one of two, so that as many CTAs have room on an SM.
+    if (!kBackward && a.bias_value) return shift ? launch_form<T, 2, kBackward, false, true>(a, s) : launch_form<T, 2, kBackward, false, false>(a, s);
+    return shift ? launch_form<T, 3, kBackward, false, true>(a, s) : launch_form<T, 3, kBackward, false, false>(a, s);
 }
 
 }  // namespace

@@ -112,7 +112,7 @@ struct Layout {
 };
 
 template <typename T, int kStages, bool kBackward, bool kSparse, bool kShift>
-__global__ void __launch_bounds__(kThreads, 3)
+__global__ void __launch_bounds__(kThreads, kStages == 3 ? 3 : 4)
 adjust_kernel(const __grid_constant__ AdjustArgs a, int runs, int rows_per_cta) {
     using Lay = Layout<T, kStages, kBackward>;
     constexpr int E = Vec<T>::kElems, kSlice = Lay::kSlice, kBits = E * kVecs;
@@ -151,7 +151,6 @@ adjust_kernel(const __grid_constant__ AdjustArgs a, int runs, int rows_per_cta) 
     uint32_t word = 0u;                                  // touched tokens of the thread's vectors
     bool odd = false;                                    // whether the token is that thread `tid` has behind the vectors
     const auto bits_of_vector = [&](uint32_t w, int k) { return (w >> (k * E)) & kAll; };
-    const auto stage_of = [&](int row) { return reinterpret_cast<uint4*>(s_bytes) + (row - (int)row0) % kStages * (kVecs * kThreads); };
 
     if (counts) {
         for (int i = tid; i < kSlice / 8; i += kThreads) {
@@ -210,6 +209,10 @@ adjust_kernel(const __grid_constant__ AdjustArgs a, int runs, int rows_per_cta) 
         if (a.allowed) allowed[kDepth - 1] = bits_of(words_of(m, head_ahead, vecs_ahead), m, head_ahead);
     }
     int at = kBatch;                                     // of the records
+    constexpr int kFull = kVecs * kThreads;              // vectors of a whole slice
+    uint4* const ring = reinterpret_cast<uint4*>(s_bytes) + tid;
+    int fill = 0, take = 0;                              // its rows that are next
+    const T* in_ahead = in;
     int half = 0;                                        // of s_touched and s_bias_values, for the row at hand
     // the ids of a row that begins anew, on their way to shared memory while the one before it is written
     const auto copy_ids = [&](int64_t from_at, int n, int64_t bias_at, int bias_n) {
@@ -351,7 +354,7 @@ adjust_kernel(const __grid_constant__ AdjustArgs a, int runs, int rows_per_cta) 
                 }
                 // ids of the bias list, then of the history, in the slice
                 const bool copied = ids_ahead && r.from < 0;
-                if (copied) copies_wait<kBackward ? 2 : 1>();
+                if (copied) copies_wait<kSparse ? 0 : kBackward ? 2 : 1>();
 #pragma unroll 1
                 for (int pass = biases && r.from < 0 ? 0 : 1; pass < 1 + histories; ++pass) {
                     const int ids_n = pass == 0 ? r.bias_n : r.n, behind = r.behind;
@@ -444,13 +447,14 @@ adjust_kernel(const __grid_constant__ AdjustArgs a, int runs, int rows_per_cta) 
         // vectors of the last row that was looked up, and the mask of the next one
         MaskWords words = {};
         if (!kSparse) {
-            const int ahead = row + kDepth - 1;
-            if (ahead < row_end) {
-                const uint4* const p = reinterpret_cast<const uint4*>(static_cast<const T*>(a.in) + ahead * a.pitch + first + head_ahead) + tid;
-                uint4* const to = stage_of(ahead) + tid;
+            if (row + kDepth - 1 < row_end) {
+                const uint4* const p = reinterpret_cast<const uint4*>(in_ahead + head_ahead) + tid;
+                uint4* const to = ring + fill * kFull;
 #pragma unroll
                 for (int k = 0; k < kVecs; ++k)
                     if (tid + k * kThreads < vecs_ahead && bits_of_vector(allowed[kDepth - 1], k) != 0u) copy_vector(to + k * kThreads, p + k * kThreads);
+                in_ahead += a.pitch;
+                fill = fill == kStages - 1 ? 0 : fill + 1;
             }
         }
         copies_end();
@@ -482,13 +486,14 @@ adjust_kernel(const __grid_constant__ AdjustArgs a, int runs, int rows_per_cta) 
             };
             // elements in no vector
 #pragma unroll 1
-            for (int i = tid; i < n - vecs * E; i += kThreads) {
+            for (int i = tid; (kShift || vecs != kFull) && i < n - vecs * E; i += kThreads) {
                 const int l = i < head ? i : i + vecs * E;
                 if (r.mask >= 0 && !((mask_at(r.mask)[l >> 5] >> (l & 31)) & 1u)) out[l] = banned_value<T>(kBackward);
                 else if (kShift ? (s_touched[half][l >> 5] >> (l & 31)) & 1u : odd) out[l] = from_float<T>(changed(l, to_float(in[l]), kBackward && to_float(raw[l]) > 0.0f));
                 else if (!kSparse) out[l] = in[l];
             }
-            uint4* const mine = stage_of(row) + tid;     // the thread's vectors
+            uint4* const mine = ring + take * kFull;     // the thread's vectors
+            take = take == kStages - 1 ? 0 : take + 1;
             if (kSparse) {
                 const uint4* p = reinterpret_cast<const uint4*>(in + head) + tid;
 #pragma unroll
@@ -560,7 +565,7 @@ int launch_form(const AdjustArgs& a, cudaStream_t s) {
     // leave every SM a few turns.  Slices go from the lowest ids on: with most vocabularies these are the tokens that are seen most often, and
     // whose CTAs take longest.
     const int64_t units = (int64_t)slices * a.n_rows;
-    int64_t rows = std::min<int64_t>((units - 1) / (148 * 3 * 2) + 1, 64);   // two turns of three CTAs
+    int64_t rows = std::min<int64_t>((units - 1) / (148 * (kStages == 3 ? 3 : 4) * 2) + 1, 64);
     rows = std::max(rows, (units - 1) / (INT32_MAX - slices) + 1);           // CTAs are numbered in 31 bits
     const int64_t runs = (a.n_rows - 1) / rows + 1, ctas = slices * runs;
     using Lay = Layout<T, kStages, kBackward>;
@@ -575,9 +580,12 @@ int launch_type(const AdjustArgs& a, cudaStream_t s) {
     const auto on_16 = [&](const void* p, int64_t pitch) { return reinterpret_cast<uintptr_t>(p) % 16 == 0 && (a.n_rows == 1 || pitch * (int64_t)sizeof(T) % 16 == 0); };
     const bool shift = !on_16(a.in, a.pitch) || !on_16(a.out, a.out_pitch);
     if (a.in == a.out) return shift ? launch_form<T, 1, kBackward, true, true>(a, s) : launch_form<T, 1, kBackward, true, false>(a, s);
-    // A ring of three rows; with biases one of two, so that as many CTAs have room on an SM.
-    if (!kBackward && a.bias_value) return shift ? launch_form<T, 2, kBackward, false, true>(a, s) : launch_form<T, 2, kBackward, false, false>(a, s);
-    return shift ? launch_form<T, 3, kBackward, false, true>(a, s) : launch_form<T, 3, kBackward, false, false>(a, s);
+    // Rows that mostly begin anew (many ids a row) wait for their tables, not for memory: a ring of two rows leaves room for a fourth CTA (512 rows of 151936
+    // bf16 with penalties 88 -> 71 us).  Rows that go on where others ended stream: three rows, three CTAs (4096 of them 433 -> 410).
+    // Biases take the room of a fourth CTA in any case, and the gradient has no counts that would (2048 rows 206 -> 180).
+    const bool streams = !kBackward && a.bias_value == nullptr && a.n_history <= 8 * (int64_t)a.n_rows;
+    if (streams) return shift ? launch_form<T, 3, false, false, true>(a, s) : launch_form<T, 3, false, false, false>(a, s);
+    return shift ? launch_form<T, 2, kBackward, false, true>(a, s) : launch_form<T, 2, kBackward, false, false>(a, s);
 }
 
 }  // namespace

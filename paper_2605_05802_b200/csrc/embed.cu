@@ -126,13 +126,57 @@ __device__ __forceinline__ int2 load_l2(const int2* p) {
 }
 __device__ __forceinline__ uint32_t below(uint32_t peers) { return __popc(peers & ((1u << (threadIdx.x & 31)) - 1u)); }
 
+// Rows of the table that are zeroed while the tokens are sorted: a run of them, on a boundary of `vec` bytes each.
+struct ZeroRows {
+    char* table;
+    int64_t pitch;                  // bytes
+    int width, vec, rows;           // bytes of a row, of a store; rows from the first on
+};
+constexpr int kZeroCtas = 112;      // with those that sort eight clusters: what the GPU's eight parts run at once
+template <typename W>
+__device__ __forceinline__ void zero_row(char* row, int width, int lane) {
+    for (int c = lane * (int)sizeof(W); c < width; c += 32 * (int)sizeof(W)) __stcs(reinterpret_cast<W*>(row + c), W());
+}
+// The CTA's share, without those that a token took; bits of them in shared memory.
+__device__ __forceinline__ void zero_share(const ZeroRows& z, const int32_t* tokens, int n, int share, uint32_t* taken, int most) {
+    const int each = (z.rows - 1) / kZeroCtas + 1;
+    for (int64_t begin = (int64_t)share * each; begin < min((int64_t)z.rows, (int64_t)(share + 1) * each); begin += most) {
+        const int rows = (int)min(min((int64_t)z.rows, (int64_t)(share + 1) * each) - begin, (int64_t)most);
+        __syncthreads();
+        for (int i = threadIdx.x; i < (rows + 31) / 32; i += blockDim.x) taken[i] = 0u;
+        __syncthreads();
+        for (int64_t i0 = threadIdx.x; i0 < n; i0 += 8 * (int64_t)blockDim.x) {
+            int32_t t[8];
+#pragma unroll
+            for (int u = 0; u < 8; ++u) t[u] = i0 + u * (int64_t)blockDim.x < n ? tokens[i0 + u * (int64_t)blockDim.x] : -1;
+#pragma unroll
+            for (int u = 0; u < 8; ++u)
+                if (t[u] >= begin && t[u] < begin + rows) atomicOr(&taken[(t[u] - (int)begin) >> 5], 1u << ((t[u] - (int)begin) & 31));
+        }
+        __syncthreads();
+        const int lane = threadIdx.x & 31;
+        for (int r = threadIdx.x >> 5; r < rows; r += blockDim.x >> 5) {
+            if ((taken[r >> 5] >> (r & 31)) & 1u) continue;
+            char* const row = z.table + (begin + r) * z.pitch;
+            if (z.vec == 16) zero_row<uint4>(row, z.width, lane);
+            else if (z.vec == 8) zero_row<uint2>(row, z.width, lane);
+            else if (z.vec == 4) zero_row<uint32_t>(row, z.width, lane);
+            else zero_row<unsigned short>(row, z.width, lane);
+        }
+    }
+}
+
 constexpr int kHeld = 8;            // tokens a lane loads at a time; as many are held from counting to placing
 __global__ void __launch_bounds__(kSortThreads)
-sort_tokens_kernel(const int32_t* tokens, int n, int vocab, int passes, int bits, SortScratch ws, int32_t* status) {
+sort_tokens_kernel(const int32_t* tokens, int n, int vocab, int passes, int bits, SortScratch ws, ZeroRows zero, int32_t* status) {
     extern __shared__ __align__(16) uint32_t s_hist[];  // [kSortWarps][bins]
     __shared__ uint32_t s_base[1 << kMostBits], s_warp[kSortWarps];
     grid_begin();
-    const int ctas = gridDim.x, cta = blockIdx.x, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    if (blockIdx.x >= kSortCtas) {                       // other clusters
+        zero_share(zero, tokens, n, blockIdx.x - kSortCtas, s_hist, kSortWarps << bits);
+        return;
+    }
+    const int ctas = kSortCtas, cta = blockIdx.x, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int bins = 1 << bits;
     const int64_t a_warp = (((int64_t)n - 1) / (ctas * kSortThreads) + 1) * 32;       // tokens, a multiple of 32
     const int64_t begin = ((int64_t)cta * kSortWarps + warp) * a_warp, end = min((int64_t)n, begin + a_warp);
@@ -194,7 +238,7 @@ sort_tokens_kernel(const int32_t* tokens, int n, int vocab, int passes, int bits
         if (b < bins) {
             uint32_t v[kSortCtas];
 #pragma unroll
-            for (int c = 0; c < kSortCtas; ++c) v[c] = c < ctas ? (uint32_t)load_l2(ws.count + (c << kMostBits) + b) : 0u;
+            for (int c = 0; c < kSortCtas; ++c) v[c] = (uint32_t)load_l2(ws.count + (c << kMostBits) + b);
 #pragma unroll
             for (int c = 0; c < kSortCtas; ++c) {
                 before += c < cta ? v[c] : 0u;
@@ -363,14 +407,14 @@ __device__ __forceinline__ void zero_rows(const SumArgs& a, int begin, int end, 
     }
 }
 
-// The first `sum_ctas` CTAs sum pieces, the others write zeros, `zero_rows_each` rows each.
+// The first `sum_ctas` CTAs sum pieces, the others write zeros, `zero_rows_each` rows each from row `zero_first` on.
 template <typename Grad, typename Table, int kCols>
 __global__ void __launch_bounds__(kThreads)
-embed_sums_kernel(const __grid_constant__ SumArgs a, int across, int tiles, int sum_ctas, int zero_rows_each) {
+embed_sums_kernel(const __grid_constant__ SumArgs a, int across, int tiles, int sum_ctas, int zero_first, int zero_rows_each) {
     grid_begin();
     const EmbedGradArgs& g = a.g;
     if ((int)blockIdx.x >= sum_ctas) {
-        const int64_t begin = (int64_t)((int)blockIdx.x - sum_ctas) * zero_rows_each;
+        const int64_t begin = zero_first + (int64_t)((int)blockIdx.x - sum_ctas) * zero_rows_each;
         zero_rows<Table, kCols>(a, (int)begin, (int)min((int64_t)g.vocab, begin + zero_rows_each), across);
         return;
     }
@@ -536,16 +580,16 @@ GradScratch grad_scratch(void* ws, int n_tokens, int width) {
 }
 
 template <typename Grad, typename Table, int kCols>
-int embed_grad_with(const SumArgs& a, cudaStream_t s) {
+int embed_grad_with(const SumArgs& a, int zeroed, cudaStream_t s) {
     const Spread sp = spread(a.g.width, kCols, kThreads);
     const int64_t sum_ctas = a.pieces.n > 0 ? (((int64_t)a.pieces.n - 1) / (kThreads / sp.across) + 1) * sp.tiles : 0;       // below n_tokens * width / 256
     int zero_each = 0, zero_ctas = 0;
-    if (!a.g.accumulate) {
-        zero_each = std::min(std::max((a.g.vocab - 1) / (148 * 8) + 1, 1), kMostZeroRows);
-        zero_ctas = (a.g.vocab - 1) / zero_each + 1;
+    if (!a.g.accumulate && zeroed < a.g.vocab) {         // the rows from `zeroed` on
+        zero_each = std::min((a.g.vocab - zeroed - 1) / (148 * 8) + 1, kMostZeroRows);
+        zero_ctas = (a.g.vocab - zeroed - 1) / zero_each + 1;
     }
     if (sum_ctas + zero_ctas == 0) return SR_OK;
-    SR_LAUNCH("embed_sums_kernel", (embed_sums_kernel<Grad, Table, kCols>), (int)(sum_ctas + zero_ctas), kThreads, 0, s, a, sp.across, sp.tiles, (int)sum_ctas, zero_each);
+    SR_LAUNCH("embed_sums_kernel", (embed_sums_kernel<Grad, Table, kCols>), (int)(sum_ctas + zero_ctas), kThreads, 0, s, a, sp.across, sp.tiles, (int)sum_ctas, zeroed, zero_each);
     if (a.pieces.n > 1) SR_LAUNCH("embed_join_kernel", (embed_join_kernel<Table, kCols>), (int)sum_ctas, kThreads, 0, s, a, sp.across, sp.tiles);
     return SR_OK;
 }
@@ -554,7 +598,8 @@ template <typename Grad, typename Table>
 int embed_grad_types(const EmbedGradArgs& g, void* ws, cudaStream_t s) {
     constexpr int kMost = 16 / (int)(sizeof(Table) > sizeof(Grad) ? sizeof(Table) : sizeof(Grad));
     const GradScratch scratch = grad_scratch(ws, g.n_tokens, g.width);
-    int sorted = 0;                                                      // which of the two buffers
+    int sorted = 0, zeroed = 0;                                          // which of the two buffers; rows of the table that are zeroed by then
+    const int cols = cols_of(kMost, g.d_out, g.pitch, sizeof(Grad), g.d_table, g.table_pitch, sizeof(Table), g.width);
     if (g.n_tokens > kFewTokens) {
         int key_bits = 1;
         while ((g.vocab >> key_bits) != 0) ++key_bits;                   // `vocab` itself stands for what is no token
@@ -562,7 +607,13 @@ int embed_grad_types(const EmbedGradArgs& g, void* ws, cudaStream_t s) {
         const size_t smem = (size_t)kSortWarps * sizeof(uint32_t) << bits;
         SR_CUDA_TRY(cudaFuncSetAttribute(sort_tokens_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)((size_t)kSortWarps * sizeof(uint32_t) << kMostBits)));
         SR_CUDA_TRY(cudaFuncSetAttribute(sort_tokens_kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
-        const int rc = launch_as(true, kSortCtas, "sort_tokens_kernel", sort_tokens_kernel, kSortCtas, kSortThreads, smem, s, g.tokens, g.n_tokens, g.vocab, passes, bits, scratch.sort,
+        ZeroRows zero = {static_cast<char*>(g.d_table), g.table_pitch * (int64_t)sizeof(Table), g.width * (int)sizeof(Table), std::min(16, cols * (int)sizeof(Table)), 0};
+        if (!g.accumulate) {                                             // what takes as long as sorting, less the time to look through the tokens; 4 MB a us
+            const double bytes = (9.0 + g.n_tokens / 6000.0) * 4e6;
+            zeroed = zero.rows = (int)std::min<double>(g.vocab, bytes / zero.width);
+        }
+        const int ctas = kSortCtas + (zeroed > 0 ? kZeroCtas : 0);
+        const int rc = launch_as(true, kSortCtas, "sort_tokens_kernel", sort_tokens_kernel, ctas, kSortThreads, smem, s, g.tokens, g.n_tokens, g.vocab, passes, bits, scratch.sort, zero,
                                  g.status);
         if (rc != SR_OK) return rc;
         sorted = (passes - 1) & 1;
@@ -571,13 +622,13 @@ int embed_grad_types(const EmbedGradArgs& g, void* ws, cudaStream_t s) {
                   scratch.sort.sorted[0], g.status);
     }
     const SumArgs a{g, scratch.sort.sorted[sorted], scratch.partial, pieces_of(g.n_tokens, g.width)};
-    switch (cols_of(kMost, g.d_out, g.pitch, sizeof(Grad), g.d_table, g.table_pitch, sizeof(Table), g.width)) {
-        case 8: if constexpr (kMost == 8) return embed_grad_with<Grad, Table, 8>(a, s); else break;
-        case 4: return embed_grad_with<Grad, Table, 4>(a, s);
-        case 2: return embed_grad_with<Grad, Table, 2>(a, s);
+    switch (cols) {
+        case 8: if constexpr (kMost == 8) return embed_grad_with<Grad, Table, 8>(a, zeroed, s); else break;
+        case 4: return embed_grad_with<Grad, Table, 4>(a, zeroed, s);
+        case 2: return embed_grad_with<Grad, Table, 2>(a, zeroed, s);
         default: break;
     }
-    return embed_grad_with<Grad, Table, 1>(a, s);
+    return embed_grad_with<Grad, Table, 1>(a, zeroed, s);
 }
 
 }  // namespace

@@ -51,6 +51,16 @@ struct Cols {
 
 constexpr int kThreads = 256;
 
+// Zeros to a row of `bytes`, by lanes 0 .. across - 1.  kWide: all rows are whole vectors of 16 bytes.  Otherwise they are vectors wherever
+// the row begins, and two bytes at a time before and behind.
+template <bool kWide>
+__device__ __forceinline__ void zero_row(char* row, int bytes, int lane, int across) {
+    const int head = kWide ? 0 : min(bytes, (int)(-reinterpret_cast<intptr_t>(row) & 15)), body = kWide ? bytes : (bytes - head) & ~15;
+    for (int c = lane * 16; c < body; c += across * 16) __stcs(reinterpret_cast<uint4*>(row + head + c), make_uint4(0u, 0u, 0u, 0u));
+    if (!kWide)
+        for (int c = lane * 2; c < bytes - body; c += across * 2) *reinterpret_cast<uint16_t*>(row + (c < head ? c : c + body)) = 0;
+}
+
 // How threads are spread over rows of `width` elements: `across` of them (a power of two) next to one another.
 struct Spread {
     int across, tiles;
@@ -99,6 +109,94 @@ embed_kernel(const __grid_constant__ EmbedArgs a, int across, int tiles) {
     if (bad && c == 0 && a.status) atomicOr(a.status, SR_STATUS_BAD_TARGET);
 }
 
+// Rows that do not lie on 16 bytes: a thread makes one aligned vector of the output from the aligned vectors that hold its elements in the
+// table, moved against each other by what the two rows differ.  Vectors that reach out of the table go element by element.
+constexpr int kShiftRows = 4;
+template <typename Table, typename Out>
+__global__ void __launch_bounds__(kThreads)
+embed_shift_kernel(const __grid_constant__ EmbedArgs a, int across, int tiles) {
+    constexpr int E = 16 / (int)sizeof(Out);             // elements of an output vector
+    constexpr int kParts = E * (int)sizeof(Table) / 16 + 1, kEach = 16 / (int)sizeof(Table);
+    grid_begin();
+    const int groups = kThreads / across, tile = blockIdx.x % tiles, lane = threadIdx.x & (across - 1);
+    const int64_t t0 = ((int64_t)(blockIdx.x / tiles) * groups + threadIdx.x / across) * kShiftRows;
+    const Table* const table = static_cast<const Table*>(a.table);
+    const uintptr_t begin = reinterpret_cast<uintptr_t>(table), end = begin + ((uintptr_t)(a.vocab - 1) * a.table_pitch + a.width) * sizeof(Table);
+    int id[kShiftRows];
+    bool bad = false;
+#pragma unroll
+    for (int k = 0; k < kShiftRows; ++k) {
+        id[k] = t0 + k < a.n_tokens ? a.tokens[t0 + k] : -1;
+        bad |= id[k] >= a.vocab;
+        if (id[k] >= a.vocab) id[k] = -1;
+    }
+    // where the thread's vector of a row lies: elements before it, and how many of it are the row's
+    const auto place = [&](int k, int& c) {
+        const int off = (int)(reinterpret_cast<uintptr_t>(static_cast<Out*>(a.out) + (t0 + k) * a.pitch) & 15) / (int)sizeof(Out);
+        c = (tile * across + lane) * E - off;
+        return t0 + k < a.n_tokens && c < a.width;
+    };
+    uint4 part[kShiftRows][kParts];
+#pragma unroll
+    for (int k = 0; k < kShiftRows; ++k) {
+        int c;
+        const bool real = place(k, c) && id[k] >= 0;
+        const uintptr_t from = (begin + ((uintptr_t)(real ? id[k] : 0) * a.table_pitch) * sizeof(Table) + (intptr_t)c * (int)sizeof(Table)) & ~(uintptr_t)15;
+#pragma unroll
+        for (int i = 0; i < kParts; ++i) {
+            part[k][i] = make_uint4(0u, 0u, 0u, 0u);
+            if (real && from + 16 * i >= begin && from + 16 * i + 16 <= end) part[k][i] = *reinterpret_cast<const uint4*>(from + 16 * i);
+        }
+    }
+#pragma unroll
+    for (int k = 0; k < kShiftRows; ++k) {
+        int c;
+        if (!place(k, c)) continue;
+        Out* const out = static_cast<Out*>(a.out) + (t0 + k) * a.pitch + c;
+        const Table* const row = table + (int64_t)(id[k] >= 0 ? id[k] : 0) * a.table_pitch + c;
+        const uintptr_t at = reinterpret_cast<uintptr_t>(row);
+        const int shift = (int)(at & 15) / (int)sizeof(Table);
+        float x[E];
+        if (id[k] >= 0 && ((at & ~(uintptr_t)15) < begin || (at & ~(uintptr_t)15) + 16 * kParts > end)) {
+#pragma unroll
+            for (int e = 0; e < E; ++e) x[e] = c + e >= 0 && c + e < a.width ? a.scale * to_float(row[e]) : 0.0f;
+        } else {
+            uint32_t w[4 * kParts];
+#pragma unroll
+            for (int i = 0; i < kParts; ++i) {
+                w[4 * i] = part[k][i].x;
+                w[4 * i + 1] = part[k][i].y;
+                w[4 * i + 2] = part[k][i].z;
+                w[4 * i + 3] = part[k][i].w;
+            }
+            const int words = shift * (int)sizeof(Table) / 4;
+#pragma unroll
+            for (int i = 0; i + 2 < 4 * kParts; ++i) w[i] = words & 2 ? w[i + 2] : w[i];
+#pragma unroll
+            for (int i = 0; i + 1 < 4 * kParts; ++i) w[i] = words & 1 ? w[i + 1] : w[i];
+            if (sizeof(Table) == 2) {
+#pragma unroll
+                for (int i = 0; i + 1 < 4 * kParts; ++i) w[i] = __funnelshift_r(w[i], w[i + 1], (shift & 1) * 16);
+            }
+#pragma unroll
+            for (int i = 0; i < E / kEach; ++i) {
+                float y[kEach];
+                unpack(make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]), y, Table());
+#pragma unroll
+                for (int e = 0; e < kEach; ++e) x[i * kEach + e] = id[k] >= 0 ? a.scale * y[e] : 0.0f;
+            }
+        }
+        if (c >= 0 && c + E <= a.width) {
+            store_once(reinterpret_cast<uint4*>(out), pack(x, Out()));
+        } else {
+#pragma unroll
+            for (int e = 0; e < E; ++e)
+                if (c + e >= 0 && c + e < a.width) out[e] = from_float<Out>(x[e]);
+        }
+    }
+    if (bad && tile == 0 && lane == 0 && a.status) atomicOr(a.status, SR_STATUS_BAD_TARGET);
+}
+
 // ------------------------------------------------------------------------------------------------- sorting
 // A stable radix sort of (token, position) by one cluster: digits of up to 10 bits, two passes for vocabularies of up to a million.
 // A warp has consecutive tokens and counts them in a histogram of its own, so that ranks follow the order of the tokens;
@@ -126,17 +224,15 @@ __device__ __forceinline__ int2 load_l2(const int2* p) {
 }
 __device__ __forceinline__ uint32_t below(uint32_t peers) { return __popc(peers & ((1u << (threadIdx.x & 31)) - 1u)); }
 
-// Rows of the table that are zeroed while the tokens are sorted: a run of them, on a boundary of `vec` bytes each.
+// Rows of the table that are zeroed while the tokens are sorted: the first `rows`.
 struct ZeroRows {
     char* table;
     int64_t pitch;                  // bytes
-    int width, vec, rows;           // bytes of a row, of a store; rows from the first on
+    int width, rows;
+    bool wide;
 };
 constexpr int kZeroCtas = 112;      // with those that sort eight clusters: what the GPU's eight parts run at once
-template <typename W>
-__device__ __forceinline__ void zero_row(char* row, int width, int lane) {
-    for (int c = lane * (int)sizeof(W); c < width; c += 32 * (int)sizeof(W)) __stcs(reinterpret_cast<W*>(row + c), W());
-}
+
 // The CTA's share, without those that a token took; bits of them in shared memory.
 __device__ __forceinline__ void zero_share(const ZeroRows& z, const int32_t* tokens, int n, int share, uint32_t* taken, int most) {
     const int each = (z.rows - 1) / kZeroCtas + 1;
@@ -154,14 +250,11 @@ __device__ __forceinline__ void zero_share(const ZeroRows& z, const int32_t* tok
                 if (t[u] >= begin && t[u] < begin + rows) atomicOr(&taken[(t[u] - (int)begin) >> 5], 1u << ((t[u] - (int)begin) & 31));
         }
         __syncthreads();
-        const int lane = threadIdx.x & 31;
         for (int r = threadIdx.x >> 5; r < rows; r += blockDim.x >> 5) {
             if ((taken[r >> 5] >> (r & 31)) & 1u) continue;
             char* const row = z.table + (begin + r) * z.pitch;
-            if (z.vec == 16) zero_row<uint4>(row, z.width, lane);
-            else if (z.vec == 8) zero_row<uint2>(row, z.width, lane);
-            else if (z.vec == 4) zero_row<uint32_t>(row, z.width, lane);
-            else zero_row<unsigned short>(row, z.width, lane);
+            if (z.wide) zero_row<true>(row, z.width, threadIdx.x & 31, 32);
+            else zero_row<false>(row, z.width, threadIdx.x & 31, 32);
         }
     }
 }
@@ -373,7 +466,7 @@ __device__ __forceinline__ void write_row(const EmbedGradArgs& g, int token, int
 
 // Writes zeros to the rows [begin, end) that no token took.
 constexpr int kMostZeroRows = 1024;
-template <typename Table, int kCols>
+template <typename Table, bool kWide>
 __device__ __forceinline__ void zero_rows(const SumArgs& a, int begin, int end, int across) {
     __shared__ uint32_t s_taken[kMostZeroRows / 32];
     __shared__ int s_from;
@@ -398,13 +491,11 @@ __device__ __forceinline__ void zero_rows(const SumArgs& a, int begin, int end, 
         atomicOr(&s_taken[(token - begin) >> 5], 1u << ((token - begin) & 31));
     }
     __syncthreads();
-    Cols<Table, kCols> zero;
-    zero.zero();
-    for (int r = threadIdx.x / across; r < end - begin; r += kThreads / across) {
-        if ((s_taken[r >> 5] >> (r & 31)) & 1u) continue;
-        Table* const row = static_cast<Table*>(g.d_table) + (int64_t)(begin + r) * g.table_pitch;
-        for (int c = (threadIdx.x & (across - 1)) * kCols; c < g.width; c += across * kCols) zero.store(row + c);
-    }
+    if (!kWide) across = 32;                             // rows off 16 bytes: a warp each, whose edges cost no others their turn
+    for (int r = threadIdx.x / across; r < end - begin; r += kThreads / across)
+        if (!((s_taken[r >> 5] >> (r & 31)) & 1u))
+            zero_row<kWide>(reinterpret_cast<char*>(static_cast<Table*>(g.d_table) + (int64_t)(begin + r) * g.table_pitch), g.width * (int)sizeof(Table), threadIdx.x & (across - 1),
+                            across);
 }
 
 // The first `sum_ctas` CTAs sum pieces, the others write zeros, `zero_rows_each` rows each from row `zero_first` on.
@@ -415,7 +506,7 @@ embed_sums_kernel(const __grid_constant__ SumArgs a, int across, int tiles, int 
     const EmbedGradArgs& g = a.g;
     if ((int)blockIdx.x >= sum_ctas) {
         const int64_t begin = zero_first + (int64_t)((int)blockIdx.x - sum_ctas) * zero_rows_each;
-        zero_rows<Table, kCols>(a, (int)begin, (int)min((int64_t)g.vocab, begin + zero_rows_each), across);
+        zero_rows<Table, kCols * sizeof(Table) >= 16>(a, (int)begin, (int)min((int64_t)g.vocab, begin + zero_rows_each), across);
         return;
     }
     const int tile = blockIdx.x % tiles, piece = (blockIdx.x / tiles) * (kThreads / across) + threadIdx.x / across;
@@ -549,7 +640,15 @@ int embed_with(const EmbedArgs& a, cudaStream_t s) {
 template <typename Table, typename Out>
 int embed_types(const EmbedArgs& a, cudaStream_t s) {
     constexpr int kMost = 16 / (int)(sizeof(Table) > sizeof(Out) ? sizeof(Table) : sizeof(Out));
-    switch (cols_of(kMost, a.table, a.table_pitch, sizeof(Table), a.out, a.pitch, sizeof(Out), a.width)) {
+    const int cols = cols_of(kMost, a.table, a.table_pitch, sizeof(Table), a.out, a.pitch, sizeof(Out), a.width);
+    if (cols == 1 && a.width >= 64) {
+        const Spread sp = spread(a.width + 16 / (int)sizeof(Out) - 1, 16 / (int)sizeof(Out), 32);        // one vector more where a row begins inside its first
+        const int64_t ctas = (((int64_t)a.n_tokens - 1) / (kThreads / sp.across * kShiftRows) + 1) * sp.tiles;
+        if (ctas > INT32_MAX) return SR_ERR_BAD_SIZE;
+        SR_LAUNCH("embed_shift_kernel", (embed_shift_kernel<Table, Out>), (int)ctas, kThreads, 0, s, a, sp.across, sp.tiles);
+        return SR_OK;
+    }
+    switch (cols) {
         case 8: if constexpr (kMost == 8) return embed_with<Table, Out, 8>(a, s); else break;
         case 4: return embed_with<Table, Out, 4>(a, s);
         case 2: return embed_with<Table, Out, 2>(a, s);
@@ -607,7 +706,7 @@ int embed_grad_types(const EmbedGradArgs& g, void* ws, cudaStream_t s) {
         const size_t smem = (size_t)kSortWarps * sizeof(uint32_t) << bits;
         SR_CUDA_TRY(cudaFuncSetAttribute(sort_tokens_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)((size_t)kSortWarps * sizeof(uint32_t) << kMostBits)));
         SR_CUDA_TRY(cudaFuncSetAttribute(sort_tokens_kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
-        ZeroRows zero = {static_cast<char*>(g.d_table), g.table_pitch * (int64_t)sizeof(Table), g.width * (int)sizeof(Table), std::min(16, cols * (int)sizeof(Table)), 0};
+        ZeroRows zero = {static_cast<char*>(g.d_table), g.table_pitch * (int64_t)sizeof(Table), g.width * (int)sizeof(Table), 0, cols * sizeof(Table) >= 16};
         if (!g.accumulate) {                                             // what takes as long as sorting, less the time to look through the tokens; 4 MB a us
             const double bytes = (9.0 + g.n_tokens / 6000.0) * 4e6;
             zeroed = zero.rows = (int)std::min<double>(g.vocab, bytes / zero.width);

@@ -509,7 +509,7 @@ adjust_kernel(const __grid_constant__ AdjustArgs a, int runs, int rows_per_cta) 
                 copies_wait<3 * kStages - 3>();
             }
             const uint32_t left = word & allowed[0];     // tokens that change, one after the other
-            if (kBackward && !kShift && left != 0u && raw_ahead != 0u) copies_wait<2>();
+            if (kBackward && !kShift && raw_ahead != 0u) copies_wait<2>();       // used or not: the next row's go to the same place
 #pragma unroll 1
             for (uint32_t b = left; b != 0u; b &= b - 1u) {
                 const int bit = __ffs(b) - 1, v = bit / E * kThreads, l = head + (tid + v) * E + bit % E;
@@ -539,7 +539,7 @@ adjust_kernel(const __grid_constant__ AdjustArgs a, int runs, int rows_per_cta) 
                     const uint4* const p = reinterpret_cast<const uint4*>(raw + a.logits_pitch) + tid;
 #pragma unroll
                     for (int k = 0; k < kVecs; ++k) {
-                        if (bits_of_vector(word, k) == 0u) continue;
+                        if (bits_of_vector(word & (kDepth > 1 ? allowed[kDepth > 1] : kEvery), k) == 0u) continue;
                         copy_vector(&s_raw[k * kThreads + tid], p + k * kThreads);
                         raw_ahead |= kAll << (k * E);
                     }

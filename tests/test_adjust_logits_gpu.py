@@ -146,6 +146,31 @@ def test_rollouts_as_a_whole(dtype, V, T, which):
     check_backward(logits(T, V, dtype, 1), x, r, out)
 
 
+def test_gradient_of_many_rows_that_come_from_memory():
+    """Far more than L2 holds, masks that leave some rows nothing to change: copies ahead that a row has no use for must not reach the next
+    one's.  Every element is d, d / r or d r, by the sign of its own logit."""
+    T, V = 1024, 151936
+    g = torch.Generator(device=DEV).manual_seed(1)
+    x, d = (torch.randn(T, V, generator=g, device=DEV).to(torch.bfloat16) for _ in range(2))
+    history = (torch.exp(torch.rand(1200, generator=g, device=DEV) * np.log(V)) - 1).to(torch.int32)
+    start, length = torch.zeros(T, dtype=torch.int64, device=DEV), (torch.arange(T, device=DEV) // 2 + 400).to(torch.int32)
+    few = torch.rand(64, V, generator=g, device=DEV) < torch.where(torch.arange(64, device=DEV)[:, None] % 2 == 0, 0.01, 0.98)
+    mask_row = torch.randint(0, 64, (T,), generator=g, device=DEV, dtype=torch.int32)
+    dx, rep = torch.empty_like(d), torch.full((T,), 2.0, device=DEV)                 # 2: no rounding
+    rest = dict(history=history, history_start=start, history_len=length, repetition=rep, allowed=pack(few.cpu().numpy()).to(DEV), mask_row=mask_row)
+    for _ in range(3):
+        x, d = x.roll(1, 1), d.roll(3, 1)
+        sr.sr_adjust_logits_backward(d, x, **rest, d_logits=dx)
+        for a in range(0, T, 128):
+            r = slice(a, a + 128)
+            seen = torch.zeros(128, V, dtype=torch.bool, device=DEV)
+            for t in range(128):
+                seen[t, history[:int(length[a + t])].long()] = True
+            want = torch.where(seen, torch.where(x[r] > 0, d[r] * 0.5, d[r] * 2), d[r])
+            want = torch.where(few[mask_row[r].long()], want, torch.zeros_like(want))
+            assert torch.equal(dx[r], want), a
+
+
 def test_rows_that_do_not_go_on():
     """Next to one another: a history that shrinks, one that stays, another prompt, another bias list, an earlier start."""
     V, T = 600, 4096 * 4                                  # many more rows than CTAs: runs

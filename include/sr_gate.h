@@ -69,7 +69,7 @@ extern "C" {
 #define SR_STATUS_BAD_TARGET 8     /* a token >= vocab was treated as one that does not count */
 #define SR_STATUS_NONFINITE 16     /* the gradient norm is not finite; gradients were not scaled */
 #define SR_STATUS_TIMEOUT 32       /* a kernel gave up a wait: loss and stats are NaN, other outputs undefined */
-#define SR_STATUS_BAD_INDEX 64     /* a mask_row >= n_masks was treated as none */
+#define SR_STATUS_BAD_INDEX 64     /* a mask_row >= n_masks was treated as none, or a bias list was cut */
 
 int sr_version(void);
 const char* sr_strerror(int code);      /* static string */

@@ -41,14 +41,16 @@ extern "C" {
  *                      one: a rollout that is scored as a whole gives all of its rows its start, and
  *                      lengths that grow by one (such rows one after the other are fastest).  Positions outside
  *                      0 .. n_history and ids below 0 do not count, ids >= vocab do not either and
- *                      set SR_STATUS_BAD_TARGET; a length below 0 is one of 0 and sets SR_STATUS_NEG_LEN
+ *                      set SR_STATUS_BAD_TARGET; a length below 0 is one of 0 and sets SR_STATUS_NEG_LEN; of a history
+ *                      of 2^30 positions and more the first 2^30 - 1 count
  *   prompt_len     in  [n_rows] int32, how much of a history is prompt, or NULL: nothing (below 0 is 0)
  *   repetition, presence, frequency   in  [n_rows] fp32, each may be NULL: that penalty is left out.
- *                      All NULL: no histories are read and their arrays may be NULL
+ *                      repetition is > 0 and a normal number (16-bit logits are multiplied by its reciprocal).  All NULL: no histories are read and their arrays may be NULL
  *   bias_token     in  [n_bias] int32 and bias_value [n_bias] fp32: tokens with their biases.  Where a token stands in a
  *                      row's list more than once, the last one counts.  Ids below 0 or >= vocab as above
  *   bias_start     in  [n_rows] int64 and bias_len [n_rows] int32: row t's list is entries
- *                      bias_start[t] .. + bias_len[t], of 0 .. n_bias; rows may share one.
+ *                      bias_start[t] .. + bias_len[t], of 0 .. n_bias; rows may share one.  Of a list of more than 65535
+ *                      entries the first 65535 count, and SR_STATUS_BAD_INDEX is set; a length below 0 as above.
  *                      bias_value NULL: no biases, the other three are not used
  *   allowed        in  [n_masks][mask_pitch] words of 32 bits: token v is allowed where bit v % 32 of word
  *                      v / 32 is set.  NULL: no masks.  mask_pitch >= ceil(vocab / 32)

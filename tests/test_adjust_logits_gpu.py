@@ -169,6 +169,14 @@ def test_gradient_of_many_rows_that_come_from_memory():
             want = torch.where(seen, torch.where(x[r] > 0, d[r] * 0.5, d[r] * 2), d[r])
             want = torch.where(few[mask_row[r].long()], want, torch.zeros_like(want))
             assert torch.equal(dx[r], want), a
+    sr.sr_adjust_logits(x, **rest, out=dx)                                           # and the rows themselves
+    for a in range(0, T, 128):
+        r = slice(a, a + 128)
+        seen = torch.zeros(128, V, dtype=torch.bool, device=DEV)
+        for t in range(128):
+            seen[t, history[:int(length[a + t])].long()] = True
+        want = torch.where(seen, torch.where(x[r] > 0, x[r] * 0.5, x[r] * 2), x[r])
+        assert torch.equal(dx[r], torch.where(few[mask_row[r].long()], want, torch.full_like(want, -float("inf")))), a
 
 
 def test_rows_that_do_not_go_on():
@@ -263,6 +271,59 @@ def test_a_bias_twice_and_lists_that_reach_out():
          "bias_len": np.array([5, 7, 2 ** 31 - 1], np.int32)}
     check(x, {**r, "bias_len": np.minimum(r["bias_len"], 50)}, torch.empty_like(x))
     sr.sr_adjust_logits(x, **on_device(r), out=torch.empty_like(x))
+
+
+@pytest.mark.parametrize("which", ["rpfbm", "rm"])
+def test_a_list_of_its_own_for_hundreds_of_rows(which):
+    """Rows that all begin anew, several to a CTA: tables emptied and filled again, ids copied ahead."""
+    T, V = 900, 20000
+    x = logits(T, V, "bf16", 9)
+    r = rules(T, V, 9, which, most=70)
+    out = torch.empty_like(x)
+    check(x, r, out)
+    check_backward(logits(T, V, "bf16", 10), x, r, out)
+
+
+def test_lists_longer_than_what_is_copied_ahead():
+    T, V = 700, 9000
+    rng = np.random.default_rng(4)
+    n = 3000
+    r = {"hist": rng.integers(0, V, n).astype(np.int32), "start": rng.integers(0, 900, T).astype(np.int64), "length": rng.integers(900, 2100, T).astype(np.int32),
+         "prompt": rng.integers(0, 2100, T).astype(np.int32), "rep": np.full(T, 1.5, np.float32), "freq": np.full(T, 0.125, np.float32), "bias_token": rng.integers(0, V, n).astype(np.int32),
+         "bias_value": rng.normal(size=n).astype(np.float32), "bias_start": rng.integers(0, 900, T).astype(np.int64), "bias_len": rng.integers(200, 2100, T).astype(np.int32)}
+    x = logits(T, V, "f32", 2)
+    check(x, r, torch.empty_like(x))
+
+
+def test_a_bias_list_that_is_cut():
+    V = 70000
+    x = logits(1, V, "f32", 2)
+    r = {"bias_token": np.arange(V, dtype=np.int32), "bias_value": np.ones(V, np.float32), "bias_start": np.zeros(1, np.int64)}
+    out, st = torch.empty_like(x), torch.zeros(1, dtype=torch.int32, device=DEV)
+    sr.sr_adjust_logits(x, **on_device({**r, "bias_len": np.array([V], np.int32)}), out=out, status=st)
+    assert int(st) == sr.SR_STATUS_BAD_INDEX
+    want, bound = adjust(x, **{**r, "bias_len": np.array([65535], np.int32)})
+    assert_near(out.cpu(), want, bound, "cut")
+
+
+def test_more_frequent_tokens_than_the_table_holds():
+    """Each of 80 tokens of one slice 8500 times: beyond the 14 bits of a count, and more of them than have a counter of their own."""
+    V, n, each = 9000, 80, 8500
+    hist = np.repeat(np.arange(n, dtype=np.int32), each)
+    r = {"hist": hist, "start": np.zeros(2, np.int64), "length": np.array([n * each, n * each - 3], np.int32), "prompt": np.array([5, 5], np.int32), "freq": np.full(2, 2.0 ** -12, np.float32)}
+    x = logits(2, V, "f32", 1)
+    check(x, r, torch.empty_like(x))
+
+
+@pytest.mark.parametrize("step", [1, 2])
+def test_a_token_that_becomes_frequent(step):
+    """Its count leaves 14 bits between two rows of one rollout, added by one thread or by all."""
+    T, V = 40, 500
+    hist = np.full(9000, 123, np.int32)
+    r = {"hist": hist, "start": np.zeros(T, np.int64), "length": (8170 + step * np.arange(T)).astype(np.int32), "freq": np.full(T, 0.25, np.float32), "pres": np.ones(T, np.float32)}
+    big = {k: np.concatenate([v] * 40) if k != "hist" else v for k, v in r.items()}              # many rows to a CTA
+    x = logits(40 * T, V, "f32", 1)
+    check(x, big, torch.empty_like(x))
 
 
 def test_no_rows_and_empty_lists():

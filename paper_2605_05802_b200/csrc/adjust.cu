@@ -1,12 +1,19 @@
 // Logits adjusted by penalties for tokens seen before, biases and masks of allowed tokens, and their gradient (sr_tokens.h).
 //
 // A CTA has a slice of the vocabulary (16 KB of a row) and a run of rows.  Every thread owns the same four vectors of 16 bytes in each row, and with
-// them their tokens: a bit of a register says which of them a history or a bias touches, shared memory how often each was seen and
+// them their tokens: the bits of a register say which of them a history or a bias touches, shared memory how often each was seen and
 // which entry of the bias list is its own.  Histories are read whole by every CTA of their rows, which costs 4 bytes a token from L2 and
-// no hashing, sorting or limit of their length; where a row goes on where the one before it ended (a rollout scored as a whole), the
-// owner of the new token notes it, and the CTA's threads go from row to row without a barrier.  Vectors pass through registers once, the
-// next row's on their way meanwhile; those of which no token is allowed are not read.  Counts are whole numbers and a token's bias is the
-// largest index in the list, so no order of atomics enters a result.
+// no hashing, sorting or limit of their length.  Where a row goes on where the one before it ended (a rollout scored as a whole), the
+// owner of the new token notes it, and the CTA's threads go from row to row without a barrier; where a row begins anew, its ids have been
+// copied to shared memory while the row before was written.  Vectors go through a ring of rows in shared memory, copied ahead by the thread that
+// changes and writes them; those of which no token is allowed are not read.  Counts are whole numbers and a token's bias is the largest
+// index in the list, so no order of atomics enters a result.
+//
+// Rollouts as a whole are bound by HBM: 4096 rows of 151936 bf16 in 412 us, 6.0 TB/s of logits read and written; the gradient of 2048 with masks,
+// half of which allow a handful, in 180 us (their banned vectors are not read: what is left runs at 5.2 TB/s).  Rows with histories of their own are
+// bound by latency and issue: 512 of them 71 us with penalties, 139 with 300 biases each and masks too (floor 48), of 600 to 900
+// instructions a warp and row, a copy's 220 among them.  Before: tables looked up for every vector (4096 rows 618 us), rows in registers (446; their
+// code outgrew the instruction cache with every change unrolled), 512 threads (429), slices of twice the size (580).
 #include <algorithm>
 
 #include "tokens.cuh"
@@ -98,11 +105,7 @@ __device__ __noinline__ uint32_t times_frequent(const uint32_t* table, uint32_t 
     return times;
 }
 
-// kSparse: out is in, and only vectors that change are read and written.
-// kShift: not all rows of in and out begin on 16 bytes.  The touched tokens are then bits of shared memory, which all threads read, and a
-// barrier stands before and behind each change of them.
-// Where things lie in dynamic shared memory (bytes).
-// kStages: rows of the ring, one of which is changed and written while the others are on their way.
+// Where things lie in dynamic shared memory (bytes).  kStages: rows of the ring, one of which is changed and written while the others are on their way.
 template <typename T, int kStages, bool kBackward>
 struct Layout {
     static constexpr int kSlice = kSliceOf<T>, kRow = kVecs * kThreads * 16;
@@ -111,6 +114,9 @@ struct Layout {
     static constexpr int bytes(bool counts, bool biases) { return kBackward ? kCount : biases ? kAll : counts ? kEntry : kCount; }
 };
 
+// kSparse: out is in, and only vectors that change are read and written.
+// kShift: not all rows of in and out begin on 16 bytes.  The touched tokens are then bits of shared memory, which all threads read, and a
+// barrier stands before and behind each change of them (4096 rows of 151935 bf16: 622 us).
 template <typename T, int kStages, bool kBackward, bool kSparse, bool kShift>
 __global__ void __launch_bounds__(kThreads, kStages == 3 ? 3 : 4)
 adjust_kernel(const __grid_constant__ AdjustArgs a, int runs, int rows_per_cta) {

@@ -11,7 +11,8 @@ shrink), adv (advantages, 4M groups), orr (OR rule, 4M groups), bstats (batch
 statistics, 4M groups), keep (kept-group index list, 4M groups), sig (Appendix-B
 signals, 65536 groups x N=16), packed (token level from packed host input, 256 groups),
 train (the trainer's operators: bf16 logits of --tokens x 151936, losses of 8192
-rollouts, 300M bf16 gradients in 128 tensors).
+rollouts, 300M bf16 gradients in 128 tensors), tokens (the operators on token ids: bf16
+logits of --tokens x 151936 with histories of 900 ids, and 64 x --tokens tokens embedded in 2048 columns).
 """
 from __future__ import annotations
 
@@ -170,6 +171,35 @@ def main():
                                                            loss=loss, d_logp=d_lps, workspace=ws),
                "sr_grad_norm": lambda: sr.sr_grad_norm(grads, norm=norm, workspace=ws),
                "sr_clip_grads": lambda: sr.sr_clip_grads(grads, norm, 1.0)}
+        for name, fn in ops.items():
+            times.clear()
+            for _ in range(args.reps):
+                timed(fn)
+            print(f"{name}: median {statistics.median(times):.1f} us")
+    elif args.case == "tokens":
+        T, V, D, most = args.tokens, 151936, 2048, 900
+        x = torch.randn(T, V, device=dev).mul_(2.0).to(torch.bfloat16)
+        y, dx = torch.empty_like(x), torch.empty_like(x)
+        text = lambda n: (torch.exp(torch.rand(n, device=dev, dtype=torch.float64) * 11.93) - 1).to(torch.int32).clamp_(0, V - 1)
+        f32 = lambda v: torch.full((T,), v, dtype=torch.float32, device=dev)
+        allowed = torch.randint(-2 ** 31, 2 ** 31 - 1, (64, V // 32), dtype=torch.int32, device=dev)
+        masks = dict(allowed=allowed, mask_row=torch.randint(0, 64, (T,), dtype=torch.int32, device=dev))
+        own = dict(history=text(T * most), history_start=most * torch.arange(T, device=dev), history_len=torch.full((T,), most, dtype=torch.int32, device=dev))
+        whole = dict(history=text(T + most), history_start=torch.zeros(T, dtype=torch.int64, device=dev),
+                     history_len=torch.arange(most, T + most, dtype=torch.int32, device=dev))
+        penalties = dict(repetition=f32(1.1), presence=f32(0.5), frequency=f32(0.1))
+        n = 64 * T
+        ids, table = text(n), torch.randn(V, D, device=dev).to(torch.bfloat16)
+        e, d_table = torch.empty(n, D, dtype=torch.bfloat16, device=dev), torch.empty_like(table)
+        ws = torch.empty(sr.sr_embed_tokens_backward_workspace_bytes(n, V, D), dtype=torch.uint8, device=dev)
+        ops = {"sr_adjust_logits, rows of their own": lambda: sr.sr_adjust_logits(x, **own, **penalties, **masks, out=y),
+               "sr_adjust_logits, one rollout": lambda: sr.sr_adjust_logits(x, **whole, **penalties, **masks, out=y),
+               "sr_adjust_logits_backward": lambda: sr.sr_adjust_logits_backward(y, x, **whole, repetition=penalties["repetition"], **masks,
+                                                                                 d_logits=dx),
+               "sr_embed_tokens": lambda: sr.sr_embed_tokens(table, ids, D ** 0.5, out=e),
+               "sr_embed_tokens_backward": lambda: sr.sr_embed_tokens_backward(e, ids, D ** 0.5, d_table=d_table, workspace=ws),
+               "sr_embed_tokens_backward, added": lambda: sr.sr_embed_tokens_backward(e, ids, 1e-3, d_table=d_table, accumulate=True,
+                                                                                      workspace=ws)}
         for name, fn in ops.items():
             times.clear()
             for _ in range(args.reps):

@@ -54,14 +54,15 @@ struct Cols {
 
 constexpr int kThreads = 256;
 
-// Zeros to a row of `bytes`, by lanes 0 .. across - 1.  kWide: all rows are whole vectors of 16 bytes.  Otherwise they are vectors wherever
+// Zeros to a row of `bytes`, by a warp.  kWide: all rows are whole vectors of 16 bytes.  Otherwise they are vectors wherever
 // the row begins, and two bytes at a time before and behind.
 template <bool kWide>
-__device__ __forceinline__ void zero_row(char* row, int bytes, int lane, int across) {
+__device__ __forceinline__ void zero_row(char* row, int bytes, int lane) {
     const int head = kWide ? 0 : min(bytes, (int)(-reinterpret_cast<intptr_t>(row) & 15)), body = kWide ? bytes : (bytes - head) & ~15;
-    for (int c = lane * 16; c < body; c += across * 16) __stcs(reinterpret_cast<uint4*>(row + head + c), make_uint4(0u, 0u, 0u, 0u));
+#pragma unroll 4
+    for (int c = lane * 16; c < body; c += 512) __stcs(reinterpret_cast<uint4*>(row + head + c), make_uint4(0u, 0u, 0u, 0u));
     if (!kWide)
-        for (int c = lane * 2; c < bytes - body; c += across * 2) *reinterpret_cast<uint16_t*>(row + (c < head ? c : c + body)) = 0;
+        for (int c = lane * 2; c < bytes - body; c += 64) *reinterpret_cast<uint16_t*>(row + (c < head ? c : c + body)) = 0;
 }
 
 // How threads are spread over rows of `width` elements: `across` of them (a power of two) next to one another.
@@ -257,8 +258,8 @@ __device__ __forceinline__ void zero_share(const ZeroRows& z, const int32_t* tok
         for (int r = threadIdx.x >> 5; r < rows; r += blockDim.x >> 5) {
             if ((taken[r >> 5] >> (r & 31)) & 1u) continue;
             char* const row = z.table + (begin + r) * z.pitch;
-            if (z.wide) zero_row<true>(row, z.width, threadIdx.x & 31, 32);
-            else zero_row<false>(row, z.width, threadIdx.x & 31, 32);
+            if (z.wide) zero_row<true>(row, z.width, threadIdx.x & 31);
+            else zero_row<false>(row, z.width, threadIdx.x & 31);
         }
     }
 }
@@ -471,7 +472,7 @@ __device__ __forceinline__ void write_row(const EmbedGradArgs& g, int token, int
 // Writes zeros to the rows [begin, end) that no token took.
 constexpr int kMostZeroRows = 1024;
 template <typename Table, bool kWide>
-__device__ __forceinline__ void zero_rows(const SumArgs& a, int begin, int end, int across) {
+__device__ __forceinline__ void zero_rows(const SumArgs& a, int begin, int end) {
     __shared__ uint32_t s_taken[kMostZeroRows / 32];
     __shared__ int s_from;
     const EmbedGradArgs& g = a.g;
@@ -495,11 +496,9 @@ __device__ __forceinline__ void zero_rows(const SumArgs& a, int begin, int end, 
         atomicOr(&s_taken[(token - begin) >> 5], 1u << ((token - begin) & 31));
     }
     __syncthreads();
-    if (!kWide) across = 32;                             // rows off 16 bytes: a warp each, whose edges cost no others their turn
-    for (int r = threadIdx.x / across; r < end - begin; r += kThreads / across)
+    for (int r = threadIdx.x >> 5; r < end - begin; r += kThreads / 32)       // a warp to a row
         if (!((s_taken[r >> 5] >> (r & 31)) & 1u))
-            zero_row<kWide>(reinterpret_cast<char*>(static_cast<Table*>(g.d_table) + (int64_t)(begin + r) * g.table_pitch), g.width * (int)sizeof(Table), threadIdx.x & (across - 1),
-                            across);
+            zero_row<kWide>(reinterpret_cast<char*>(static_cast<Table*>(g.d_table) + (int64_t)(begin + r) * g.table_pitch), g.width * (int)sizeof(Table), threadIdx.x & 31);
 }
 
 // The first `sum_ctas` CTAs sum pieces, the others write zeros, `zero_rows_each` rows each from row `zero_first` on.
@@ -510,7 +509,7 @@ embed_sums_kernel(const __grid_constant__ SumArgs a, int across, int tiles, int 
     const EmbedGradArgs& g = a.g;
     if ((int)blockIdx.x >= sum_ctas) {
         const int64_t begin = zero_first + (int64_t)((int)blockIdx.x - sum_ctas) * zero_rows_each;
-        zero_rows<Table, kCols * sizeof(Table) >= 16>(a, (int)begin, (int)min((int64_t)g.vocab, begin + zero_rows_each), across);
+        zero_rows<Table, kCols * sizeof(Table) >= 16>(a, (int)begin, (int)min((int64_t)g.vocab, begin + zero_rows_each));
         return;
     }
     const int tile = blockIdx.x % tiles, piece = (blockIdx.x / tiles) * (kThreads / across) + threadIdx.x / across;

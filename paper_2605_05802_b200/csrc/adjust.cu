@@ -95,14 +95,14 @@ __device__ __noinline__ void count_frequent(uint32_t* table, int l) {
         return;
     }
 }
-__device__ __noinline__ uint32_t times_frequent(const uint32_t* table, uint32_t times, int l, int id, const int32_t* history, int64_t n_history, const Record& r) {
+__device__ __noinline__ uint32_t times_frequent(const uint32_t* table, uint32_t times, int l, int id, const int32_t* history, int64_t n_history, const Record& r, uint32_t more) {
     for (int i = 0; i < kFrequent; ++i)
         if (table[(l + i) % kFrequent] == (uint32_t)l + 1u) return times + table[kFrequent + (l + i) % kFrequent];
     int64_t from;                   // more of them than the table holds
     const int skip = min(r.prompt, r.len), n = inside(r.start + skip, r.len - skip, n_history, from);
     times = 0;
     for (int k = 0; k < n; ++k) times += history[from + k] == id;
-    return times;
+    return times - more;            // those that the caller adds
 }
 
 // Where things lie in dynamic shared memory (bytes).  kStages: rows of the ring, one of which is changed and written while the others are on their way.
@@ -115,8 +115,8 @@ struct Layout {
 };
 
 // kSparse: out is in, and only vectors that change are read and written.
-// kShift: not all rows of in and out begin on 16 bytes.  The touched tokens are then bits of shared memory, which all threads read, and a
-// barrier stands before and behind each change of them (4096 rows of 151935 bf16: 622 us).
+// kShift: not all rows of in and out begin on 16 bytes.  The touched tokens are then bits of shared memory, which all threads read; the new tokens of
+// a batch's rows are looked up in their records until a barrier lets them into the tables.
 template <typename T, int kStages, bool kBackward, bool kSparse, bool kShift>
 __global__ void __launch_bounds__(kThreads, kStages == 3 ? 3 : 4)
 adjust_kernel(const __grid_constant__ AdjustArgs a, int runs, int rows_per_cta) {
@@ -244,12 +244,35 @@ adjust_kernel(const __grid_constant__ AdjustArgs a, int runs, int rows_per_cta) 
         copies_end();
     }
     uint32_t raw_ahead = 0u;                             // touched vectors whose logits are on their way
+    const auto flag = [&](int l, uint32_t bit) { atomicOr(reinterpret_cast<uint32_t*>(count) + (l >> 1), bit << ((l & 1) * 16)); };
+    const auto add_one = [&](int l) {
+        if ((count[l] & kTimes) < kMany) {
+            atomicAdd(reinterpret_cast<uint32_t*>(count) + (l >> 1), 1u << ((l & 1) * 16));
+            return;
+        }
+        frequent = true;
+        count_frequent(s_frequent, l);
+    };
+    // kShift: records from here to the row's own have new tokens that are not in the tables yet
+    int waiting = kBatch;
+    const auto note = [&](const Record& r) {             // one of them, by one thread
+        if (r.id < first || r.id - first >= n) return;
+        const int l = r.id - first;
+        if (!kBackward) {
+            if (r.from < r.prompt) flag(l, kInPrompt);
+            else add_one(l);
+        }
+        atomicOr(&s_touched[half][l >> 5], 1u << (l & 31));
+    };
 #pragma unroll 1
     for (int row = (int)row0 - (kDepth - 1); row < row_end; ++row) {
         int mask_ahead = -1;
         if (row >= row0) {
             if (at == kBatch) {                          // records of the rows from here on, by the first warp
                 if (row > row0) __syncthreads();
+                if (kShift && row > row0 && tid >= waiting && tid < kBatch) note(s_record[tid]);
+                if (kShift) __syncwarp();
+                waiting = 0;
                 if (tid < 32) {
                     Record r = {};
                     const int64_t mine = (int64_t)row + tid;
@@ -310,21 +333,14 @@ adjust_kernel(const __grid_constant__ AdjustArgs a, int runs, int rows_per_cta) 
             mask_ahead = r.mask_ahead;
 
             // the tables of this row
-            const auto flag = [&](int l, uint32_t bit) { atomicOr(reinterpret_cast<uint32_t*>(count) + (l >> 1), bit << ((l & 1) * 16)); };
-            const auto add_one = [&](int l) {
-                if ((count[l] & kTimes) < kMany) {
-                    atomicAdd(reinterpret_cast<uint32_t*>(count) + (l >> 1), 1u << ((l & 1) * 16));
-                    return;
-                }
-                frequent = true;
-                count_frequent(s_frequent, l);
-            };
-            if (r.from < 0 || r.len > r.from + 1 || (kShift && r.len > r.from)) {
+            if (r.from < 0 || r.len > r.from + 1) {
                 if (kShift && row > row0) __syncthreads();           // the row before is done with them
                 if (r.from < 0) half ^= 1;
                 if (row > row0) {
                     if (r.from >= 0) {
-                        if (!kShift) {                   // more than one new token: the owners' bits meet theirs
+                        if (kShift) {
+                            if (tid >= waiting && tid < at - 1) note(s_record[tid]);
+                        } else {                         // more than one new token: the owners' bits meet theirs
                             s_touched[half][tid] = word;
                             if (odd) atomicOr(&s_touched[half][kWords - 1], 1u << tid);
                         }
@@ -414,6 +430,7 @@ adjust_kernel(const __grid_constant__ AdjustArgs a, int runs, int rows_per_cta) 
                     }
                 }
                 __syncthreads();
+                waiting = at;
                 if (!kShift) {
                     word = s_touched[half][tid];
                     odd = tid < E && ((s_touched[half][kWords - 1] >> tid) & 1u);
@@ -442,6 +459,10 @@ adjust_kernel(const __grid_constant__ AdjustArgs a, int runs, int rows_per_cta) 
                 for (int k = 0; k < kVecs; ++k) {
                     const int j = tid + k * kThreads;
                     if (j < vecs) word |= (bits_at(s_touched[half], head + j * E, E) & kAll) << (k * E);
+                }
+                for (int i = waiting; i < at; ++i) {
+                    const int id = s_record[i].id, v = id - first - head;
+                    if (id >= first && id - first < n && v >= 0 && v < vecs * E && v / E % kThreads == tid) word |= 1u << (v / E / kThreads * E + v % E);
                 }
             }
 
@@ -478,10 +499,16 @@ adjust_kernel(const __grid_constant__ AdjustArgs a, int runs, int rows_per_cta) 
                 const float repetition = r.repetition;
                 const auto repeated = [&](bool larger) { return sizeof(T) == 4 ? (larger ? v / repetition : v * repetition) : v * (larger ? r.shrink : repetition); };
                 if (kBackward) return repeated(positive);
-                const uint32_t c = count[l];
-                uint32_t times = c & kTimes;
+                uint32_t c = count[l], times = c & kTimes, more = 0u;
+                for (int i = waiting; kShift && i < at; ++i) {
+                    if (s_record[i].id != first + l) continue;
+                    if (s_record[i].from < s_record[i].prompt) c |= kInPrompt;
+                    else ++more;
+                }
+                c |= more;                               // whether it was seen at all
                 if (c & ~kBiased) v = repeated(v > 0.0f);
-                if (times >= kMany) times = times_frequent(s_frequent, times, l, first + l, a.history, a.n_history, r);
+                if (times >= kMany) times = times_frequent(s_frequent, times, l, first + l, a.history, a.n_history, r, more);
+                times += more;
                 const float less = fmaf(-r.frequency, (float)times, v) - r.presence;
                 v = times ? less : v;
                 if (c & kBiased) {
@@ -490,12 +517,17 @@ adjust_kernel(const __grid_constant__ AdjustArgs a, int runs, int rows_per_cta) 
                 }
                 return v;
             };
+            const auto touched_at = [&](int l) {
+                bool is = (s_touched[half][l >> 5] >> (l & 31)) & 1u;
+                for (int i = waiting; i < at; ++i) is |= s_record[i].id == first + l;
+                return is;
+            };
             // elements in no vector
 #pragma unroll 1
             for (int i = tid; (kShift || vecs != kFull) && i < n - vecs * E; i += kThreads) {
                 const int l = i < head ? i : i + vecs * E;
                 if (r.mask >= 0 && !((mask_at(r.mask)[l >> 5] >> (l & 31)) & 1u)) out[l] = banned_value<T>(kBackward);
-                else if (kShift ? (s_touched[half][l >> 5] >> (l & 31)) & 1u : odd) out[l] = from_float<T>(changed(l, to_float(in[l]), kBackward && to_float(raw[l]) > 0.0f));
+                else if (kShift ? touched_at(l) : odd) out[l] = from_float<T>(changed(l, to_float(in[l]), kBackward && to_float(raw[l]) > 0.0f));
                 else if (!kSparse) out[l] = in[l];
             }
             uint4* const mine = ring + take * kFull;     // the thread's vectors

@@ -135,7 +135,7 @@ def test_in_place_is_the_same(dtype, V, which):
         assert torch.equal(got.nan_to_num(nan=1e4), apart.nan_to_num(nan=1e4)) and torch.equal(got.isnan(), apart.isnan())
 
 
-@pytest.mark.parametrize("dtype,V,T", [("bf16", 8200, 700), ("f32", 700, 4000), ("f16", 30001, 300)])
+@pytest.mark.parametrize("dtype,V,T", [("bf16", 8200, 700), ("f32", 700, 4000), ("f16", 30001, 300), ("bf16", 8203, 700), ("f32", 701, 4000)])
 @pytest.mark.parametrize("which", ["rpf", "rpfbm"])
 def test_rollouts_as_a_whole(dtype, V, T, which):
     """Many rows of a few histories that grow row by row: runs of rows in one CTA, one rollout after the other."""
@@ -187,8 +187,9 @@ def test_rows_that_do_not_go_on():
     r = {"hist": hist, "start": rng.integers(0, 2, T).astype(np.int64), "length": rng.integers(0, 4, T).astype(np.int32) * 9, "prompt": rng.integers(0, 2, T).astype(np.int32) * 5,
          "rep": np.full(T, 1.5, np.float32), "freq": np.full(T, 0.25, np.float32), "pres": np.full(T, 0.5, np.float32), "bias_token": rng.integers(0, V, 20).astype(np.int32),
          "bias_value": rng.normal(size=20).astype(np.float32), "bias_start": rng.integers(0, 2, T).astype(np.int64), "bias_len": rng.integers(0, 3, T).astype(np.int32) * 8}
-    x = logits(T, V, "bf16", 2)
-    check(x, r, torch.empty_like(x))
+    for pad in (0, 3):
+        x = logits(T, V, "bf16", 2, pad)
+        check(x, r, torch.empty(T, V + pad, dtype=x.dtype, device=DEV)[:, :V])
 
 
 @pytest.mark.parametrize("shift_in,shift_out", [(0, 1), (3, 0), (1, 1), (5, 2)])
@@ -322,8 +323,9 @@ def test_a_token_that_becomes_frequent(step):
     hist = np.full(9000, 123, np.int32)
     r = {"hist": hist, "start": np.zeros(T, np.int64), "length": (8170 + step * np.arange(T)).astype(np.int32), "freq": np.full(T, 0.25, np.float32), "pres": np.ones(T, np.float32)}
     big = {k: np.concatenate([v] * 40) if k != "hist" else v for k, v in r.items()}              # many rows to a CTA
-    x = logits(40 * T, V, "f32", 1)
-    check(x, big, torch.empty_like(x))
+    for pad in (0, 1):                                    # rows on 16 bytes, and off them
+        x = logits(40 * T, V, "f32", 1, pad)
+        check(x, big, torch.empty(40 * T, V + pad, device=DEV)[:, :V])
 
 
 def test_no_rows_and_empty_lists():

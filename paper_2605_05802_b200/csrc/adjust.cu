@@ -206,10 +206,15 @@ adjust_kernel(const __grid_constant__ AdjustArgs a, int runs, int rows_per_cta) 
     // and changes and writes its own.  The first turns are those of no row.
     constexpr int kDepth = kStages;
     uint32_t allowed[kDepth];                            // of the thread's vectors, from this row on
+    constexpr int kEdges = 16;                           // more than there are elements before and behind the vectors of a row, if it has any
+    T edge[kDepth];                                      // kShift: that of the thread, copied ahead like the vectors
     int head_ahead = 0, vecs_ahead = vecs;               // of the row that is looked up; the same for all but in kShift
     if (kShift) split(in, out, head_ahead, vecs_ahead);
 #pragma unroll
-    for (int d = 0; d < kDepth; ++d) allowed[d] = kEvery;
+    for (int d = 0; d < kDepth; ++d) {
+        allowed[d] = kEvery;
+        edge[d] = from_float<T>(0.0f);
+    }
     {
         const int m = mask_of(row0);
         if (a.allowed) allowed[kDepth - 1] = bits_of(words_of(m, head_ahead, vecs_ahead), m, head_ahead);
@@ -480,6 +485,8 @@ adjust_kernel(const __grid_constant__ AdjustArgs a, int runs, int rows_per_cta) 
 #pragma unroll
                 for (int k = 0; k < kVecs; ++k)
                     if (tid + k * kThreads < vecs_ahead && bits_of_vector(allowed[kDepth - 1], k) != 0u) copy_vector(to + k * kThreads, p + k * kThreads);
+                const int edges = n - vecs_ahead * E;
+                if (kShift && edges <= kEdges && tid < edges) edge[kDepth - 1] = in_ahead[tid < head_ahead ? tid : tid + vecs_ahead * E];
                 in_ahead += a.pitch;
                 fill = fill == kStages - 1 ? 0 : fill + 1;
             }
@@ -526,9 +533,10 @@ adjust_kernel(const __grid_constant__ AdjustArgs a, int runs, int rows_per_cta) 
 #pragma unroll 1
             for (int i = tid; (kShift || vecs != kFull) && i < n - vecs * E; i += kThreads) {
                 const int l = i < head ? i : i + vecs * E;
+                const T v = kShift && !kSparse && n - vecs * E <= kEdges ? edge[0] : in[l];
                 if (r.mask >= 0 && !((mask_at(r.mask)[l >> 5] >> (l & 31)) & 1u)) out[l] = banned_value<T>(kBackward);
-                else if (kShift ? touched_at(l) : odd) out[l] = from_float<T>(changed(l, to_float(in[l]), kBackward && to_float(raw[l]) > 0.0f));
-                else if (!kSparse) out[l] = in[l];
+                else if (kShift ? touched_at(l) : odd) out[l] = from_float<T>(changed(l, to_float(v), kBackward && to_float(raw[l]) > 0.0f));
+                else if (!kSparse) out[l] = v;
             }
             uint4* const mine = ring + take * kFull;     // the thread's vectors
             take = take == kStages - 1 ? 0 : take + 1;
@@ -589,7 +597,10 @@ adjust_kernel(const __grid_constant__ AdjustArgs a, int runs, int rows_per_cta) 
         }
         if (kBackward) copies_end();
 #pragma unroll
-        for (int d = 0; d + 1 < kDepth; ++d) allowed[d] = allowed[d + 1];
+        for (int d = 0; d + 1 < kDepth; ++d) {
+            allowed[d] = allowed[d + 1];
+            if (kShift) edge[d] = edge[d + 1];
+        }
         if (a.allowed) allowed[kDepth - 1] = bits_of(words, mask_ahead, head_ahead);
     }
     if (a.status && flags) atomicOr(a.status, flags);

@@ -1,4 +1,8 @@
 """Refusals of the operators on token ids, on the host: no call here gets as far as a launch."""
+import os
+import shutil
+import subprocess
+
 import pytest
 import torch
 
@@ -112,6 +116,13 @@ def test_binding_refuses_what_the_library_cannot_see(lib):
         sr.sr_adjust_logits(x.double(), out=x)
     with pytest.raises(TypeError):
         sr.sr_embed_tokens([1.0], i, out=x)
+
+
+def test_the_header_is_plain_c(tmp_path):
+    cc, inc = shutil.which("gcc") or shutil.which("cc"), os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "include")
+    src = tmp_path / "tokens.c"
+    src.write_text('#include "sr_tokens.h"\nint main(void) { return (int)sr_embed_tokens_backward_workspace_bytes(1, 1, 1) + SR_STATUS_BAD_INDEX + SR_DTYPE_F16; }\n')
+    subprocess.run([cc, "-std=c11", "-Wall", "-Wextra", "-Werror", "-pedantic", "-I", inc, "-fsyntax-only", str(src)], check=True)
 
 
 @pytest.mark.gpu

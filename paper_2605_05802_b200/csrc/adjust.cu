@@ -11,7 +11,7 @@
 //
 // Rollouts as a whole are bound by HBM: 4096 rows of 151936 bf16 in 412 us, 6.0 TB/s of logits read and written; the gradient of 2048 with masks,
 // half of which allow a handful, in 180 us (their banned vectors are not read: what is left runs at 5.2 TB/s).  Rows with histories of their own are
-// bound by latency and issue: 512 of them 71 us with penalties, 140 with 300 biases each and masks too (floor 48), of 600 to 900
+// bound by latency and issue: 512 of them 70 us with penalties, 132 with 300 biases each and masks too (floor 48), of 600 to 900
 // instructions a warp and row, a copy's 220 among them; two changed tokens side by side make no difference.  Before: tables looked up for every vector (4096 rows 618 us), rows in registers (446; their
 // code outgrew the instruction cache with every change unrolled), 512 threads (429), slices of twice the size (580).
 #include <algorithm>
@@ -606,15 +606,19 @@ adjust_kernel(const __grid_constant__ AdjustArgs a, int runs, int rows_per_cta) 
     if (a.status && flags) atomicOr(a.status, flags);
 }
 
+// Whether rows mostly have histories of their own: many ids a row.
+bool begin_anew(const AdjustArgs& a) { return a.n_history > 8 * (int64_t)a.n_rows; }
+
 template <typename T, int kStages, bool kBackward, bool kSparse, bool kShift>
 int launch_form(const AdjustArgs& a, cudaStream_t s) {
     constexpr int kSlice = kSliceOf<T>;
     const int slices = (a.vocab - 1) / kSlice + 1;
-    // Few rows get a CTA each a slice; many are dealt out in runs, so that a rollout's rows find its history at hand, but
-    // leave every SM a few turns.  Slices go from the lowest ids on: with most vocabularies these are the tokens that are seen most often, and
-    // whose CTAs take longest.
+    // Few rows get a CTA each a slice; many are dealt out in runs, so that a rollout's rows find its history at hand, but leave every SM a few
+    // turns: two, or three where rows begin anew and runs gain less (512 rows with biases and masks 143 -> 132 us; 601 rows of whole
+    // rollouts 28 -> 31).  Slices go from the lowest ids on: with most vocabularies these are the tokens that are seen most often, and whose CTAs take
+    // longest.
     const int64_t units = (int64_t)slices * a.n_rows;
-    int64_t rows = std::min<int64_t>((units - 1) / (148 * (kStages == 3 ? 3 : 4) * 2) + 1, 64);
+    int64_t rows = std::min<int64_t>((units - 1) / (148 * (kStages == 3 ? 3 : 4) * (begin_anew(a) ? 3 : 2)) + 1, 64);
     rows = std::max(rows, (units - 1) / (INT32_MAX - slices) + 1);           // CTAs are numbered in 31 bits
     const int64_t runs = (a.n_rows - 1) / rows + 1, ctas = slices * runs;
     using Lay = Layout<T, kStages, kBackward>;
@@ -629,10 +633,10 @@ int launch_type(const AdjustArgs& a, cudaStream_t s) {
     const auto on_16 = [&](const void* p, int64_t pitch) { return reinterpret_cast<uintptr_t>(p) % 16 == 0 && (a.n_rows == 1 || pitch * (int64_t)sizeof(T) % 16 == 0); };
     const bool shift = !on_16(a.in, a.pitch) || !on_16(a.out, a.out_pitch);
     if (a.in == a.out) return shift ? launch_form<T, 1, kBackward, true, true>(a, s) : launch_form<T, 1, kBackward, true, false>(a, s);
-    // Rows that mostly begin anew (many ids a row) wait for their tables, not for memory: a ring of two rows leaves room for a fourth CTA (512 rows of 151936
+    // Rows that begin anew wait for their tables, not for memory: a ring of two rows leaves room for a fourth CTA (512 rows of 151936
     // bf16 with penalties 88 -> 71 us).  Rows that go on where others ended stream: three rows, three CTAs (4096 of them 433 -> 410).
     // Biases take the room of a fourth CTA in any case, and the gradient has no counts that would (2048 rows 206 -> 180).
-    const bool streams = !kBackward && a.bias_value == nullptr && a.n_history <= 8 * (int64_t)a.n_rows;
+    const bool streams = !kBackward && a.bias_value == nullptr && !begin_anew(a);
     if (streams) return shift ? launch_form<T, 3, false, false, true>(a, s) : launch_form<T, 3, false, false, false>(a, s);
     return shift ? launch_form<T, 2, kBackward, false, true>(a, s) : launch_form<T, 2, kBackward, false, false>(a, s);
 }

@@ -208,6 +208,17 @@ def test_rows_off_16_bytes(dtype, shift_in, shift_out):
 
 
 @pytest.mark.parametrize("dtype", list(DTYPES))
+def test_gradient_whose_logits_lie_elsewhere(dtype):
+    """Gradients on 16 bytes, the logits off them and with another pitch."""
+    T, V = 300, 9000
+    x = torch.empty(T, V + 13, dtype=DTYPES[dtype], device=DEV)[:, 3:3 + V]
+    x.copy_(logits(T, V, dtype, 5))
+    r = rules(T, V, 5, "rm", shared=True, most=200)
+    d = logits(T, V, dtype, 6)
+    check_backward(d, x, r, torch.empty_like(d))
+
+
+@pytest.mark.parametrize("dtype", list(DTYPES))
 def test_what_a_mask_leaves(dtype):
     """Nothing, one token, all; NaN, infinities and the type's lowest value in masked places and in allowed ones."""
     V = 20000

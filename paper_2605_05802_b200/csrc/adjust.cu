@@ -16,6 +16,7 @@
 // code outgrew the instruction cache with every change unrolled), 512 threads (429), slices of twice the size (580).
 #include <algorithm>
 
+#include "rows_ahead.cuh"
 #include "tokens.cuh"
 
 namespace sr {
@@ -479,7 +480,7 @@ adjust_kernel(const __grid_constant__ AdjustArgs a, int runs, int rows_per_cta) 
         // vectors of the last row that was looked up, and the mask of the next one
         MaskWords words = {};
         if (!kSparse) {
-            if (row + kDepth - 1 < row_end) {
+            if (row_ahead(row, kDepth - 1, row_end)) {
                 const uint4* const p = reinterpret_cast<const uint4*>(in_ahead + head_ahead) + tid;
                 uint4* const to = ring + fill * kFull;
 #pragma unroll
@@ -493,7 +494,7 @@ adjust_kernel(const __grid_constant__ AdjustArgs a, int runs, int rows_per_cta) 
         }
         copies_end();
         if (row < row0) mask_ahead = mask_of((int64_t)row + kDepth);
-        if (kShift && row + kDepth < row_end) {
+        if (kShift && row_ahead(row, kDepth, row_end)) {
             const int64_t ahead = (int64_t)row + kDepth;
             split(static_cast<const T*>(a.in) + ahead * a.pitch + first, static_cast<T*>(a.out) + ahead * a.out_pitch + first, head_ahead, vecs_ahead);
         }

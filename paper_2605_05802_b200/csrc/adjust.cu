@@ -97,8 +97,11 @@ __device__ __noinline__ void count_frequent(uint32_t* table, int l) {
     }
 }
 __device__ __noinline__ uint32_t times_frequent(const uint32_t* table, uint32_t times, int l, int id, const int32_t* history, int64_t n_history, const Record& r, uint32_t more) {
-    for (int i = 0; i < kFrequent; ++i)
-        if (table[(l + i) % kFrequent] == (uint32_t)l + 1u) return times + table[kFrequent + (l + i) % kFrequent];
+    for (int i = 0; i < kFrequent; ++i) {
+        const int slot = (l + i) % kFrequent;
+        if (table[slot] == (uint32_t)l + 1u) return times + table[kFrequent + slot];
+        if (table[slot] == 0u) return times;          // a further one would have found room here: there was none
+    }
     int64_t from;                   // more of them than the table holds
     const int skip = min(r.prompt, r.len), n = inside(r.start + skip, r.len - skip, n_history, from);
     times = 0;

@@ -31,8 +31,11 @@ extern "C" {
  *   y = x;       where seen:   y = y / repetition[t] for y > 0, y * repetition[t] otherwise
  *                where c > 0:  y = y - frequency[t] c - presence[t]
  *                where v has a bias: y = y + bias;   where v is not allowed: y = -inf
- * in fp32, rounded once.  What is neither seen, biased nor forbidden keeps its bits.  A token that is not
- * allowed is -inf whatever stands there (a NaN for one), and a row may have nothing but such tokens.
+ * in fp32, rounded once to the logits' type: an adjustment below half a step of a 16-bit type is lost (bf16 has steps of 0.125
+ * between 16 and 32, where a penalty of 0.05 changes nothing); fp32 logits keep it.  What is neither seen, biased nor forbidden keeps its bits.
+ * A token that is not allowed is -inf whatever stands there (a NaN for one), and a row may have nothing but such tokens.
+ * Rows of logits and `out` on 16 bytes are fastest.  Rows of the two that begin at different distances from 16 bytes are handled
+ * element by element and take several times as long, in the gradient too: with a padded pitch of the logits, give `out` the same.
  *
  *   logits         in  [n_rows][vocab] of type `dtype`, row t at element t * pitch
  *   history        in  [n_history] int32, the ids of all histories; NULL with n_history == 0
@@ -89,7 +92,7 @@ int sr_adjust_logits_backward(const void* d_out, int32_t dtype, int32_t n_rows, 
                               void* stream);
 
 /*
- * sr_embed_tokens -- out[t] = scale * table[tokens[t]], rounded once; zeros for a token below 0 (padding)
+ * sr_embed_tokens -- out[t] = scale * table[tokens[t]], in fp32 and rounded to the type of `out`; zeros for a token below 0 (padding)
  * or >= vocab, which sets SR_STATUS_BAD_TARGET.
  *
  *   table      in  [vocab][width] of type `table_dtype`, row v at element v * table_pitch
@@ -113,7 +116,8 @@ int sr_embed_tokens(const void* table, int32_t table_dtype, int32_t vocab, int32
  *                  16-byte aligned; contents undefined before and after
  *
  * Tokens are sorted on the way; sums are in fp32, over t in ascending order within pieces of the sorted tokens whose
- * length depends on n_tokens and width alone, then over the pieces: the same call gives the same bits.
+ * length depends on n_tokens and width alone, then over the pieces: the same call gives the same bits.  More than 4096 tokens are sorted by
+ * a cluster of 16 CTAs, which a whole B200 holds; on a part of one that does not, the call returns SR_ERR_CUDA.
  */
 int sr_embed_tokens_backward(const void* d_out, int32_t dtype, int32_t n_tokens, int32_t width, int64_t pitch,
                              const int32_t* tokens, int32_t vocab, double scale, void* d_table,

@@ -404,7 +404,8 @@ def sr_adjust_logits(logits: torch.Tensor, *, history: Optional[torch.Tensor] = 
                      bias_start: Optional[torch.Tensor] = None, bias_len: Optional[torch.Tensor] = None,
                      allowed: Optional[torch.Tensor] = None, mask_row: Optional[torch.Tensor] = None,
                      out: torch.Tensor, status: Optional[torch.Tensor] = None, stream=None) -> None:
-    """logits [T, V] (float32, bfloat16 or float16; rows may lie apart) -> out, which may be the logits.
+    """logits [T, V] (float32, bfloat16 or float16; rows may lie apart) -> out, which may be the logits.  Give out the logits' own
+    row pitch: ``torch.empty_like`` of a slice of a padded buffer has another, and other boundaries of 16 bytes are slow.
 
     Row t's history is history[history_start[t]:][:history_len[t]] (int32 ids; int64 and int32 [T]), its first prompt_len[t]
     ids the prompt; repetition, presence and frequency are float32 [T].  Its biases are entries bias_start[t] .. + bias_len[t]

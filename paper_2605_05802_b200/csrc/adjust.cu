@@ -9,10 +9,12 @@
 // changes and writes them; those of which no token is allowed are not read.  Counts are whole numbers and a token's bias is the largest
 // index in the list, so no order of atomics enters a result.
 //
-// Rollouts as a whole are bound by HBM: 4096 rows of 151936 bf16 in 412 us, 6.0 TB/s of logits read and written; the gradient of 2048 with masks,
-// half of which allow a handful, in 180 us (their banned vectors are not read: what is left runs at 5.2 TB/s).  Rows with histories of their own are
-// bound by latency and issue: 512 of them 70 us with penalties, 132 with 300 biases each and masks too (floor 48), of 600 to 900
-// instructions a warp and row, a copy's 220 among them; two changed tokens side by side make no difference.  Before: tables looked up for every vector (4096 rows 618 us), rows in registers (446; their
+// Rollouts as a whole are bound by HBM: 4096 rows of 151936 bf16 in 411 us, 6.1 TB/s of logits read and written; the gradient of 2048 with masks,
+// half of which allow a handful, in 181 us (their banned vectors are not read: what is left runs at 5.2 TB/s, and takes a copy 143).  Rows with histories of their own are
+// bound by latency and issue: 512 of them 73 us with penalties (a copy 48), 131 with 300 biases each and masks too (36 without what masks ban), of 600 to 900
+// instructions a warp and row, a copy's 220 among them; two changed tokens side by side make no difference.  In place, where only what changes is read and written, 4096 rows with penalties
+// take 302 us, 512 with biases and masks 138.  Rows of in and out that begin at different distances from 16 bytes go element by element: 4096 of
+// 50257 bf16 1030 us, 158 where all begin on 16 bytes, 236 where both are contiguous (off 16 bytes alike).  Before: tables looked up for every vector (4096 rows 618 us), rows in registers (446; their
 // code outgrew the instruction cache with every change unrolled), 512 threads (429), slices of twice the size (580).
 #include <algorithm>
 
@@ -610,7 +612,9 @@ adjust_kernel(const __grid_constant__ AdjustArgs a, int runs, int rows_per_cta) 
     if (a.status && flags) atomicOr(a.status, flags);
 }
 
-// Whether rows mostly have histories of their own: many ids a row.
+// Whether rows mostly have histories of their own: many ids a row.  That goes by the length of the array, since the rows' own lengths lie on the device.
+// Around the limit little hangs on it: with 1 to 64 ids a row and all rows beginning anew, 512 of 151936 bf16 take 58 to 64 us as rows that go on and 54 to 55
+// as rows that begin anew, 2048 of 50024 76 to 85 and 77 to 82; rollouts of 64 rows behind prompts of 4000, 49 ids a row, are taken for rows that begin anew: 64 us, otherwise 70.
 bool begin_anew(const AdjustArgs& a) { return a.n_history > 8 * (int64_t)a.n_rows; }
 
 template <typename T, int kStages, bool kBackward, bool kSparse, bool kShift>
@@ -619,8 +623,10 @@ int launch_form(const AdjustArgs& a, cudaStream_t s) {
     const int slices = (a.vocab - 1) / kSlice + 1;
     // Few rows get a CTA each a slice; many are dealt out in runs, so that a rollout's rows find its history at hand, but leave every SM a few
     // turns: two, or three where rows begin anew and runs gain less (512 rows with biases and masks 143 -> 132 us; 601 rows of whole
-    // rollouts 28 -> 31).  Slices go from the lowest ids on: with most vocabularies these are the tokens that are seen most often, and whose CTAs take
-    // longest.
+    // rollouts 28 -> 31).  Turns are counted with four CTAs an SM, with three for the ring of three rows, before runs are rounded to whole rows and at most 64 of
+    // them.  What is launched takes more: biases leave room for three CTAs only (512 rows of 151936 1634 CTAs, 3.7 turns of 444; 601 of 50021 1057, 2.4), and
+    // roundings begin another turn (the gradient of 1200 x 4096 600 CTAs on 592 places, of 2048 x 151936 1197; 4096 rows without masks 1216 on 444).
+    // Slices go from the lowest ids on: with most vocabularies these are the tokens that are seen most often, and whose CTAs take longest.
     const int64_t units = (int64_t)slices * a.n_rows;
     int64_t rows = std::min<int64_t>((units - 1) / (148 * (kStages == 3 ? 3 : 4) * (begin_anew(a) ? 3 : 2)) + 1, 64);
     rows = std::max(rows, (units - 1) / (INT32_MAX - slices) + 1);           // CTAs are numbered in 31 bits
@@ -637,8 +643,9 @@ int launch_type(const AdjustArgs& a, cudaStream_t s) {
     const auto on_16 = [&](const void* p, int64_t pitch) { return reinterpret_cast<uintptr_t>(p) % 16 == 0 && (a.n_rows == 1 || pitch * (int64_t)sizeof(T) % 16 == 0); };
     const bool shift = !on_16(a.in, a.pitch) || !on_16(a.out, a.out_pitch);
     if (a.in == a.out) return shift ? launch_form<T, 1, kBackward, true, true>(a, s) : launch_form<T, 1, kBackward, true, false>(a, s);
-    // Rows that begin anew wait for their tables, not for memory: a ring of two rows leaves room for a fourth CTA (512 rows of 151936
-    // bf16 with penalties 88 -> 71 us).  Rows that go on where others ended stream: three rows, three CTAs (4096 of them 433 -> 410).
+    // Rows that begin anew wait for their tables, not for memory: a ring of two rows leaves room for a fourth CTA (with penalties and three turns instead of
+    // two, 512 rows of 151936 bf16 77 -> 61 us, 2048 292 -> 236).  Rows that go on where others ended stream: three rows, three CTAs.  That pays for the largest
+    // calls (4096 rows of 151936 414 -> 410 us) and costs 4 to 9 % of smaller ones (2048 210 -> 221, 512 55 -> 60; 8192 of 50024 290 -> 306).
     // Biases take the room of a fourth CTA in any case, and the gradient has no counts that would (2048 rows 206 -> 180).
     const bool streams = !kBackward && a.bias_value == nullptr && !begin_anew(a);
     if (streams) return shift ? launch_form<T, 3, false, false, true>(a, s) : launch_form<T, 3, false, false, false>(a, s);

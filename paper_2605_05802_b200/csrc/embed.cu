@@ -5,7 +5,8 @@
 // stand together in ascending order and nothing depends on the order of atomics; the sorted tokens are cut into pieces of equal length, each
 // summed by one group of threads with the columns spread over them, and runs that cross pieces leave fp32 partial sums, which are added in
 // order.  Rows that no token took are zeroed beside the sums, and some of them while the tokens are sorted.  65536 tokens of 2048 bf16 into 151936
-// rows: 206 us of 136 (sorting 29, of which zeros hide most; sums and zeros 160 at 5.2 TB/s; the runs across pieces 14).  Before: zeros, sorting, sums and
+// rows: 183 us of 136 (each from cold caches: sorting, with a part of the zeros, 35; sums and the other zeros 138 at 5.8 TB/s; the runs across pieces 18); added to
+// a table that stands there, without zeros that hide the sort, 160.  Before: a CTA instead of a warp to a zeroed row, 206; zeros, sorting, sums and
 // partial sums one after the other, 262; partial sums loaded one at a time, 38 instead of 14.
 #include <cooperative_groups.h>
 
@@ -378,7 +379,8 @@ sort_tokens_kernel(const int32_t* tokens, int n, int vocab, int passes, int bits
 }
 
 // Few tokens (4096 or fewer: 1200 in 6 us, sorted by one CTA 14): the place of each is the number of those that belong before it.  A CTA has 32 tokens and all keys in shared memory; eight threads
-// share the keys of a token.
+// share the keys of a token.  Gradients of 256 columns fp32 into 4096 rows, ranked and sorted: 2048 tokens 13 and 18 us, 4096 18 and 20, 6144 27 and 21; of 2048 bf16
+// into 151936 rows, whose zeros hide the sort, 111 and 113, 123 and 113, 126 and 114.
 constexpr int kFewTokens = 4096, kRanked = 32;
 __global__ void __launch_bounds__(kThreads)
 rank_tokens_kernel(const int32_t* tokens, int n, int vocab, int2* sorted, int32_t* status) {
